@@ -41,17 +41,19 @@ C4_HEADLINE = 2            # index of 10 % in the C4 budget sweep
 # kernels and sources behind each entry point (the counter summaries are tied to them)
 ENTRY = {
     "sparse_attn": ("k_attn_stream<sparse> + k_attn_merge",
-                    ("attention.hip", "score_unit.h", "topk.h", "common.h", "wave.h")),
+                    ("attention.hip", "attention_split.h", "score_unit.h", "topk.h", "common.h",
+                     "wave.h")),
     "dense_attn": ("k_attn_stream<dense> + k_attn_merge",
-                   ("attention.hip", "score_unit.h", "topk.h", "common.h", "wave.h")),
+                   ("attention.hip", "attention_split.h", "score_unit.h", "topk.h", "common.h",
+                    "wave.h")),
     "append_score_topk": ("k_page_score + k_topk, or k_score_select (with append)",
                           ("score_topk.hip", "score_unit.h", "topk.h", "common.h", "wave.h")),
     "score_topk": ("k_page_score + k_topk, or k_score_select",
                    ("score_topk.hip", "score_unit.h", "topk.h", "common.h", "wave.h")),
     "decode_step": ("k_decode_unit, or k_page_score (with append) + k_select_attn_unit, or "
                     "the kernels of append_score_topk + k_attn_stream<sparse> + k_attn_merge",
-                    ("score_topk.hip", "score_unit.h", "attention.hip", "topk.h", "common.h",
-                     "wave.h")),
+                    ("score_topk.hip", "score_unit.h", "attention.hip", "attention_split.h",
+                     "topk.h", "common.h", "wave.h")),
     "append": ("k_append_kv", ("append.hip", "common.h")),
 }
 

@@ -31,6 +31,7 @@
 // The softmax runs in the log2 domain (scale * log2(e) folded into one multiply).
 #include <atomic>
 
+#include "attention_split.h"
 #include "common.h"
 #include "score_unit.h"
 #include "topk.h"
@@ -39,34 +40,11 @@
 namespace sparrow {
 namespace {
 
-constexpr int kAttnThreads = 256;
-constexpr int kAttnWaves = kAttnThreads / 64;
-constexpr int kBatch = 64;        // pages per prefetched page-list batch
-constexpr int kMaxWaves = 4096;   // upper bound of streaming waves (sizes the workspace)
 // Streaming waves per (sequence, KV head) unit, on average: at most, and up to which a wave may
 // have a single 16-token chunk (with at most kFewRows query-head rows in the batch, else half).
 constexpr int kUnitSegments = 256;
 constexpr int kFineSegments = 128;
 constexpr int kFewRows = 32;
-
-struct AttnArgs {
-    const uint16_t *q;
-    const uint16_t *k_cache;
-    const uint16_t *v_cache;
-    const int32_t *block_table;
-    const int32_t *seq_lens;
-    const int32_t *ksel;
-    const int32_t *idx;
-    int32_t *plan_off;    // [batch + 1] page offsets of the sequences (written by workgroup 0)
-    int32_t *unit_waves;  // [batch * num_kv_heads][2] first and last wave of each unit
-    float *o_part;
-    float *ml_part;
-    void *out;
-    int k_max, batch, num_q_heads, num_kv_heads, ps, max_pages, out_bf16;
-    int max_waves, fine_waves;  // streaming waves at most; and with single chunks (see k_attn_stream)
-    int64_t num_phys;  // physical pages in the caches
-    float scale_log2;
-};
 
 struct Chunk {
     u32x4_t k[4];  // A operand of the 4 QK instructions
@@ -84,128 +62,6 @@ __device__ __forceinline__ void load_chunk(Chunk &c, const uint16_t *__restrict_
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         c.v[j] = ld16_nt(vp + j * kHeadDim);
-}
-
-// Element `c` (0..7) of two 8 x bf16 vectors, packed as (x[c], y[c]).
-__device__ __forceinline__ uint32_t pair_of(u32x4_t x, u32x4_t y, int c)
-{
-    const uint32_t a = x[c >> 1], b = y[c >> 1];
-    return (c & 1) ? __builtin_amdgcn_perm(b, a, 0x07060302u)
-                   : __builtin_amdgcn_perm(b, a, 0x05040100u);
-}
-
-__device__ __forceinline__ void store_out(void *out, int out_bf16, int64_t i, float v)
-{
-    if (out_bf16)
-        static_cast<uint16_t *>(out)[i] = (uint16_t)to_bf16_bits(v);
-    else
-        static_cast<float *>(out)[i] = v;
-}
-
-// Pages in the attention list of sequence b.
-template <bool kSparse>
-__device__ __forceinline__ int list_pages(const AttnArgs &a, int b)
-{
-    const int L = clamp_len(a.seq_lens[b], a.ps, a.max_pages);
-    const int n = (L + a.ps - 1) / a.ps;
-    if (!kSparse)
-        return n;
-    const int c = a.ksel[b];
-    return c < 0 ? 0 : (c > a.k_max ? a.k_max : c);
-}
-
-// Block-wide exclusive prefix of list_pages over the batch into s_off[0 .. batch].
-template <bool kSparse>
-__device__ void seq_prefix(const AttnArgs &a, int32_t *s_off, int32_t *s_tmp)
-{
-    const int tid = threadIdx.x;
-    const int lane = tid & 63;
-    const int wave = tid >> 6;
-    const int B = a.batch;
-    const int per = (B + kAttnThreads - 1) / kAttnThreads;
-    const int b0 = min(B, tid * per);
-    const int b1 = min(B, b0 + per);
-    int local = 0;
-    for (int b = b0; b < b1; ++b)
-        local += list_pages<kSparse>(a, b);
-    const int incl = (int)wave_scan_add((uint32_t)local);  // totals < 2^31 (max batch x pages)
-    if (lane == 63)
-        s_tmp[wave] = incl;
-    __syncthreads();
-    int run = incl - local;
-    for (int w = 0; w < wave; ++w)
-        run += s_tmp[w];
-    for (int b = b0; b < b1; ++b) {
-        s_off[b] = run;
-        run += list_pages<kSparse>(a, b);
-    }
-    if (tid == kAttnThreads - 1)
-        s_off[B] = run;  // this thread's range ends at B (or is empty): run is the total
-    __syncthreads();
-}
-
-// Position cursor over the (sequence, head, page) list.
-struct Cursor {
-    int b, h, j, cnt;  // sequence, KV head, page position within the unit, unit length
-    int64_t pos;       // global position
-};
-
-// One page-list batch of at most kBatch pages of one unit; lane i describes page j0 + i.
-struct Batch {
-    int b, h, j0, n, L;
-    bool ends_unit;
-    int lp;    // logical page (-1: none)
-    int phys;  // physical page, as the block table gives it (checked when used)
-    int tok0;  // first token of the page
-};
-
-// A page-list batch is fetched in two phases so that no wait on its loads drains the K/V
-// loads in flight (a wave's loads complete in order): fetch_batch_begin issues the index
-// loads and advances the cursor; fetch_batch_end, called one chunk later, when the
-// indices have arrived, issues the block-table loads, which are consumed a batch later.
-template <bool kSparse>
-__device__ __forceinline__ void fetch_batch_begin(const AttnArgs &a, const int32_t *s_off,
-                                                  Cursor &c, int64_t pos_end, Batch &t, int lane)
-{
-    const int Hkv = a.num_kv_heads;
-    t.b = c.b;
-    t.h = c.h;
-    t.j0 = c.j;
-    const int64_t left = pos_end - c.pos;
-    int n = c.cnt - c.j;
-    if (n > kBatch)
-        n = kBatch;
-    if (n > left)
-        n = (int)left;
-    t.n = n;
-    t.ends_unit = c.j + n == c.cnt;
-    t.L = clamp_len(a.seq_lens[c.b], a.ps, a.max_pages);
-    t.lp = -1;
-    if (lane < n)
-        t.lp = kSparse ? a.idx[((int64_t)c.b * Hkv + c.h) * a.k_max + c.j + lane] : c.j + lane;
-    c.pos += n;
-    c.j += n;
-    if (c.j == c.cnt && c.pos < pos_end) {  // next unit with pages
-        c.j = 0;
-        if (++c.h == Hkv) {
-            c.h = 0;
-            do {
-                ++c.b;
-            } while (s_off[c.b + 1] == s_off[c.b]);
-        }
-        c.cnt = s_off[c.b + 1] - s_off[c.b];
-    }
-}
-
-__device__ __forceinline__ void fetch_batch_end(const AttnArgs &a, Batch &t)
-{
-    const int np = (t.L + a.ps - 1) / a.ps;
-    t.phys = -1;
-    t.tok0 = 0;
-    if (t.lp >= 0 && t.lp < np) {  // entries outside the sequence: no page
-        t.phys = a.block_table[(int64_t)t.b * a.max_pages + t.lp];
-        t.tok0 = t.lp * a.ps;
-    }
 }
 
 // One live 16-token chunk into a wave's online-softmax state: logits on MFMA, the running
@@ -1173,6 +1029,19 @@ bool attention_unit_path(const sparrow_shape_t &s, int64_t list_bound)
            list_bound * s.page_size <= kUnitMaxTokens && s.max_pages_per_seq <= kUnitBtLds;
 }
 
+hipError_t launch_attn_merge(const AttnArgs &a, hipStream_t stream)
+{
+    const int64_t units = (int64_t)a.batch * a.num_kv_heads;
+    const int rows = a.batch * a.num_q_heads;
+    if (units <= kWideMaxUnits && rows <= kWideMaxRows)
+        hipLaunchKernelGGL(k_attn_merge_wide, dim3((unsigned)rows), dim3(kWideThreads), 0, stream,
+                           a);
+    else
+        hipLaunchKernelGGL(k_attn_merge, dim3((rows + kMergeRows - 1) / kMergeRows),
+                           dim3(kMergeThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_attention(const sparrow_shape_t &s, const AttnPlan &plan, const void *q,
                             const void *k_cache, const void *v_cache, const int32_t *block_table,
                             const int32_t *seq_lens, const int32_t *k, const int32_t *idx,
@@ -1201,14 +1070,7 @@ hipError_t launch_attention(const sparrow_shape_t &s, const AttnPlan &plan, cons
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    const int rows = s.batch * s.num_q_heads;
-    if (units <= kWideMaxUnits && rows <= kWideMaxRows)
-        hipLaunchKernelGGL(k_attn_merge_wide, dim3((unsigned)rows), dim3(kWideThreads), 0, stream,
-                           a);
-    else
-        hipLaunchKernelGGL(k_attn_merge, dim3((rows + kMergeRows - 1) / kMergeRows),
-                           dim3(kMergeThreads), 0, stream, a);
-    return hipGetLastError();
+    return launch_attn_merge(a, stream);
 }
 
 hipError_t launch_select_attention(const sparrow_shape_t &s, const void *q, const void *k_cache,
