@@ -403,6 +403,55 @@ int sparrow_tail_stats(int64_t num_tokens, const float *alpha, const int32_t *po
                        double *mean, int64_t *count, void *stream);
 
 /*
+ * RMS norm of every query and key head and the position rotation, in one pass: what stands
+ * between a layer's projections and the decode step (the workloads' models normalise each head).
+ *
+ * For every token t < num_tokens with positions[t] >= 0, every head j of q (num_q_heads of them,
+ * weight w = q_weight) and of k (num_k_heads, w = k_weight), with x its row of 128 channels:
+ *     r = 1 / sqrt(mean(x^2) + eps),  n_i = x_i r w_i,  a_i = positions[t] * inv_freq[i]
+ *     y_i = n_i cos a_i - n_{i+64} sin a_i,  y_{i+64} = n_{i+64} cos a_i + n_i sin a_i   (i < 64)
+ * written to q_out, k_out.  fp32 arithmetic (the angle in fp64), one rounding to bf16.  Rows of a
+ * token with a negative position (padding) are left as they were.  inv_freq holds any
+ * frequencies, in radians per token, scaled ones included.  The sum of squares is fp32: rows with
+ * entries beyond 1e18 overflow it.
+ *
+ * Arguments: num_tokens >= 0; 1 <= num_q_heads, num_k_heads <= 1024; head_dim == 128; q, k (device
+ * bf16; head j of token t starts at t * stride + j * 128 elements; the strides are multiples of 8 and
+ * at least num_heads * 128, so that both may lie in one fused projection output); q_weight, k_weight
+ * (device bf16 [128]); inv_freq (device fp64 [64], 8-byte aligned); positions (device int32
+ * [num_tokens]); eps >= 0; q_out, k_out (device bf16 [num_tokens][num_heads][128], written; either
+ * may be its input where that is contiguous); stream.
+ * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED (head_dim), SPARROW_EHIP.
+ */
+int sparrow_qk_norm_rope(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
+                         int32_t head_dim, const void *q, int64_t q_stride, const void *k,
+                         int64_t k_stride, const void *q_weight, const void *k_weight,
+                         const double *inv_freq, const int32_t *positions, float eps,
+                         void *q_out, void *k_out, void *stream);
+
+/*
+ * Gradient of sparrow_qk_norm_rope.  With dy a row of dq_out or dk_out and g its rotation by the
+ * negative angle, u_i = g_i w_i:
+ *     dx_i = r (u_i - x_i r mean(u x r)),   dw_i = sum over tokens and heads of g_i x_i r
+ * dx goes to dq, dk (bf16, strided like q and k, so that both may lie in one buffer; either may
+ * be the array it derives from, with the same strides), dw to dq_weight, dk_weight (fp32 [128]
+ * each, overwritten; fp32 sums in an order that depends on the sizes alone).  Tokens with a
+ * negative position get dx = 0 and add nothing to dw.
+ *
+ * Arguments: as above; dq_out, dk_out (device bf16 [num_tokens][num_heads][128]); workspace of at
+ * least SPARROW_ROPE_WORKSPACE_BYTES (device, scratch of this call); stream.
+ * Errors: as above, plus SPARROW_EWORKSPACE.
+ */
+#define SPARROW_ROPE_WORKSPACE_BYTES 1048576
+int sparrow_qk_norm_rope_bwd(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
+                             int32_t head_dim, const void *dq_out, const void *dk_out,
+                             const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                             const void *q_weight, const void *k_weight, const double *inv_freq,
+                             const int32_t *positions, float eps, void *dq, int64_t dq_stride,
+                             void *dk, int64_t dk_stride, float *dq_weight, float *dk_weight,
+                             void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * Read-only streaming reference (a measurement helper, not a step of the method): reads
  * `bytes` bytes at src once, with the 16-byte non-temporal vector loads and the
  * consecutive-lanes layout of the decode-step kernels, from a grid that keeps every

@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "common.h"
+#include "qk_norm_rope.h"
 
 using namespace sparrow;
 
@@ -44,6 +45,42 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t decode_step_workspace(const sparrow_shape_t &s)
 {
     return round256(score_topk_workspace(s)) + plan_attention(s).workspace_bytes;
+}
+
+bool al8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
+// Token strides of rows of `heads` heads: rows may not overlap and start on 16 bytes.
+bool row_stride_ok(int64_t stride, int heads)
+{
+    return stride % 8 == 0 && stride >= (int64_t)heads * kHeadDim;
+}
+
+// Shared by sparrow_qk_norm_rope and its gradient; fills `a` where the arguments are fine.
+int rope_args(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads, int32_t head_dim,
+              const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+              const void *q_weight, const void *k_weight, const double *inv_freq,
+              const int32_t *positions, float eps, RopeArgs &a)
+{
+    if (num_tokens < 0 || num_tokens > 0x7fffffff || num_q_heads < 1 || num_k_heads < 1 ||
+        num_q_heads > 1024 || num_k_heads > 1024)
+        return SPARROW_EINVAL;
+    if (head_dim != kHeadDim)
+        return SPARROW_EUNSUPPORTED;
+    if (!q || !k || !q_weight || !k_weight || !inv_freq || !positions)
+        return SPARROW_EINVAL;
+    if (!al16(q) || !al16(k) || !al16(q_weight) || !al16(k_weight) || !al8(inv_freq) ||
+        !al4(positions))
+        return SPARROW_EINVAL;
+    if (!row_stride_ok(q_stride, num_q_heads) || !row_stride_ok(k_stride, num_k_heads) ||
+        !(eps >= 0.f) || !std::isfinite(eps))
+        return SPARROW_EINVAL;
+    a = RopeArgs{static_cast<const uint16_t *>(q),        static_cast<const uint16_t *>(k),
+                 q_stride,                                k_stride,
+                 static_cast<const uint16_t *>(q_weight), static_cast<const uint16_t *>(k_weight),
+                 inv_freq,                                positions,
+                 num_tokens,                              num_q_heads,
+                 num_k_heads,                             eps};
+    return SPARROW_OK;
 }
 
 }  // namespace
@@ -356,6 +393,62 @@ int sparrow_tail_stats(int64_t num_tokens, const float *alpha, const int32_t *po
     return status_of(launch_tail_stats(num_tokens, alpha, positions, bin_tokens, n_bins,
                                        percentile, quantile, mean, count,
                                        static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_qk_norm_rope(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
+                         int32_t head_dim, const void *q, int64_t q_stride, const void *k,
+                         int64_t k_stride, const void *q_weight, const void *k_weight,
+                         const double *inv_freq, const int32_t *positions, float eps,
+                         void *q_out, void *k_out, void *stream)
+{
+    RopeArgs a;
+    const int rc = rope_args(num_tokens, num_q_heads, num_k_heads, head_dim, q, q_stride, k,
+                             k_stride, q_weight, k_weight, inv_freq, positions, eps, a);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!q_out || !k_out || !al16(q_out) || !al16(k_out))
+        return SPARROW_EINVAL;
+    if (num_tokens == 0)
+        return SPARROW_OK;
+    return status_of(launch_qk_norm_rope(a, static_cast<uint16_t *>(q_out),
+                                         static_cast<uint16_t *>(k_out),
+                                         static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_qk_norm_rope_bwd(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
+                             int32_t head_dim, const void *dq_out, const void *dk_out,
+                             const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                             const void *q_weight, const void *k_weight, const double *inv_freq,
+                             const int32_t *positions, float eps, void *dq, int64_t dq_stride,
+                             void *dk, int64_t dk_stride, float *dq_weight, float *dk_weight,
+                             void *workspace, size_t ws_bytes, void *stream)
+{
+    RopeArgs a;
+    const int rc = rope_args(num_tokens, num_q_heads, num_k_heads, head_dim, q, q_stride, k,
+                             k_stride, q_weight, k_weight, inv_freq, positions, eps, a);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!dq_out || !dk_out || !dq || !dk || !dq_weight || !dk_weight)
+        return SPARROW_EINVAL;
+    if (!al16(dq_out) || !al16(dk_out) || !al16(dq) || !al16(dk) || !al4(dq_weight) ||
+        !al4(dk_weight) || !al16(workspace))
+        return SPARROW_EINVAL;
+    if (!row_stride_ok(dq_stride, num_q_heads) || !row_stride_ok(dk_stride, num_k_heads))
+        return SPARROW_EINVAL;
+    static_assert(sizeof(float) * kRopeGradBlocks * 2 * kHeadDim == SPARROW_ROPE_WORKSPACE_BYTES,
+                  "one row of both weights per workgroup");
+    if (!workspace || ws_bytes < SPARROW_ROPE_WORKSPACE_BYTES)
+        return SPARROW_EWORKSPACE;
+    const RopeGradArgs g{static_cast<const uint16_t *>(dq_out),
+                         static_cast<const uint16_t *>(dk_out),
+                         static_cast<uint16_t *>(dq),
+                         static_cast<uint16_t *>(dk),
+                         dq_stride,
+                         dk_stride,
+                         dq_weight,
+                         dk_weight,
+                         static_cast<float *>(workspace)};
+    return status_of(launch_qk_norm_rope_bwd(a, g, static_cast<hipStream_t>(stream)));
 }
 
 int sparrow_stream_read(const void *src, int64_t bytes, uint32_t *checksum, void *stream)

@@ -11,6 +11,7 @@ visible, the tensor-level calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -40,11 +41,13 @@ SPARROW_OP_SPARSE_ATTN = 1
 SPARROW_OP_DENSE_ATTN = 2
 SPARROW_OP_DECODE_STEP = 3
 SPARROW_NOALLOC_SCRATCH_BYTES = 32 << 20
+SPARROW_ROPE_WORKSPACE_BYTES = 1 << 20
 
 EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_topk",
            "sparrow_append_score_topk", "sparrow_sparse_decode_attn", "sparrow_dense_decode_attn",
            "sparrow_acceptance_rate", "sparrow_acceptance_rate_topk", "sparrow_tail_stats",
            "sparrow_stream_read", "sparrow_sparse_decode_attn_noalloc", "sparrow_decode_step",
+           "sparrow_qk_norm_rope", "sparrow_qk_norm_rope_bwd",
            "sparrow_budget_bound", "sparrow_workspace_size", "sparrow_status_string")
 
 
@@ -105,7 +108,14 @@ def load():
     lib.sparrow_decode_step.argtypes = [sp, _p, _p, _p, _p, _p, _p, _p, _p,
                                         ctypes.POINTER(Schedule), _i32, ctypes.c_float, _p, _p,
                                         _p, _i32, _p, ctypes.c_size_t, _p]
-    for fn in EXPORTS[:12]:
+    lib.sparrow_qk_norm_rope.argtypes = [ctypes.c_int64, _i32, _i32, _i32, _p, ctypes.c_int64, _p,
+                                         ctypes.c_int64, _p, _p, _p, _p, ctypes.c_float, _p, _p,
+                                         _p]
+    lib.sparrow_qk_norm_rope_bwd.argtypes = [ctypes.c_int64, _i32, _i32, _i32, _p, _p, _p,
+                                             ctypes.c_int64, _p, ctypes.c_int64, _p, _p, _p, _p,
+                                             ctypes.c_float, _p, ctypes.c_int64, _p,
+                                             ctypes.c_int64, _p, _p, _p, ctypes.c_size_t, _p]
+    for fn in EXPORTS[:-3]:
         getattr(lib, fn).restype = ctypes.c_int
     lib.sparrow_budget_bound.argtypes = [_p, ctypes.c_int64, _i32, _i32, _i32, _p, _p, _i32, _p]
     lib.sparrow_budget_bound.restype = ctypes.c_int32
@@ -188,6 +198,23 @@ def sparrow_tail_stats(num_tokens, alpha, positions, bin_tokens, n_bins, percent
                        mean, count, stream):
     return load().sparrow_tail_stats(num_tokens, alpha, positions, bin_tokens, n_bins, percentile,
                                      quantile, mean, count, stream)
+
+
+def sparrow_qk_norm_rope(num_tokens, num_q_heads, num_k_heads, head_dim, q, q_stride, k, k_stride,
+                         q_weight, k_weight, inv_freq, positions, eps, q_out, k_out, stream):
+    return load().sparrow_qk_norm_rope(num_tokens, num_q_heads, num_k_heads, head_dim, q, q_stride,
+                                       k, k_stride, q_weight, k_weight, inv_freq, positions, eps,
+                                       q_out, k_out, stream)
+
+
+def sparrow_qk_norm_rope_bwd(num_tokens, num_q_heads, num_k_heads, head_dim, dq_out, dk_out, q,
+                             q_stride, k, k_stride, q_weight, k_weight, inv_freq, positions, eps,
+                             dq, dq_stride, dk, dk_stride, dq_weight, dk_weight, workspace,
+                             ws_bytes, stream):
+    return load().sparrow_qk_norm_rope_bwd(num_tokens, num_q_heads, num_k_heads, head_dim, dq_out,
+                                           dk_out, q, q_stride, k, k_stride, q_weight, k_weight,
+                                           inv_freq, positions, eps, dq, dq_stride, dk, dk_stride,
+                                           dq_weight, dk_weight, workspace, ws_bytes, stream)
 
 
 def sparrow_stream_read(src, nbytes, checksum, stream):
@@ -276,6 +303,13 @@ def _check(fn: str, rc: int) -> None:
 def _workspace(nbytes: int, device):
     import torch
     return torch.empty(max(int(nbytes), 16), dtype=torch.uint8, device=device)
+
+
+def _expect_workspace(t, device):
+    """Raise unless ``t`` is contiguous memory on ``device`` (its size is the library's check)."""
+    _require_device(t)
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace must be contiguous memory on {device}")
 
 
 def _require_device(t):
@@ -549,6 +583,106 @@ def tail_stats(alpha, positions, bin_tokens, n_bins, percentile=5.0):
         alpha.numel(), _ptr(alpha), _ptr(positions), int(bin_tokens), int(n_bins),
         float(percentile), _ptr(q), _ptr(m), _ptr(c), _stream(dev)))
     return q, m, c
+
+
+def _on(device):
+    """Makes ``device`` the current one for the launches inside, where it is not."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _expect_rows(t, name, shape, device):
+    """Raise unless ``t`` is bf16 ``[T][heads][128]`` on ``device`` with contiguous heads; returns
+    its token stride in elements (a view into a fused projection's output has a larger one)."""
+    import torch
+    if t is None:
+        raise ValueError(f"{name} is required")
+    _require_device(t)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {torch.bfloat16}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    st = t.stride()
+    row = shape[1] * shape[2]
+    if shape[0] <= 1:
+        st = (row, shape[2] if shape[1] <= 1 else st[1], st[2])
+    elif shape[1] <= 1:
+        st = (st[0], shape[2], st[2])
+    if st[2] != 1 or st[1] != shape[2] or st[0] < row or st[0] % 8:
+        raise ValueError(f"{name}: strides {t.stride()}, expected contiguous heads and a token "
+                         f"stride that is a multiple of 8 and at least {row}")
+    return st[0]
+
+
+def _expect_rope(q, k, q_weight, k_weight, inv_freq, positions):
+    """(tokens, query heads, key heads, token strides of q and k) of checked arguments."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [T][heads][128]")
+    dev = q.device
+    T, Hq, D = q.shape
+    Hk = k.shape[1]
+    qs, ks = _expect_rows(q, "q", (T, Hq, D), dev), _expect_rows(k, "k", (T, Hk, D), dev)
+    _expect(q_weight, "q_weight", torch.bfloat16, (D,), dev)
+    _expect(k_weight, "k_weight", torch.bfloat16, (D,), dev)
+    _expect(inv_freq, "inv_freq", torch.float64, (D // 2,), dev)
+    _expect(positions, "positions", torch.int32, (T,), dev)
+    return T, Hq, Hk, D, qs, ks
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=None, k_out=None):
+    """RMS norm of every head of q ``[T][Hq][128]`` and k ``[T][Hk][128]`` (bf16, views of a fused
+    projection welcome) with its weight, and the rotation by ``positions * inv_freq``.  Returns
+    (q_out, k_out), contiguous bf16; rows of tokens with a negative position are not written."""
+    import torch
+    T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
+    dev = q.device
+    q_out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev) if q_out is None else q_out
+    k_out = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=dev) if k_out is None else k_out
+    _expect(q_out, "q_out", torch.bfloat16, (T, Hq, D), dev)
+    _expect(k_out, "k_out", torch.bfloat16, (T, Hk, D), dev)
+    if T == 0:
+        return q_out, k_out
+    with _on(dev):
+        _check("sparrow_qk_norm_rope", sparrow_qk_norm_rope(
+            T, Hq, Hk, D, _ptr(q), qs, _ptr(k), ks, _ptr(q_weight), _ptr(k_weight),
+            _ptr(inv_freq), _ptr(positions), float(eps), _ptr(q_out), _ptr(k_out), _stream(dev)))
+    return q_out, k_out
+
+
+def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6,
+                     dq=None, dk=None, dq_weight=None, dk_weight=None, workspace=None):
+    """Gradient of ``qk_norm_rope``: (dq, dk bf16, dq_weight, dk_weight fp32 ``[128]``).  dq and dk
+    may be views into one buffer of the fused projection's gradient."""
+    import torch
+    T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
+    dev = q.device
+    _expect(dq_out, "dq_out", torch.bfloat16, (T, Hq, D), dev)
+    _expect(dk_out, "dk_out", torch.bfloat16, (T, Hk, D), dev)
+    dq = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev) if dq is None else dq
+    dk = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=dev) if dk is None else dk
+    dqs, dks = _expect_rows(dq, "dq", (T, Hq, D), dev), _expect_rows(dk, "dk", (T, Hk, D), dev)
+    dws = []
+    for name, w in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
+        w = torch.empty(D, dtype=torch.float32, device=dev) if w is None else w
+        _expect(w, name, torch.float32, (D,), dev)
+        dws.append(w)
+    if T == 0:
+        return dq, dk, dws[0].zero_(), dws[1].zero_()
+    if workspace is None:
+        workspace = _workspace(SPARROW_ROPE_WORKSPACE_BYTES, dev)
+    _expect_workspace(workspace, dev)
+    with _on(dev):
+        _check("sparrow_qk_norm_rope_bwd", sparrow_qk_norm_rope_bwd(
+            T, Hq, Hk, D, _ptr(dq_out), _ptr(dk_out), _ptr(q), qs, _ptr(k), ks, _ptr(q_weight),
+            _ptr(k_weight), _ptr(inv_freq), _ptr(positions), float(eps), _ptr(dq), dqs, _ptr(dk),
+            dks, _ptr(dws[0]), _ptr(dws[1]), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream(dev)))
+    return dq, dk, dws[0], dws[1]
 
 
 def stream_read(buf, checksum=None):
