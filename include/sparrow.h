@@ -452,6 +452,58 @@ int sparrow_qk_norm_rope_bwd(int64_t num_tokens, int32_t num_q_heads, int32_t nu
                              void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * The e4m3 cache: K and V in 8 bits, half the bytes that a decode step streams.
+ *
+ *     k_cache, v_cache  e4m3  [num_phys_pages][num_kv_heads][page_size][128]   (OCP float8 e4m3,
+ *                             no infinities)
+ *     exps              uint8 [num_phys_pages][num_kv_heads][page_size / 4][2][4]: for every four
+ *                             tokens K's four bytes, then V's
+ * A channel of a row of K (V) is code * 2^(byte - 127) with the row's byte of K (V).  From a bf16
+ * row with largest magnitude m, byte - 127 is the least integer e with m <= 448 * 2^e, clamped to
+ * [-117, 119], and code = x * 2^-e rounded to nearest even (clamped to +-448, which only a row
+ * beyond 448 * 2^119 reaches).  The scale is a power of two, so every value is exactly a bf16 number:
+ * what sparrow_read_kv_e4m3 returns is what the cache holds, and the bf16 entry points applied to
+ * it describe the 8-bit ones.
+ *
+ * sparrow_append_kv_e4m3 writes new tokens.  Sequence b's rows are cu_tokens[b] .. cu_tokens[b+1] - 1
+ * (n_b of them); they go to the positions seq_lens[b] - n_b .. seq_lens[b] - 1, and seq_lens counts
+ * them.  With cu_tokens == NULL every sequence has one row (num_tokens == batch): the decode step.
+ * The landmarks of the pages that they land on follow, from the values as the cache holds them: for
+ * a page whose slot 0 is among the new tokens they are its new tokens' min/max (or fp32 sum in
+ * token order), else the old landmarks joined with them - what sparrow_page_meta_update would make
+ * of the cache's values.  Selection (sparrow_page_score_topk) then works on meta as ever.  A
+ * sequence with seq_lens[b] < 1 or > max_pages_per_seq * page_size is left untouched, tokens before
+ * position 0 and on absent pages are dropped, and rows behind cu_tokens[batch] are not read.
+ * cu_tokens is non-decreasing; entries outside [0, num_tokens] count as the nearer end.  Sequences
+ * must use distinct physical pages.  NaN is not supported; an infinity becomes 448 * 2^119.
+ *
+ * Arguments: shape (host); k_new, v_new (device bf16: head h of row r starts at r * stride + h * 128
+ * elements; strides are multiples of 8 and at least num_kv_heads * 128); cu_tokens (device int32
+ * [batch + 1], or NULL); 0 <= num_tokens <= 134217728 (rows that k_new and v_new have); k_cache,
+ * v_cache, exps (device; caches on 16, exps on 8 bytes; updated in place); block_table, seq_lens
+ * (device); meta (device, updated); stream.
+ * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED, SPARROW_EHIP.
+ */
+int sparrow_append_kv_e4m3(const sparrow_shape_t *shape, const void *k_new, int64_t k_stride,
+                           const void *v_new, int64_t v_stride, const int32_t *cu_tokens,
+                           int64_t num_tokens, void *k_cache, void *v_cache, void *exps,
+                           const int32_t *block_table, const int32_t *seq_lens, void *meta,
+                           void *stream);
+
+/*
+ * The last n_b = cu_tokens[b+1] - cu_tokens[b] tokens of every sequence from an e4m3 cache, as bf16
+ * rows cu_tokens[b] .. of k_out and v_out [num_tokens][num_kv_heads][128] (exact).  Rows of positions
+ * before 0, past the block table or on absent pages are zeros; rows behind cu_tokens[batch] are left
+ * as they were.  cu_tokens as above (NULL: the last token of each).
+ *
+ * Errors: as above.
+ */
+int sparrow_read_kv_e4m3(const sparrow_shape_t *shape, const void *k_cache, const void *v_cache,
+                         const void *exps, const int32_t *block_table, const int32_t *seq_lens,
+                         const int32_t *cu_tokens, int64_t num_tokens, void *k_out, void *v_out,
+                         void *stream);
+
+/*
  * Read-only streaming reference (a measurement helper, not a step of the method): reads
  * `bytes` bytes at src once, with the 16-byte non-temporal vector loads and the
  * consecutive-lanes layout of the decode-step kernels, from a grid that keeps every

@@ -2,6 +2,7 @@
 // Declarations and the contract of every entry point are in include/sparrow.h.
 #include <cmath>
 
+#include "cache_e4m3.h"
 #include "common.h"
 #include "qk_norm_rope.h"
 
@@ -80,6 +81,18 @@ int rope_args(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads, int3
                  inv_freq,                                positions,
                  num_tokens,                              num_q_heads,
                  num_k_heads,                             eps};
+    return SPARROW_OK;
+}
+
+// Rows of new (or read) tokens of an e4m3 cache.
+int check_rows(const sparrow_shape_t &s, const int32_t *cu_tokens, int64_t num_tokens)
+{
+    if (num_tokens < 0 || num_tokens > (1 << 27) || !al4(cu_tokens))
+        return SPARROW_EINVAL;
+    if (cu_tokens == nullptr && num_tokens != s.batch)
+        return SPARROW_EINVAL;
+    if (s.num_kv_heads > 65535 || s.batch > (1 << 20))  // grid dimensions
+        return SPARROW_EINVAL;
     return SPARROW_OK;
 }
 
@@ -449,6 +462,62 @@ int sparrow_qk_norm_rope_bwd(int64_t num_tokens, int32_t num_q_heads, int32_t nu
                          dk_weight,
                          static_cast<float *>(workspace)};
     return status_of(launch_qk_norm_rope_bwd(a, g, static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_append_kv_e4m3(const sparrow_shape_t *shape, const void *k_new, int64_t k_stride,
+                           const void *v_new, int64_t v_stride, const int32_t *cu_tokens,
+                           int64_t num_tokens, void *k_cache, void *v_cache, void *exps,
+                           const int32_t *block_table, const int32_t *seq_lens, void *meta,
+                           void *stream)
+{
+    int rc = check_shape(shape);
+    if (rc != SPARROW_OK)
+        return rc;
+    rc = check_rows(*shape, cu_tokens, num_tokens);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!k_new || !v_new || !k_cache || !v_cache || !exps || !block_table || !seq_lens || !meta)
+        return SPARROW_EINVAL;
+    if (!al16(k_new) || !al16(v_new) || !al16(k_cache) || !al16(v_cache) || !al8(exps) ||
+        !al4(block_table) || !al4(seq_lens) || !al16(meta))
+        return SPARROW_EINVAL;
+    if (!row_stride_ok(k_stride, shape->num_kv_heads) ||
+        !row_stride_ok(v_stride, shape->num_kv_heads))
+        return SPARROW_EINVAL;
+    if (shape->batch == 0 || num_tokens == 0)
+        return SPARROW_OK;
+    const NewRows rows{static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new),
+                       k_stride, v_stride, cu_tokens, num_tokens};
+    const CacheE4m3 cache{static_cast<uint8_t *>(k_cache), static_cast<uint8_t *>(v_cache),
+                          static_cast<uint8_t *>(exps)};
+    return status_of(launch_append_e4m3(*shape, rows, cache, block_table, seq_lens, meta,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_read_kv_e4m3(const sparrow_shape_t *shape, const void *k_cache, const void *v_cache,
+                         const void *exps, const int32_t *block_table, const int32_t *seq_lens,
+                         const int32_t *cu_tokens, int64_t num_tokens, void *k_out, void *v_out,
+                         void *stream)
+{
+    int rc = check_shape(shape);
+    if (rc != SPARROW_OK)
+        return rc;
+    rc = check_rows(*shape, cu_tokens, num_tokens);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!k_cache || !v_cache || !exps || !block_table || !seq_lens || !k_out || !v_out)
+        return SPARROW_EINVAL;
+    if (!al16(k_cache) || !al16(v_cache) || !al8(exps) || !al4(block_table) || !al4(seq_lens) ||
+        !al16(k_out) || !al16(v_out))
+        return SPARROW_EINVAL;
+    if (shape->batch == 0 || num_tokens == 0)
+        return SPARROW_OK;
+    // (the kernel only reads the cache)
+    const CacheE4m3 cache{static_cast<uint8_t *>(const_cast<void *>(k_cache)),
+                          static_cast<uint8_t *>(const_cast<void *>(v_cache)),
+                          static_cast<uint8_t *>(const_cast<void *>(exps))};
+    return status_of(launch_read_e4m3(*shape, cache, block_table, seq_lens, cu_tokens, num_tokens,
+                                      k_out, v_out, static_cast<hipStream_t>(stream)));
 }
 
 int sparrow_stream_read(const void *src, int64_t bytes, uint32_t *checksum, void *stream)

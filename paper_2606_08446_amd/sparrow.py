@@ -47,7 +47,8 @@ EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_
            "sparrow_append_score_topk", "sparrow_sparse_decode_attn", "sparrow_dense_decode_attn",
            "sparrow_acceptance_rate", "sparrow_acceptance_rate_topk", "sparrow_tail_stats",
            "sparrow_stream_read", "sparrow_sparse_decode_attn_noalloc", "sparrow_decode_step",
-           "sparrow_qk_norm_rope", "sparrow_qk_norm_rope_bwd",
+           "sparrow_qk_norm_rope", "sparrow_qk_norm_rope_bwd", "sparrow_append_kv_e4m3",
+           "sparrow_read_kv_e4m3",
            "sparrow_budget_bound", "sparrow_workspace_size", "sparrow_status_string")
 
 
@@ -115,6 +116,9 @@ def load():
                                              ctypes.c_int64, _p, ctypes.c_int64, _p, _p, _p, _p,
                                              ctypes.c_float, _p, ctypes.c_int64, _p,
                                              ctypes.c_int64, _p, _p, _p, ctypes.c_size_t, _p]
+    lib.sparrow_append_kv_e4m3.argtypes = [sp, _p, ctypes.c_int64, _p, ctypes.c_int64, _p,
+                                           ctypes.c_int64, _p, _p, _p, _p, _p, _p, _p]
+    lib.sparrow_read_kv_e4m3.argtypes = [sp, _p, _p, _p, _p, _p, _p, ctypes.c_int64, _p, _p, _p]
     for fn in EXPORTS[:-3]:
         getattr(lib, fn).restype = ctypes.c_int
     lib.sparrow_budget_bound.argtypes = [_p, ctypes.c_int64, _i32, _i32, _i32, _p, _p, _i32, _p]
@@ -215,6 +219,19 @@ def sparrow_qk_norm_rope_bwd(num_tokens, num_q_heads, num_k_heads, head_dim, dq_
                                            dk_out, q, q_stride, k, k_stride, q_weight, k_weight,
                                            inv_freq, positions, eps, dq, dq_stride, dk, dk_stride,
                                            dq_weight, dk_weight, workspace, ws_bytes, stream)
+
+
+def sparrow_append_kv_e4m3(shape, k_new, k_stride, v_new, v_stride, cu_tokens, num_tokens, k_cache,
+                           v_cache, exps, block_table, seq_lens, meta, stream):
+    return load().sparrow_append_kv_e4m3(ctypes.byref(shape), k_new, k_stride, v_new, v_stride,
+                                         cu_tokens, num_tokens, k_cache, v_cache, exps,
+                                         block_table, seq_lens, meta, stream)
+
+
+def sparrow_read_kv_e4m3(shape, k_cache, v_cache, exps, block_table, seq_lens, cu_tokens,
+                         num_tokens, k_out, v_out, stream):
+    return load().sparrow_read_kv_e4m3(ctypes.byref(shape), k_cache, v_cache, exps, block_table,
+                                       seq_lens, cu_tokens, num_tokens, k_out, v_out, stream)
 
 
 def sparrow_stream_read(src, nbytes, checksum, stream):
@@ -683,6 +700,86 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positio
             dks, _ptr(dws[0]), _ptr(dws[1]), _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream(dev)))
     return dq, dk, dws[0], dws[1]
+
+
+def new_cache_e4m3(num_phys_pages, num_kv_heads, page_size, device):
+    """A zeroed e4m3 cache: (k_cache, v_cache float8_e4m3fn [P][Hkv][ps][128], exps uint8
+    [P][Hkv][ps / 4][2][4])."""
+    import torch
+    shape = (num_phys_pages, num_kv_heads, page_size, 128)
+    k, v = (torch.zeros(shape, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+            for _ in range(2))
+    return k, v, torch.zeros((num_phys_pages, num_kv_heads, page_size // 4, 2, 4),
+                             dtype=torch.uint8, device=device)
+
+
+def _expect_cache_e4m3(k_cache, v_cache, exps, block_table, seq_lens, device):
+    """e4m3 caches [P][Hkv][ps][D], exps [P][Hkv][ps / 4][2][4], block_table int32 [B][M], seq_lens
+    int32 [B].  Returns (B, Hkv, ps, D, P, M)."""
+    import torch
+    if k_cache.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("the caches must be [P][Hkv][ps][D], block_table [B][M]")
+    P, Hkv, ps, D = k_cache.shape
+    B, M = block_table.shape
+    _expect(k_cache, "k_cache", torch.float8_e4m3fn, (P, Hkv, ps, D), device)
+    _expect(v_cache, "v_cache", torch.float8_e4m3fn, (P, Hkv, ps, D), device)
+    _expect(exps, "exps", torch.uint8, (P, Hkv, ps // 4, 2, 4), device)
+    _expect(block_table, "block_table", torch.int32, (B, M), device)
+    _expect(seq_lens, "seq_lens", torch.int32, (B,), device)
+    return B, Hkv, ps, D, P, M
+
+
+def append_kv_e4m3(k_new, v_new, k_cache, v_cache, exps, block_table, seq_lens, meta,
+                   cu_tokens=None, landmark=SPARROW_LANDMARK_MINMAX):
+    """Write new tokens (bf16 rows [T][Hkv][128], views of a fused projection welcome) into an e4m3
+    cache and update their pages' landmarks, all in place.  Sequence b's rows are cu_tokens[b] ..
+    cu_tokens[b+1]-1 and end at position seq_lens[b]-1; without cu_tokens every sequence has one."""
+    import torch
+    _require_device(k_cache)
+    dev = k_cache.device
+    B, Hkv, ps, D, P, M = _expect_cache_e4m3(k_cache, v_cache, exps, block_table, seq_lens, dev)
+    if k_new.dim() != 3:
+        raise ValueError("k_new must be [T][Hkv][D]")
+    T = k_new.shape[0] if cu_tokens is not None else B
+    ks = _expect_rows(k_new, "k_new", (T, Hkv, D), dev)
+    vs = _expect_rows(v_new, "v_new", (T, Hkv, D), dev)
+    if cu_tokens is not None:
+        _expect(cu_tokens, "cu_tokens", torch.int32, (B + 1,), dev)
+    _expect_meta(meta, P, Hkv, D, landmark, dev)
+    if B == 0 or T == 0:
+        return
+    shape = make_shape(B, Hkv, Hkv, ps, M, P, D, landmark=landmark)
+    with _on(dev):
+        _check("sparrow_append_kv_e4m3", sparrow_append_kv_e4m3(
+            shape, _ptr(k_new), ks, _ptr(v_new), vs, _ptr(cu_tokens), T, _ptr(k_cache),
+            _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens), _ptr(meta),
+            _stream(dev)))
+
+
+def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_tokens, k_out=None,
+                 v_out=None):
+    """The last cu_tokens[b+1] - cu_tokens[b] tokens of every sequence from an e4m3 cache: (k_out,
+    v_out) bf16 [num_tokens][Hkv][128], exactly the values that the cache holds."""
+    import torch
+    _require_device(k_cache)
+    dev = k_cache.device
+    B, Hkv, ps, D, P, M = _expect_cache_e4m3(k_cache, v_cache, exps, block_table, seq_lens, dev)
+    T = int(num_tokens)
+    if cu_tokens is not None:
+        _expect(cu_tokens, "cu_tokens", torch.int32, (B + 1,), dev)
+    outs = []
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        t = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=dev) if t is None else t
+        _expect(t, name, torch.bfloat16, (T, Hkv, D), dev)
+        outs.append(t)
+    if B == 0 or T == 0:
+        return outs[0], outs[1]
+    shape = make_shape(B, Hkv, Hkv, ps, M, P, D)
+    with _on(dev):
+        _check("sparrow_read_kv_e4m3", sparrow_read_kv_e4m3(
+            shape, _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens),
+            _ptr(cu_tokens), T, _ptr(outs[0]), _ptr(outs[1]), _stream(dev)))
+    return outs[0], outs[1]
 
 
 def stream_read(buf, checksum=None):
