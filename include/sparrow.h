@@ -504,6 +504,32 @@ int sparrow_read_kv_e4m3(const sparrow_shape_t *shape, const void *k_cache, cons
                          void *stream);
 
 /*
+ * Decode attention of one new token per sequence over an e4m3 cache: sparrow_sparse_decode_attn and
+ * sparrow_dense_decode_attn with K and V as the cache's values,
+ *     z_t = scale * 2^(kbyte_t - 127) * (q[b][j] . kcode_t),  w = softmax(z),
+ *     out[b][j] = sum_t w_t 2^(vbyte_t - 127) vcode_t
+ * with fp32 sums; the softmax numerators enter the product with V as two bf16 numbers each (17
+ * bits).  Page lists, lengths, absent pages and empty sequences are those calls'; so is the
+ * workspace (SPARROW_OP_SPARSE_ATTN, SPARROW_OP_DENSE_ATTN).  The order of the sums depends only on the
+ * shape, k_max, the page lists and the device.
+ *
+ * Arguments: as there, with k_cache, v_cache (16-byte aligned) and exps (8-byte aligned) of an e4m3
+ * cache.
+ * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED, SPARROW_EWORKSPACE, SPARROW_EHIP.
+ */
+int sparrow_sparse_decode_attn_e4m3(const sparrow_shape_t *shape, const void *q,
+                                    const void *k_cache, const void *v_cache, const void *exps,
+                                    const int32_t *block_table, const int32_t *seq_lens,
+                                    const int32_t *k, const int32_t *idx, int32_t k_max,
+                                    float scale, void *out, int32_t out_dtype, void *workspace,
+                                    size_t ws_bytes, void *stream);
+int sparrow_dense_decode_attn_e4m3(const sparrow_shape_t *shape, const void *q,
+                                   const void *k_cache, const void *v_cache, const void *exps,
+                                   const int32_t *block_table, const int32_t *seq_lens,
+                                   float scale, void *out, int32_t out_dtype, void *workspace,
+                                   size_t ws_bytes, void *stream);
+
+/*
  * Read-only streaming reference (a measurement helper, not a step of the method): reads
  * `bytes` bytes at src once, with the 16-byte non-temporal vector loads and the
  * consecutive-lanes layout of the decode-step kernels, from a grid that keeps every

@@ -2,6 +2,7 @@
 // Declarations and the contract of every entry point are in include/sparrow.h.
 #include <cmath>
 
+#include "attention_e4m3.h"
 #include "cache_e4m3.h"
 #include "common.h"
 #include "qk_norm_rope.h"
@@ -94,6 +95,42 @@ int check_rows(const sparrow_shape_t &s, const int32_t *cu_tokens, int64_t num_t
     if (s.num_kv_heads > 65535 || s.batch > (1 << 20))  // grid dimensions
         return SPARROW_EINVAL;
     return SPARROW_OK;
+}
+
+// Shared by the two attention calls over an e4m3 cache (dense: k and idx are null, k_max 0).
+int attention_e4m3_call(bool sparse, const sparrow_shape_t *shape, const void *q,
+                        const void *k_cache, const void *v_cache, const void *exps,
+                        const int32_t *block_table, const int32_t *seq_lens, const int32_t *k,
+                        const int32_t *idx, int32_t k_max, float scale, void *out,
+                        int32_t out_dtype, void *workspace, size_t ws_bytes, void *stream)
+{
+    const int rc = check_shape(shape);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!q || !k_cache || !v_cache || !exps || !block_table || !seq_lens || !out ||
+        (sparse && (!k || !idx)))
+        return SPARROW_EINVAL;
+    if (!al16(q) || !al16(k_cache) || !al16(v_cache) || !al8(exps) || !al4(block_table) ||
+        !al4(seq_lens) || !al4(k) || !al4(idx) || !al16(out) || !al16(workspace))
+        return SPARROW_EINVAL;
+    if (sparse && (k_max < 1 || k_max > SPARROW_MAX_PAGES_PER_SEQ))
+        return SPARROW_EINVAL;
+    if (out_dtype != SPARROW_OUT_F32 && out_dtype != SPARROW_OUT_BF16)
+        return SPARROW_EUNSUPPORTED;
+    if (shape->batch == 0)
+        return SPARROW_OK;
+    if (shape->batch > kMaxBatch)
+        return SPARROW_EUNSUPPORTED;
+    const AttnPlan plan = plan_attention(*shape);
+    if (!workspace || ws_bytes < plan.workspace_bytes)
+        return SPARROW_EWORKSPACE;
+    // (the kernels only read the cache)
+    const CacheE4m3 cache{static_cast<uint8_t *>(const_cast<void *>(k_cache)),
+                          static_cast<uint8_t *>(const_cast<void *>(v_cache)),
+                          static_cast<uint8_t *>(const_cast<void *>(exps))};
+    return status_of(launch_attention_e4m3(*shape, plan, q, cache, block_table, seq_lens, k, idx,
+                                           k_max, scale, out, out_dtype, workspace,
+                                           static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
@@ -518,6 +555,28 @@ int sparrow_read_kv_e4m3(const sparrow_shape_t *shape, const void *k_cache, cons
                           static_cast<uint8_t *>(const_cast<void *>(exps))};
     return status_of(launch_read_e4m3(*shape, cache, block_table, seq_lens, cu_tokens, num_tokens,
                                       k_out, v_out, static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_sparse_decode_attn_e4m3(const sparrow_shape_t *shape, const void *q,
+                                    const void *k_cache, const void *v_cache, const void *exps,
+                                    const int32_t *block_table, const int32_t *seq_lens,
+                                    const int32_t *k, const int32_t *idx, int32_t k_max,
+                                    float scale, void *out, int32_t out_dtype, void *workspace,
+                                    size_t ws_bytes, void *stream)
+{
+    return attention_e4m3_call(true, shape, q, k_cache, v_cache, exps, block_table, seq_lens, k,
+                               idx, k_max, scale, out, out_dtype, workspace, ws_bytes, stream);
+}
+
+int sparrow_dense_decode_attn_e4m3(const sparrow_shape_t *shape, const void *q,
+                                   const void *k_cache, const void *v_cache, const void *exps,
+                                   const int32_t *block_table, const int32_t *seq_lens,
+                                   float scale, void *out, int32_t out_dtype, void *workspace,
+                                   size_t ws_bytes, void *stream)
+{
+    return attention_e4m3_call(false, shape, q, k_cache, v_cache, exps, block_table, seq_lens,
+                               nullptr, nullptr, 0, scale, out, out_dtype, workspace, ws_bytes,
+                               stream);
 }
 
 int sparrow_stream_read(const void *src, int64_t bytes, uint32_t *checksum, void *stream)

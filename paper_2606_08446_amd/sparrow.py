@@ -48,7 +48,8 @@ EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_
            "sparrow_acceptance_rate", "sparrow_acceptance_rate_topk", "sparrow_tail_stats",
            "sparrow_stream_read", "sparrow_sparse_decode_attn_noalloc", "sparrow_decode_step",
            "sparrow_qk_norm_rope", "sparrow_qk_norm_rope_bwd", "sparrow_append_kv_e4m3",
-           "sparrow_read_kv_e4m3",
+           "sparrow_read_kv_e4m3", "sparrow_sparse_decode_attn_e4m3",
+           "sparrow_dense_decode_attn_e4m3",
            "sparrow_budget_bound", "sparrow_workspace_size", "sparrow_status_string")
 
 
@@ -119,6 +120,11 @@ def load():
     lib.sparrow_append_kv_e4m3.argtypes = [sp, _p, ctypes.c_int64, _p, ctypes.c_int64, _p,
                                            ctypes.c_int64, _p, _p, _p, _p, _p, _p, _p]
     lib.sparrow_read_kv_e4m3.argtypes = [sp, _p, _p, _p, _p, _p, _p, ctypes.c_int64, _p, _p, _p]
+    lib.sparrow_sparse_decode_attn_e4m3.argtypes = [sp, _p, _p, _p, _p, _p, _p, _p, _p, _i32,
+                                                    ctypes.c_float, _p, _i32, _p,
+                                                    ctypes.c_size_t, _p]
+    lib.sparrow_dense_decode_attn_e4m3.argtypes = [sp, _p, _p, _p, _p, _p, _p, ctypes.c_float, _p,
+                                                   _i32, _p, ctypes.c_size_t, _p]
     for fn in EXPORTS[:-3]:
         getattr(lib, fn).restype = ctypes.c_int
     lib.sparrow_budget_bound.argtypes = [_p, ctypes.c_int64, _i32, _i32, _i32, _p, _p, _i32, _p]
@@ -232,6 +238,20 @@ def sparrow_read_kv_e4m3(shape, k_cache, v_cache, exps, block_table, seq_lens, c
                          num_tokens, k_out, v_out, stream):
     return load().sparrow_read_kv_e4m3(ctypes.byref(shape), k_cache, v_cache, exps, block_table,
                                        seq_lens, cu_tokens, num_tokens, k_out, v_out, stream)
+
+
+def sparrow_sparse_decode_attn_e4m3(shape, q, k_cache, v_cache, exps, block_table, seq_lens, k, idx,
+                                    k_max, scale, out, out_dtype, workspace, ws_bytes, stream):
+    return load().sparrow_sparse_decode_attn_e4m3(ctypes.byref(shape), q, k_cache, v_cache, exps,
+                                                  block_table, seq_lens, k, idx, k_max, scale, out,
+                                                  out_dtype, workspace, ws_bytes, stream)
+
+
+def sparrow_dense_decode_attn_e4m3(shape, q, k_cache, v_cache, exps, block_table, seq_lens, scale,
+                                   out, out_dtype, workspace, ws_bytes, stream):
+    return load().sparrow_dense_decode_attn_e4m3(ctypes.byref(shape), q, k_cache, v_cache, exps,
+                                                 block_table, seq_lens, scale, out, out_dtype,
+                                                 workspace, ws_bytes, stream)
 
 
 def sparrow_stream_read(src, nbytes, checksum, stream):
@@ -780,6 +800,65 @@ def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_t
             shape, _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens),
             _ptr(cu_tokens), T, _ptr(outs[0]), _ptr(outs[1]), _stream(dev)))
     return outs[0], outs[1]
+
+
+def _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, scale, out, out_dtype,
+                    workspace):
+    """Checks and buffers of the two attention calls over an e4m3 cache (dense: idx None)."""
+    import torch
+    _require_device(q)
+    dev = q.device
+    B, Hkv, ps, D, P, M = _expect_cache_e4m3(k_cache, v_cache, exps, block_table, seq_lens, dev)
+    if q.dim() != 3:
+        raise ValueError("q must be [B][Hq][D]")
+    Hq = q.shape[1]
+    _expect(q, "q", torch.bfloat16, (B, Hq, D), dev)
+    k_max = 0
+    if idx is not None:
+        if idx.dim() != 3:
+            raise ValueError("idx must be [B][Hkv][k_max]")
+        k_max = idx.shape[2]
+        _expect(k, "k", torch.int32, (B,), dev)
+        _expect(idx, "idx", torch.int32, (B, Hkv, k_max), dev)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float32 if out_dtype == SPARROW_OUT_F32
+                          else torch.bfloat16, device=dev)
+    _expect_out(out, out_dtype, (B, Hq, D), dev)
+    if B == 0:
+        return out
+    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    shape = make_shape(B, Hq, Hkv, ps, M, P, D)
+    if workspace is None:
+        workspace = _workspace(sparrow_workspace_size(
+            shape, k_max, SPARROW_OP_DENSE_ATTN if idx is None else SPARROW_OP_SPARSE_ATTN), dev)
+    _expect_workspace(workspace, dev)
+    ws = (_ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
+    head = (shape, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table),
+            _ptr(seq_lens))
+    with _on(dev):
+        if idx is None:
+            _check("sparrow_dense_decode_attn_e4m3", sparrow_dense_decode_attn_e4m3(
+                *head, scale, _ptr(out), int(out_dtype), *ws))
+        else:
+            _check("sparrow_sparse_decode_attn_e4m3", sparrow_sparse_decode_attn_e4m3(
+                *head, _ptr(k), _ptr(idx), k_max, scale, _ptr(out), int(out_dtype), *ws))
+    return out
+
+
+def sparse_decode_attn_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, scale=None,
+                            out=None, out_dtype=SPARROW_OUT_F32, workspace=None):
+    """Attention over the selected pages of an e4m3 cache.  Returns out [B][Hq][D] (fp32 or bf16)."""
+    if idx is None:
+        raise ValueError("idx is required")
+    return _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, scale, out,
+                           out_dtype, workspace)
+
+
+def dense_decode_attn_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, scale=None, out=None,
+                           out_dtype=SPARROW_OUT_F32, workspace=None):
+    """Dense paged decode attention over an e4m3 cache.  Returns out [B][Hq][D] (fp32 or bf16)."""
+    return _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, None, None, scale, out,
+                           out_dtype, workspace)
 
 
 def stream_read(buf, checksum=None):
