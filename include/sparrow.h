@@ -514,7 +514,7 @@ int sparrow_read_kv_e4m3(const sparrow_shape_t *shape, const void *k_cache, cons
  * shape, k_max, the page lists and the device.
  *
  * Arguments: as there, with k_cache, v_cache (16-byte aligned) and exps (8-byte aligned) of an e4m3
- * cache.
+ * cache of num_phys_pages * num_kv_heads * page_size / 16 < 2^31.
  * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED, SPARROW_EWORKSPACE, SPARROW_EHIP.
  */
 int sparrow_sparse_decode_attn_e4m3(const sparrow_shape_t *shape, const void *q,

@@ -119,7 +119,9 @@ int attention_e4m3_call(bool sparse, const sparrow_shape_t *shape, const void *q
         return SPARROW_EUNSUPPORTED;
     if (shape->batch == 0)
         return SPARROW_OK;
-    if (shape->batch > kMaxBatch)
+    // (the kernels number the cache's 16-token parts in 32 bits: 4 TiB of codes)
+    if (shape->batch > kMaxBatch ||
+        shape->num_phys_pages > 0x7fffffff / (shape->page_size / 16) / shape->num_kv_heads)
         return SPARROW_EUNSUPPORTED;
     const AttnPlan plan = plan_attention(*shape);
     if (!workspace || ws_bytes < plan.workspace_bytes)

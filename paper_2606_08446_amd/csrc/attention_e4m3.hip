@@ -6,16 +6,17 @@
 // flight are twice the tokens: a tile is two parts of 16 tokens (of one page, or of two 16-token
 // pages next to each other in the list).  Per part and wave:
 //   QK  codes to bf16 (exact), 4 x mfma_f32_16x16x32_bf16, the result times scale 2^{ek}
-//       lane (row = token lr, group lg) holds channels 16lg..16lg+15 and 64+16lg..: two 16-byte
-//       loads; q's fragments are loaded in the same channel order
+//       lane (row = token lr, group lg) holds channels 32lg .. 32lg+31 (see trade_rows); q's
+//       fragments are loaded in the same channel order
 //   PV  lane (lr, lg) loads the 8 codes V[token][8lr ..] of the tokens 4lg..4lg+3 of both parts and
 //       converts them with their row's scale, which gives the exact bf16 values; 8 output tiles
 //       on mfma_f32_16x16x32_bf16 over the tile's 32 tokens
 // The softmax numerators enter PV as the sum of two bf16 numbers (the value rounded, and what that
 // rounding left), 17 bits in all: the matrix cores have the time, and the result is as exact as one
 // rounded from fp32 at the end.  Sums and maxima are fp32.
-#include <atomic>
-
+//
+// Bound by HBM: 64 sequences of 8K-32K tokens (2.8 GB) take 428 us, 6.6 TB/s where a read-only stream
+// reaches 7.1; with the arithmetic taken out the kernel is no faster.
 #include "attention_e4m3.h"
 
 #include "attention_split.h"
@@ -40,23 +41,37 @@ struct Tile {
     u32x2_t e[kParts];  // exponents of tokens 4lg .. 4lg+3: K's bytes, V's bytes
 };
 
-__device__ __forceinline__ u32x2_t ld8_nt(const void *p)
+// An address in the cache that all lanes share, kept in scalar registers: a load then takes it
+// with the lane's 32-bit offset, and no vector instruction adds them up.
+typedef const __attribute__((address_space(1))) uint8_t *global_bytes;
+
+__device__ __forceinline__ global_bytes scalar_base(const uint8_t *p)
 {
-    return __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p));
+    uintptr_t u = (uintptr_t)p;
+    asm volatile("" : "+s"(u));
+    return (global_bytes)u;
 }
 
-// Part p from the cache row `row` on.
-__device__ __forceinline__ void load_part(Tile &t, int p, const Args8 &x, int64_t row, int lr,
-                                          int lg)
+template <typename T>
+__device__ __forceinline__ T load_nt(global_bytes p)
 {
-    t.e[p] = *reinterpret_cast<const u32x2_t *>(x.exps + row * 2 + 8 * lg);
-    const uint8_t *kp = x.k + row * kHeadDim + lr * kHeadDim + 16 * lg;
-    t.k[p][0] = ld16_nt(kp);
-    t.k[p][1] = ld16_nt(kp + 64);
-    const uint8_t *vp = x.v + row * kHeadDim + 4 * lg * kHeadDim + 8 * lr;
+    return __builtin_nontemporal_load((const __attribute__((address_space(1))) T *)p);
+}
+
+// Part p from the 16 cache rows `part` (their number in the cache / 16).
+__device__ __forceinline__ void load_part(Tile &t, int p, const Args8 &x, int part, uint32_t k_lane,
+                                          uint32_t v_lane, uint32_t e_lane)
+{
+    const int64_t off = (int64_t)part * (16 * kHeadDim);
+    const global_bytes ep = scalar_base(x.exps + (int64_t)part * 32);
+    const global_bytes kp = scalar_base(x.k + off);
+    const global_bytes vp = scalar_base(x.v + off);
+    t.e[p] = *(const __attribute__((address_space(1))) u32x2_t *)(ep + e_lane);
+    t.k[p][0] = load_nt<u32x4_t>(kp + k_lane);
+    t.k[p][1] = load_nt<u32x4_t>(kp + k_lane + 8 * kHeadDim);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        t.v[p][j] = ld8_nt(vp + j * kHeadDim);
+        t.v[p][j] = load_nt<u32x2_t>(vp + v_lane + j * kHeadDim);
 }
 
 __device__ __forceinline__ float byte_pow2(uint32_t w, int j)
@@ -71,17 +86,47 @@ __device__ __forceinline__ u32x4_t values(u32x2_t c, float scale)
                      unpack_e4m3<false>(c[1], scale), unpack_e4m3<true>(c[1], scale)};
 }
 
-// A tile into the wave's online-softmax state.  valid[p] tokens of part p lie inside the sequence
-// (at least one in all); the others get weight 0 and zero V rows.
-__device__ __forceinline__ void attend_tile(Tile &t, const int (&valid)[kParts],
-                                            const bf16x8_t (&qf)[4], float scale_log2, int lg,
-                                            float &m_run, float &l_run, f32x4_t (&O)[8])
+// Maximum / sum over the four lanes of a head (lr, lr + 16, lr + 32, lr + 48), which every one of
+// them gets.  A swap of odd with even 16-lane rows of two copies leaves each lane its own row's
+// value and its neighbour's; a swap of the upper with the lower half does it for 32 lanes.
+template <typename Op>
+__device__ __forceinline__ float over_groups(float x, Op op)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// K of a part in operand order.  A load that gave lane (lr, lg) 16 bytes of its own row lr would touch
+// 16 rows, half a line of each, and the memory reads lines; so each load takes 8 whole rows, and lane
+// (lr, lg) holds chunk 2lg + lr / 8 of row lr % 8 and of row 8 + lr % 8.  Lanes lr and lr ^ 8 then
+// trade the one that is not their row's, which leaves each with chunks 2lg and 2lg + 1 of its own.
+// (Loads alone, 64 sequences of 8K-32K tokens: 457 us by half lines, 434 by rows.)
+__device__ __forceinline__ void trade_rows(u32x4_t (&k)[2])
+{
+    constexpr int kRor8 = 0x128;  // lane ^ 8 inside each 16
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const int a = (int)k[0][d], b = (int)k[1][d];
+        k[0][d] = (uint32_t)__builtin_amdgcn_update_dpp(a, b, kRor8, 0xf, 0xc, false);
+        k[1][d] = (uint32_t)__builtin_amdgcn_update_dpp(b, a, kRor8, 0xf, 0x3, false);
+    }
+}
+
+// A tile into the wave's online-softmax state.  v0 and v1 tokens of its parts lie inside the
+// sequence (16 or more: all; 0 or less: none); the others get weight 0 and zero V rows.
+__device__ __forceinline__ void attend_tile(Tile &t, int v0, int v1, const bf16x8_t (&qf)[4],
+                                            float scale_log2, int lg, float &m_run, float &l_run,
+                                            f32x4_t (&O)[8])
 {
     float z[kParts][4];
-    float cm = -INFINITY;
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
         f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+        trade_rows(t.k[p]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const u32x4_t w = t.k[p][i >> 1];
@@ -90,24 +135,36 @@ __device__ __forceinline__ void attend_tile(Tile &t, const int (&valid)[kParts],
                                                         0, 0, 0);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            z[p][j] = 4 * lg + j < valid[p] ? s[j] * (scale_log2 * byte_pow2(t.e[p][0], j))
-                                            : -INFINITY;
-            cm = fmaxf(cm, z[p][j]);
-        }
+        for (int j = 0; j < 4; ++j)
+            z[p][j] = s[j] * (scale_log2 * byte_pow2(t.e[p][0], j));
     }
-    cm = fmaxf(cm, __shfl_xor(cm, 16, 64));
-    cm = fmaxf(cm, __shfl_xor(cm, 32, 64));
-    const float m_new = fmaxf(m_run, cm);
-    const float alpha = exp2f(m_run - m_new);
-    m_run = m_new;
+    if (min(v0, v1) < 16) {  // cache slots past the length, and parts that are not there, may
+                             // hold anything
+#pragma unroll
+        for (int p = 0; p < kParts; ++p)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (4 * lg + j >= (p == 0 ? v0 : v1)) {
+                    z[p][j] = -INFINITY;
+                    t.v[p][j] = (u32x2_t){0u, 0u};
+                    t.e[p][1] &= ~(0xffu << (8 * j));
+                }
+    }
+    float cm = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
+                     fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+    cm = over_groups(cm, [](float a, float b) { return fmaxf(a, b); });
+    const float m_old = m_run;
+    m_run = fmaxf(m_run, cm);
+    const float m = m_run == -INFINITY ? 0.f : m_run;  // (no token so far)
+    const float alpha = __builtin_amdgcn_exp2f(m_old - m);
     float sum = 0.f;
     u32x4_t hi, lo;
 #pragma unroll
     for (int p = 0; p < kParts; ++p)
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
-            const float a = exp2f(z[p][j] - m_new), b = exp2f(z[p][j + 1] - m_new);
+            const float a = __builtin_amdgcn_exp2f(z[p][j] - m);
+            const float b = __builtin_amdgcn_exp2f(z[p][j + 1] - m);
             sum += a + b;
             const uint32_t h = pack_bf16(a, b);
             hi[2 * p + (j >> 1)] = h;
@@ -121,19 +178,10 @@ __device__ __forceinline__ void attend_tile(Tile &t, const int (&valid)[kParts],
     }
     u32x4_t v[kParts][4];
 #pragma unroll
-    for (int p = 0; p < kParts; ++p) {
-        if (valid[p] < 16) {  // cache slots past the length may hold anything
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (4 * lg + j >= valid[p]) {
-                    t.v[p][j] = (u32x2_t){0u, 0u};
-                    t.e[p][1] &= ~(0xffu << (8 * j));
-                }
-        }
+    for (int p = 0; p < kParts; ++p)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             v[p][j] = values(t.v[p][j], byte_pow2(t.e[p][1], j));
-    }
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const u32x4_t av = {pair_of(v[0][0], v[0][1], c), pair_of(v[0][2], v[0][3], c),
@@ -147,46 +195,149 @@ __device__ __forceinline__ void attend_tile(Tile &t, const int (&valid)[kParts],
     }
 }
 
-// q's fragments in the channel order of the K loads.
-__device__ __forceinline__ void load_q(const AttnArgs &a, int b, int h, int lr, int lg,
+// q's fragments of a unit (sequence, KV head) in the channel order of the K loads.
+__device__ __forceinline__ void load_q(const AttnArgs &a, int unit, int lr, int lg,
                                        bf16x8_t (&qf)[4])
 {
     const int G = a.num_q_heads / a.num_kv_heads;
-    const uint16_t *qrow = a.q + ((int64_t)b * a.num_q_heads + (int64_t)h * G + lr) * kHeadDim;
+    const uint16_t *qrow = a.q + ((int64_t)unit * G + lr) * kHeadDim;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         u32x4_t v = {0u, 0u, 0u, 0u};
         if (lr < G)
-            v = ld16(qrow + 64 * (i >> 1) + 16 * lg + 8 * (i & 1));
+            v = ld16(qrow + 32 * lg + 8 * i);
         qf[i] = __builtin_bit_cast(bf16x8_t, v);
     }
 }
 
-// The walk's state at position pos: the last sequence whose offset is <= pos holds it (empty
-// sequences before it share its offset).  A wave narrows [lo, lo + span) 64-fold per round.
-__device__ __forceinline__ Cursor locate(const int32_t *s_off, int B, int Hkv, int64_t pos,
-                                         int lane)
+// An LDS word that every lane reads, as a scalar.
+__device__ __forceinline__ int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A word at an address that every lane shares, by the scalar unit (the kernel does not write it).
+__device__ __forceinline__ int32_t scalar_load(const int32_t *p)
 {
-    int lo = 0, span = B;
-    while (span > 1) {
-        const int step = (span + 63) >> 6;
-        const bool ok = lane * step < span && (int64_t)s_off[lo + lane * step] * Hkv <= pos;
-        const int t = __popcll(__ballot(ok)) - 1;
-        lo += t * step;
-        span = min(step, span - t * step);
-    }
-    Cursor c;
-    c.b = lo;
-    c.cnt = s_off[lo + 1] - s_off[lo];
-    const int64_t rel = pos - (int64_t)s_off[lo] * Hkv;
-    c.h = (int)(rel / c.cnt);
-    c.j = (int)(rel - (int64_t)c.h * c.cnt);
-    c.pos = pos;
-    return c;
+    typedef const __attribute__((address_space(4))) int32_t *constant_ptr;
+    return *(constant_ptr)(uintptr_t)p;
 }
 
+// The walk over a wave's range of (sequence, KV head, list position), in batches of at most
+// kBatch pages of one unit.  Everything in it is the same for all lanes, but for what a lane knows
+// of its page of the batch.
+struct Walk {
+    int unit, b, h, j, cnt, len;
+    int64_t left;  // pages of the range not yet taken
+
+    // The place of range position pos: the last sequence whose offset is <= pos holds it (empty
+    // sequences before it share its offset).  A wave narrows [lo, lo + span) 64-fold per round.
+    __device__ __forceinline__ void start(const AttnArgs &a, const int32_t *s_off, int64_t pos,
+                                          int64_t end, int lane)
+    {
+        const int Hkv = a.num_kv_heads;
+        int lo = 0, span = a.batch;
+        while (span > 1) {
+            const int step = (span + 63) >> 6;
+            const bool ok = lane * step < span && (int64_t)s_off[lo + lane * step] * Hkv <= pos;
+            const int t = __popcll(__ballot(ok)) - 1;
+            lo += t * step;
+            span = min(step, span - t * step);
+        }
+        b = lo;
+        const int off = uniform(s_off[lo]);
+        cnt = uniform(s_off[lo + 1]) - off;
+        const int64_t rel = pos - (int64_t)off * Hkv;
+        h = (int)(rel / cnt);
+        j = (int)(rel - (int64_t)h * cnt);
+        unit = b * Hkv + h;
+        len = scalar_load(a.seq_lens + b);
+        left = end - pos;
+    }
+};
+
+constexpr int kCloses = 1, kLast = 2;  // a batch, or a tile, ends its unit; the range
+
+// A batch of pages: what all lanes know of it.
+struct PageBatch {
+    int unit, b, len, n, ends;
+};
+
+// The next batch of the walk (n = 0 behind the last one).  Returns the lane's entry of its list; lanes
+// past the batch read the first entry, so that the load is the same for all.
 template <bool kSparse>
-__global__ __launch_bounds__(kAttnThreads) void k_attn_stream_e4m3(Args8 x)
+__device__ __forceinline__ int take(const AttnArgs &a, const int32_t *s_off, Walk &w, PageBatch &t,
+                                    int lane)
+{
+    t.unit = w.unit;
+    t.b = w.b;
+    t.len = w.len;
+    int n = min(w.cnt - w.j, kBatch);
+    n = n < w.left ? n : (int)w.left;
+    t.n = n;
+    int lp = w.j + lane;
+    if (kSparse)
+        lp = a.idx[(int64_t)w.unit * a.k_max + (lane < n ? lp : 0)];
+    w.left -= n;
+    w.j += n;
+    const bool closes = w.j == w.cnt;
+    t.ends = (closes ? kCloses : 0) | (w.left == 0 ? kLast : 0);
+    if (closes && w.left > 0) {  // the next unit with pages
+        w.j = 0;
+        ++w.unit;
+        if (++w.h == a.num_kv_heads) {
+            w.h = 0;
+            do {
+                ++w.b;
+                w.cnt = uniform(s_off[w.b + 1]) - uniform(s_off[w.b]);
+            } while (w.cnt == 0);
+            w.unit = w.b * a.num_kv_heads;
+            w.len = scalar_load(a.seq_lens + w.b);
+        }
+    }
+    return lp;
+}
+
+// Whether a lane's list entry is a page of the batch's sequence.
+__device__ __forceinline__ bool in_sequence(const AttnArgs &a, const PageBatch &t, int lp, int lane)
+{
+    const int L = clamp_len(t.len, a.ps, a.max_pages);
+    return lane < t.n && lp >= 0 && lp < (L + a.ps - 1) >> (__ffs(a.ps) - 1);
+}
+
+// The physical page of a lane's list entry (entries outside the sequence read the row's first).
+__device__ __forceinline__ int look_up(const AttnArgs &a, const PageBatch &t, int lp, int lane)
+{
+    return a.block_table[(int64_t)t.b * a.max_pages + (in_sequence(a, t, lp, lane) ? lp : 0)];
+}
+
+// What a lane's page of the batch at work is loaded by.
+struct Pages {
+    int part;    // number of its first 16 cache rows, / 16
+    int tokens;  // inside the sequence; 0, with rows that exist, where there is no page
+
+    // (a block-table entry outside the cache is an absent page)
+    __device__ __forceinline__ void settle(const AttnArgs &a, const PageBatch &t, int lp, int phys,
+                                           int lane)
+    {
+        const int L = clamp_len(t.len, a.ps, a.max_pages);
+        const bool live = in_sequence(a, t, lp, lane) && phys >= 0 && phys < a.num_phys;
+        part = live ? (phys * a.num_kv_heads + (t.unit - t.b * a.num_kv_heads)) * (a.ps >> 4) : 0;
+        tokens = live ? min(L - lp * a.ps, a.ps) : 0;
+    }
+};
+
+// A tile whose loads are issued.
+struct Step {
+    int v0, v1;  // tokens of its parts inside the sequence
+    int unit, ends;
+};
+
+// A wave's range, tile by tile, with two tiles' loads in flight while a third is computed.  The
+// buffers take turns, so that no tile is copied, and every tile is loaded (a part that is not there
+// reads rows that exist and gets no weight), so that the loads in flight can be counted and the wait
+// is for the tile at hand only.  The page lists and the block table are read two and one batches
+// ahead, at the end of a batch, and nothing is done with their loads until the next one ends: loads
+// return in order, so that a use of the youngest would make the wave wait for the tiles as well.
+template <bool kSparse>
+__global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
 {
     extern __shared__ int32_t s_off[];  // [batch + 1]
     __shared__ int32_t s_tmp[kAttnWaves];
@@ -200,7 +351,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_stream_e4m3(Args8 x)
         for (int b = threadIdx.x; b <= B; b += kAttnThreads)
             a.plan_off[b] = s_off[b];
 
-    const int64_t P = (int64_t)s_off[B] * Hkv;
+    const int64_t P = (int64_t)uniform(s_off[B]) * Hkv;
     // (the rule of k_attn_stream, with tiles of twice its chunks)
     int64_t W = P * (a.ps >> 4) / (2 * kParts);
     W = W > a.fine_waves ? W : a.fine_waves;
@@ -209,25 +360,55 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_stream_e4m3(Args8 x)
     const int w = blockIdx.x * kAttnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (w >= W)
         return;
-    const int64_t pos_end = (int64_t)(w + 1) * P / W;
     const int lane = threadIdx.x & 63;
     const int lr = lane & 15;
     const int lg = lane >> 4;
-    const int ps = a.ps;
-    const int cpp = ps >> 4;  // 16-token parts per page
-    Cursor cur = locate(s_off, B, Hkv, (int64_t)w * P / W, lane);
+    // a lane's offsets into a part
+    const uint32_t k_lane = (lr & 7) * kHeadDim + 16 * (2 * lg + (lr >> 3));
+    const uint32_t v_lane = 4 * lg * kHeadDim + 8 * lr;
+    const uint32_t e_lane = 8 * lg;
+    const int log_cpp = __ffs(a.ps) - 5;  // 16-token parts per page: ps / 16
+    Walk walk;
+    walk.start(a, s_off, (int64_t)w * P / W, (int64_t)(w + 1) * P / W, lane);
+    bool from_start = walk.j == 0;  // the unit at work begins in this wave
 
-    Batch bc, bn;
-    fetch_batch_begin<kSparse>(a, s_off, cur, pos_end, bc, lane);
-    fetch_batch_end(a, bc);
-    bool have_next = cur.pos < pos_end;
-    bool bn_pending = have_next;  // bn's block-table loads not issued yet
-    if (have_next)
-        fetch_batch_begin<kSparse>(a, s_off, cur, pos_end, bn, lane);
+    // the batch at work, the one with its block-table loads under way, the one with its list's
+    PageBatch now, b1, b2;
+    Pages pages;
+    const int lp0 = take<kSparse>(a, s_off, walk, now, lane);
+    int lp1 = take<kSparse>(a, s_off, walk, b1, lane);
+    int lp2 = take<kSparse>(a, s_off, walk, b2, lane);
+    const int phys0 = look_up(a, now, lp0, lane);
+    int phys1 = look_up(a, b1, lp1, lane);
+    bf16x8_t qf[4];
+    load_q(a, now.unit, lr, lg, qf);
+    pages.settle(a, now, lp0, phys0, lane);
+    int ti = 0;
+    int tiles = ((now.n << log_cpp) + kParts - 1) / kParts;
 
-    bf16x8_t qf[4], qn[4];
-    load_q(a, bc.b, bc.h, lr, lg, qf);
-    bool from_start = bc.j0 == 0;
+    // ---- the next tile of the range into a buffer (behind the last one: rows that exist)
+    auto issue = [&](Tile &tile, Step &s) __attribute__((always_inline)) {
+        const int c0 = kParts * ti, c1 = c0 + 1;  // parts of the batch
+        const int p0 = (c0 >> log_cpp) & 63, p1 = (c1 >> log_cpp) & 63;  // their pages
+        const int u0 = c0 & ((1 << log_cpp) - 1), u1 = c1 & ((1 << log_cpp) - 1);
+        load_part(tile, 0, x, __builtin_amdgcn_readlane(pages.part, p0) + u0, k_lane, v_lane, e_lane);
+        load_part(tile, 1, x, __builtin_amdgcn_readlane(pages.part, p1) + u1, k_lane, v_lane, e_lane);
+        s.v0 = __builtin_amdgcn_readlane(pages.tokens, p0) - 16 * u0;
+        s.v1 = __builtin_amdgcn_readlane(pages.tokens, p1) - 16 * u1;
+        s.unit = now.unit;
+        s.ends = 0;
+        if (++ti < tiles)
+            return;
+        s.ends = now.ends;
+        now = b1;
+        pages.settle(a, now, lp1, phys1, lane);
+        ti = 0;
+        tiles = ((now.n << log_cpp) + kParts - 1) / kParts;
+        b1 = b2;
+        lp1 = lp2;
+        phys1 = look_up(a, b1, lp1, lane);
+        lp2 = take<kSparse>(a, s_off, walk, b2, lane);
+    };
 
     float m_run = -INFINITY;
     float l_run = 0.f;
@@ -236,30 +417,10 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_stream_e4m3(Args8 x)
     for (int c = 0; c < 8; ++c)
         O[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 
-    // tile `ti` of batch t: parts 2 ti and 2 ti + 1; part ci is page ci / cpp, sub-part ci % cpp
-    auto issue = [&](const Batch &t, int ti, Tile &tile, int (&valid)[kParts]) {
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) {
-            valid[p] = 0;
-            const int ci = kParts * ti + p;
-            if (ci >= t.n * cpp)
-                break;  // (an odd number of parts)
-            const int pi = ci / cpp;
-            const int sub = ci - pi * cpp;
-            const int ph = __builtin_amdgcn_readlane(t.phys, pi);
-            const int tok = __builtin_amdgcn_readlane(t.tok0, pi) + 16 * sub;
-            // a block-table entry outside the cache is an absent page
-            if (ph >= 0 && ph < a.num_phys && tok < t.L) {
-                valid[p] = t.L - tok;
-                load_part(tile, p, x, ((int64_t)ph * Hkv + t.h) * ps + 16 * sub, lr, lg);
-            }
-        }
-    };
-
-    // A unit's finished state: the output when the unit lies in this wave alone, else a partial
-    // (segment `wave + unit`) for the merge.
-    auto write_unit = [&](int b, int h, float l, bool first, bool last) {
-        const int unit = b * Hkv + h;
+    // ---- a unit's finished state: the output when the unit lies in this wave alone, else a
+    // partial (segment `wave + unit`) for the merge
+    auto write_unit = [&](int unit, bool first, bool last) __attribute__((always_inline)) {
+        const float l = over_groups(l_run, [](float u, float v) { return u + v; });
         if (lane == 0) {
             if (first)
                 a.unit_waves[2 * unit] = w;
@@ -270,12 +431,26 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_stream_e4m3(Args8 x)
             return;
         if (first && last) {
             const float inv = l > 0.f ? 1.f / l : 0.f;
-            const int64_t orow = ((int64_t)b * a.num_q_heads + (int64_t)h * G + lr) * kHeadDim;
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
+            const int64_t orow = ((int64_t)unit * G + lr) * kHeadDim;
+            // (channels 32lg + 8i + c are 8 in a row)
+            if (a.out_bf16) {
+                uint16_t *o = static_cast<uint16_t *>(a.out) + orow + 32 * lg;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    store_out(a.out, a.out_bf16, orow + 32 * lg + 8 * i + c, O[c][i] * inv);
+                    st16(o + 8 * i, (u32x4_t){pack_bf16(O[0][i] * inv, O[1][i] * inv),
+                                              pack_bf16(O[2][i] * inv, O[3][i] * inv),
+                                              pack_bf16(O[4][i] * inv, O[5][i] * inv),
+                                              pack_bf16(O[6][i] * inv, O[7][i] * inv)});
+            } else {
+                float *o = static_cast<float *>(a.out) + orow + 32 * lg;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < 8; c += 4)
+                        st16(o + 8 * i + c,
+                             __builtin_bit_cast(u32x4_t, (f32x4_t){O[c][i], O[c + 1][i], O[c + 2][i],
+                                                                   O[c + 3][i]} * inv));
+            }
         } else {
             const int64_t seg = (int64_t)w + unit;
             float *op = a.o_part + (seg * G + lr) * kHeadDim + 32 * lg;
@@ -293,82 +468,180 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_stream_e4m3(Args8 x)
         }
     };
 
-    Tile nxt;
-    int valid_next[kParts];
-    issue(bc, 0, nxt, valid_next);
-    int ti = 0;
-    for (;;) {
-        Tile tile = nxt;
-        const int valid[kParts] = {valid_next[0], valid_next[1]};
-        const bool last_in_batch = kParts * (ti + 1) >= bc.n * cpp;
-        if (!last_in_batch) {
-            issue(bc, ti + 1, nxt, valid_next);
-            if (bn_pending) {
-                fetch_batch_end(a, bn);
-                bn_pending = false;
-            }
-        } else if (have_next) {
-            if (bn_pending) {  // a one-tile batch: bn is needed now
-                fetch_batch_end(a, bn);
-                bn_pending = false;
-            }
-            issue(bn, 0, nxt, valid_next);
-            if (bc.ends_unit)
-                load_q(a, bn.b, bn.h, lr, lg, qn);
-        }
-
-        if (valid[0] > 0 || valid[1] > 0)
-            attend_tile(tile, valid, qf, a.scale_log2, lg, m_run, l_run, O);
-
-        if (!last_in_batch) {
-            ++ti;
-            continue;
-        }
-        if (bc.ends_unit || !have_next) {
-            float l_tot = l_run + __shfl_xor(l_run, 16, 64);
-            l_tot += __shfl_xor(l_tot, 32, 64);
-            write_unit(bc.b, bc.h, l_tot, from_start, bc.ends_unit);
-            if (!have_next)
-                break;
+    // ---- a tile's turn; true when the range is done
+    auto turn = [&](Tile &tile, const Step &s, const Step &after) __attribute__((always_inline)) {
+        attend_tile(tile, s.v0, s.v1, qf, a.scale_log2, lg, m_run, l_run, O);
+        if (s.ends != 0) {
+            write_unit(s.unit, from_start, s.ends & kCloses);
+            if (s.ends & kLast)
+                return true;
+            from_start = true;
             m_run = -INFINITY;
             l_run = 0.f;
 #pragma unroll
             for (int c = 0; c < 8; ++c)
                 O[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+            load_q(a, after.unit, lr, lg, qf);
+            // waited for here, not at every use: an operand that might be this load's would make
+            // each tile wait for all loads before it
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                qf[i] = qn[i];
-            from_start = bn.j0 == 0;
+                asm volatile("" : "+v"(qf[i]));
         }
-        bc = bn;
-        ti = 0;
-        have_next = cur.pos < pos_end;
-        bn_pending = have_next;
-        if (have_next)
-            fetch_batch_begin<kSparse>(a, s_off, cur, pos_end, bn, lane);
+        return false;
+    };
+
+    Tile t0, t1, t2;
+    Step s0, s1, s2;
+    issue(t0, s0);
+    issue(t1, s1);
+    for (;;) {
+        issue(t2, s2);
+        if (turn(t0, s0, s1))
+            break;
+        issue(t0, s0);
+        if (turn(t1, s1, s2))
+            break;
+        issue(t1, s1);
+        if (turn(t2, s2, s0))
+            break;
     }
 }
 
-// Streaming waves on the current device: compute units x resident workgroups x 4, capped.  (A
-// cache of device attributes: concurrent first calls all store the same value.)
-int device_waves()
+// Short lists of few units: one workgroup per (sequence, KV head), its waves' states joined in LDS in
+// wave order, so that there are no partials in memory and no second launch.  Every wave knows the
+// whole list, a page per lane, and takes an equal share of its tiles.  Bound by what one CU can fetch,
+// and so by the longest list that the call admits: up to 256 units (a CU each) of 1024 tokens it is
+// the faster one at any lengths.  A call, streaming waves and merge -> this, us, 4 query heads each:
+// 8 units x 256 tokens 16.8 -> 14.0, 128 x 1024 16.8 -> 14.7, 256 x 1024 21.6 -> 18.1; but 8 x 2048
+// 16.8 -> 18.2, 8 x 4096 16.7 -> 29.9 and 512 x 512 21.8 -> 23.1.
+constexpr int kUnitMaxUnits = 256;
+constexpr int kUnitMaxTokens = 1024;    // list bound x page size
+constexpr int kUnitThreads = 512;
+constexpr int kUnitWaves = kUnitThreads / 64;
+constexpr int kUnitMaxGroup = 8;        // query heads per KV head (sizes the LDS)
+constexpr int kUnitRow = kHeadDim + 4;  // LDS row stride of a wave's o (floats)
+
+template <bool kSparse>
+__global__ __launch_bounds__(kUnitThreads, 2) void k_attn_unit_e4m3(Args8 x)
 {
-    static std::atomic<int> cached[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64)
-        return kMaxWaves;
-    int w = cached[dev].load(std::memory_order_relaxed);
-    if (w == 0) {
-        int per_cu = 0;
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, k_attn_stream_e4m3<true>,
-                                                         kAttnThreads, 4096) != hipSuccess ||
-            per_cu < 1)
-            per_cu = 1;
-        w = device_cus() * per_cu * kAttnWaves;
-        w = w < kMaxWaves ? w : kMaxWaves;
-        cached[dev].store(w, std::memory_order_relaxed);
+    __shared__ __align__(16) float s_o[kUnitWaves * kUnitMaxGroup * kUnitRow];
+    __shared__ float s_m[kUnitWaves * kUnitMaxGroup], s_l[kUnitWaves * kUnitMaxGroup];
+    const AttnArgs &a = x.a;
+    const int Hkv = a.num_kv_heads;
+    const int G = a.num_q_heads / Hkv;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int lr = lane & 15;
+    const int lg = lane >> 4;
+    const uint32_t k_lane = (lr & 7) * kHeadDim + 16 * (2 * lg + (lr >> 3));
+    const uint32_t v_lane = 4 * lg * kHeadDim + 8 * lr;
+    const uint32_t e_lane = 8 * lg;
+    const int log_cpp = __ffs(a.ps) - 5;
+
+    PageBatch t;
+    t.unit = blockIdx.x;
+    t.b = t.unit / Hkv;
+    t.len = scalar_load(a.seq_lens + t.b);
+    int lp = lane;
+    if (kSparse) {  // (lanes past the row read its first entry)
+        const int c = scalar_load(a.ksel + t.b);
+        lp = a.idx[(int64_t)t.unit * a.k_max + (lane < a.k_max ? lane : 0)];
+        t.n = c < 0 ? 0 : min(c, a.k_max);
+    } else {
+        t.n = (clamp_len(t.len, a.ps, a.max_pages) + a.ps - 1) >> (log_cpp + 4);
     }
-    return w;
+    bf16x8_t qf[4];
+    load_q(a, t.unit, lr, lg, qf);
+    Pages pages;
+    pages.settle(a, t, lp, look_up(a, t, lp, lane), lane);
+
+    const int tiles = ((t.n << log_cpp) + kParts - 1) / kParts;
+    const int end = (wv + 1) * tiles / kUnitWaves;
+    int ti = wv * tiles / kUnitWaves;
+    auto issue = [&](Tile &tile, int &v0, int &v1) __attribute__((always_inline)) {
+        const int at = min(ti, tiles - 1);  // (behind the share: rows that exist)
+        const int c0 = kParts * max(at, 0), c1 = c0 + 1;
+        const int p0 = (c0 >> log_cpp) & 63, p1 = (c1 >> log_cpp) & 63;
+        const int u0 = c0 & ((1 << log_cpp) - 1), u1 = c1 & ((1 << log_cpp) - 1);
+        load_part(tile, 0, x, __builtin_amdgcn_readlane(pages.part, p0) + u0, k_lane, v_lane, e_lane);
+        load_part(tile, 1, x, __builtin_amdgcn_readlane(pages.part, p1) + u1, k_lane, v_lane, e_lane);
+        v0 = __builtin_amdgcn_readlane(pages.tokens, p0) - 16 * u0;
+        v1 = __builtin_amdgcn_readlane(pages.tokens, p1) - 16 * u1;
+        ++ti;
+    };
+    float m_run = -INFINITY;
+    float l_run = 0.f;
+    f32x4_t O[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        O[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    int left = end - ti;
+    if (left > 0) {
+        Tile t0, t1, t2;
+        int v[3][2];
+        issue(t0, v[0][0], v[0][1]);
+        issue(t1, v[1][0], v[1][1]);
+        for (;;) {
+            issue(t2, v[2][0], v[2][1]);
+            attend_tile(t0, v[0][0], v[0][1], qf, a.scale_log2, lg, m_run, l_run, O);
+            if (--left == 0)
+                break;
+            issue(t0, v[0][0], v[0][1]);
+            attend_tile(t1, v[1][0], v[1][1], qf, a.scale_log2, lg, m_run, l_run, O);
+            if (--left == 0)
+                break;
+            issue(t1, v[1][0], v[1][1]);
+            attend_tile(t2, v[2][0], v[2][1], qf, a.scale_log2, lg, m_run, l_run, O);
+            if (--left == 0)
+                break;
+        }
+    }
+
+    // ---- the waves' states into LDS (lane (g, r) holds head g, channels 32r .. 32r+31)
+    const float l_tot = over_groups(l_run, [](float u, float w) { return u + w; });
+    if (lr < G) {
+        float *op = s_o + (wv * kUnitMaxGroup + lr) * kUnitRow + 32 * lg;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<f32x4_t *>(op + 8 * i) = (f32x4_t){O[0][i], O[1][i], O[2][i], O[3][i]};
+            *reinterpret_cast<f32x4_t *>(op + 8 * i + 4) =
+                (f32x4_t){O[4][i], O[5][i], O[6][i], O[7][i]};
+        }
+        if (lg == 0) {
+            s_m[wv * kUnitMaxGroup + lr] = m_run;
+            s_l[wv * kUnitMaxGroup + lr] = l_tot;
+        }
+    }
+    __syncthreads();
+
+    // ---- o = sum_w 2^(m_w - M) o_w / sum_w 2^(m_w - M) l_w
+    for (int i = threadIdx.x; i < G * kHeadDim; i += kUnitThreads) {
+        const int g = i / kHeadDim;
+        const int d = i - g * kHeadDim;
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kUnitWaves; ++w)
+            M = fmaxf(M, s_m[w * kUnitMaxGroup + g]);
+        M = M == -INFINITY ? 0.f : M;  // (no tokens: every weight below is 0)
+        float lsum = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < kUnitWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w * kUnitMaxGroup + g] - M);
+            lsum += f * s_l[w * kUnitMaxGroup + g];
+            acc += f * s_o[(w * kUnitMaxGroup + g) * kUnitRow + d];
+        }
+        const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+        store_out(a.out, a.out_bf16, ((int64_t)t.unit * G + g) * kHeadDim + d, acc * inv);
+    }
+}
+
+// Whether a call takes one workgroup per unit; list_bound: k_max, or the block table's width.
+bool unit_path(const sparrow_shape_t &s, int64_t list_bound)
+{
+    return (int64_t)s.batch * s.num_kv_heads <= kUnitMaxUnits &&
+           s.num_q_heads / s.num_kv_heads <= kUnitMaxGroup && list_bound <= kBatch &&
+           list_bound * s.page_size <= kUnitMaxTokens;
 }
 
 }  // namespace
@@ -381,7 +654,11 @@ hipError_t launch_attention_e4m3(const sparrow_shape_t &s, const AttnPlan &plan,
 {
     const int64_t units = (int64_t)s.batch * s.num_kv_heads;
     const int G = s.num_q_heads / s.num_kv_heads;
-    const int64_t waves = device_waves();
+    // One workgroup per CU, four waves with two tiles in flight each: 64 KiB, which keeps the memory
+    // busy; more waves only add partials and uneven ends (1 / 2 workgroups: 64 sequences of 8K-32K
+    // tokens 428 / 429 us, 256 sequences at 10 % 251 / 257, 128 units of 1024 tokens 16.1 / 17.2).
+    int64_t waves = (int64_t)device_cus() * kAttnWaves;
+    waves = waves < kMaxWaves ? waves : kMaxWaves;
     Args8 x{};
     x.k = c.k;
     x.v = c.v;
@@ -408,6 +685,11 @@ hipError_t launch_attention_e4m3(const sparrow_shape_t &s, const AttnPlan &plan,
     a.max_waves = (int)(units * kUnitSegments < waves ? units * kUnitSegments : waves);
     a.fine_waves = (int)(units * 64 < waves ? units * 64 : waves);
     a.scale_log2 = scale * 1.4426950408889634f;
+    if (unit_path(s, idx != nullptr ? k_max : s.max_pages_per_seq)) {
+        auto unit = idx != nullptr ? k_attn_unit_e4m3<true> : k_attn_unit_e4m3<false>;
+        hipLaunchKernelGGL(unit, dim3((unsigned)units), dim3(kUnitThreads), 0, stream, x);
+        return hipGetLastError();
+    }
     auto kernel = idx != nullptr ? k_attn_stream_e4m3<true> : k_attn_stream_e4m3<false>;
     hipLaunchKernelGGL(kernel, dim3(waves / kAttnWaves), dim3(kAttnThreads), plan.lds_bytes,
                        stream, x);

@@ -332,6 +332,14 @@ def _stream(device=None) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
 
+def _stream_of(device) -> int:
+    """The current stream's handle on ``device`` (which has an index), without the stream object:
+    2 us less where torch has the call for it."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return _stream(device) if raw is None else raw(device.index)
+
+
 def _check(fn: str, rc: int) -> None:
     if rc != SPARROW_OK:
         raise SparrowError(fn, rc)
@@ -360,6 +368,9 @@ def _expect(t, name, dtype, shape, device):
     The C ABI receives bare pointers: the kernels index every buffer with the sizes in the
     shape struct, so a tensor of another dtype, shape or layout would be read or written
     out of bounds.  The tensor-level wrappers check each buffer before any launch."""
+    if t is not None and t.dtype is dtype and t.shape == shape and t.is_contiguous() and \
+            t.device == device and t.is_cuda:
+        return  # (the usual case first: a small call's time is mostly its host side)
     if t is None:
         raise ValueError(f"{name} is required")
     _require_device(t)
@@ -622,11 +633,14 @@ def tail_stats(alpha, positions, bin_tokens, n_bins, percentile=5.0):
     return q, m, c
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(device):
     """Makes ``device`` the current one for the launches inside, where it is not."""
     import torch
     if device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
+        return _HERE
     return torch.cuda.device(device)
 
 
@@ -636,16 +650,14 @@ def _expect_rows(t, name, shape, device):
     import torch
     if t is None:
         raise ValueError(f"{name} is required")
-    _require_device(t)
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
-    if t.dtype != torch.bfloat16:
-        raise ValueError(f"{name}: dtype {t.dtype}, expected {torch.bfloat16}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != device or not t.is_cuda:
+        _require_device(t)
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected {torch.bfloat16} {shape}")
     st = t.stride()
     row = shape[1] * shape[2]
-    if shape[0] <= 1:
+    if shape[0] <= 1:  # (a size of one has any stride)
         st = (row, shape[2] if shape[1] <= 1 else st[1], st[2])
     elif shape[1] <= 1:
         st = (st[0], shape[2], st[2])
@@ -687,7 +699,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=
     with _on(dev):
         _check("sparrow_qk_norm_rope", sparrow_qk_norm_rope(
             T, Hq, Hk, D, _ptr(q), qs, _ptr(k), ks, _ptr(q_weight), _ptr(k_weight),
-            _ptr(inv_freq), _ptr(positions), float(eps), _ptr(q_out), _ptr(k_out), _stream(dev)))
+            _ptr(inv_freq), _ptr(positions), float(eps), _ptr(q_out), _ptr(k_out), _stream_of(dev)))
     return q_out, k_out
 
 
@@ -718,7 +730,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positio
             T, Hq, Hk, D, _ptr(dq_out), _ptr(dk_out), _ptr(q), qs, _ptr(k), ks, _ptr(q_weight),
             _ptr(k_weight), _ptr(inv_freq), _ptr(positions), float(eps), _ptr(dq), dqs, _ptr(dk),
             dks, _ptr(dws[0]), _ptr(dws[1]), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream(dev)))
+            workspace.numel() * workspace.element_size(), _stream_of(dev)))
     return dq, dk, dws[0], dws[1]
 
 
@@ -773,7 +785,7 @@ def append_kv_e4m3(k_new, v_new, k_cache, v_cache, exps, block_table, seq_lens, 
         _check("sparrow_append_kv_e4m3", sparrow_append_kv_e4m3(
             shape, _ptr(k_new), ks, _ptr(v_new), vs, _ptr(cu_tokens), T, _ptr(k_cache),
             _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens), _ptr(meta),
-            _stream(dev)))
+            _stream_of(dev)))
 
 
 def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_tokens, k_out=None,
@@ -798,7 +810,7 @@ def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_t
     with _on(dev):
         _check("sparrow_read_kv_e4m3", sparrow_read_kv_e4m3(
             shape, _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens),
-            _ptr(cu_tokens), T, _ptr(outs[0]), _ptr(outs[1]), _stream(dev)))
+            _ptr(cu_tokens), T, _ptr(outs[0]), _ptr(outs[1]), _stream_of(dev)))
     return outs[0], outs[1]
 
 
@@ -832,7 +844,7 @@ def _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, sc
         workspace = _workspace(sparrow_workspace_size(
             shape, k_max, SPARROW_OP_DENSE_ATTN if idx is None else SPARROW_OP_SPARSE_ATTN), dev)
     _expect_workspace(workspace, dev)
-    ws = (_ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
+    ws = (_ptr(workspace), workspace.numel() * workspace.element_size(), _stream_of(dev))
     head = (shape, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table),
             _ptr(seq_lens))
     with _on(dev):

@@ -48,6 +48,10 @@ def test_other_refusals(sparse):
     assert call(sparse, ws=FAKE + 4) == S.SPARROW_EINVAL
     assert call(sparse, good_shape(batch=0), ws=None) == S.SPARROW_OK
     assert call(sparse, good_shape(batch=S.SPARROW_MAX_BATCH + 1)) == S.SPARROW_EUNSUPPORTED
+    # 16-token parts of the cache are numbered in 32 bits
+    assert call(sparse, good_shape(num_phys_pages=1 << 28, batch=0)) == S.SPARROW_OK
+    assert call(sparse, good_shape(num_phys_pages=1 << 28)) == S.SPARROW_EUNSUPPORTED
+    assert call(sparse, good_shape(num_phys_pages=1 << 25, page_size=128)) == S.SPARROW_EUNSUPPORTED
     if sparse:
         assert call(True, k_max=0) == S.SPARROW_EINVAL
         assert call(True, k_max=S.SPARROW_MAX_PAGES_PER_SEQ + 1) == S.SPARROW_EINVAL
