@@ -64,6 +64,70 @@ __device__ __forceinline__ void load_chunk(Chunk &c, const uint16_t *__restrict_
         c.v[j] = ld16_nt(vp + j * kHeadDim);
 }
 
+// Position cursor over the (sequence, head, page) list.
+struct Cursor {
+    int b, h, j, cnt;  // sequence, KV head, page position within the unit, unit length
+    int64_t pos;       // global position
+};
+
+// One page-list batch of at most kBatch pages of one unit; lane i describes page j0 + i.
+struct Batch {
+    int b, h, j0, n, L;
+    bool ends_unit;
+    int lp;    // logical page (-1: none)
+    int phys;  // physical page, as the block table gives it (checked when used)
+    int tok0;  // first token of the page
+};
+
+// A page-list batch is fetched in two phases so that no wait on its loads drains the K/V
+// loads in flight (a wave's loads complete in order): fetch_batch_begin issues the index
+// loads and advances the cursor; fetch_batch_end, called one chunk later, when the
+// indices have arrived, issues the block-table loads, which are consumed a batch later.
+template <bool kSparse>
+__device__ __forceinline__ void fetch_batch_begin(const AttnArgs &a, const int32_t *s_off,
+                                                  Cursor &c, int64_t pos_end, Batch &t, int lane)
+{
+    const int Hkv = a.num_kv_heads;
+    t.b = c.b;
+    t.h = c.h;
+    t.j0 = c.j;
+    const int64_t left = pos_end - c.pos;
+    int n = c.cnt - c.j;
+    if (n > kBatch)
+        n = kBatch;
+    if (n > left)
+        n = (int)left;
+    t.n = n;
+    t.ends_unit = c.j + n == c.cnt;
+    t.L = clamp_len(a.seq_lens[c.b], a.ps, a.max_pages);
+    t.lp = -1;
+    if (lane < n)
+        t.lp = kSparse ? a.idx[((int64_t)c.b * Hkv + c.h) * a.k_max + c.j + lane] : c.j + lane;
+    c.pos += n;
+    c.j += n;
+    if (c.j == c.cnt && c.pos < pos_end) {  // next unit with pages
+        c.j = 0;
+        if (++c.h == Hkv) {
+            c.h = 0;
+            do {
+                ++c.b;
+            } while (s_off[c.b + 1] == s_off[c.b]);
+        }
+        c.cnt = s_off[c.b + 1] - s_off[c.b];
+    }
+}
+
+__device__ __forceinline__ void fetch_batch_end(const AttnArgs &a, Batch &t)
+{
+    const int np = (t.L + a.ps - 1) / a.ps;
+    t.phys = -1;
+    t.tok0 = 0;
+    if (t.lp >= 0 && t.lp < np) {  // entries outside the sequence: no page
+        t.phys = a.block_table[(int64_t)t.b * a.max_pages + t.lp];
+        t.tok0 = t.lp * a.ps;
+    }
+}
+
 // One live 16-token chunk into a wave's online-softmax state: logits on MFMA, the running
 // maximum and sum in the log2 domain, O^T += V^T P.  `valid` (>= 1) tokens of the chunk
 // lie inside the sequence; the rest get weight 0 and their V rows are zeroed.
