@@ -22,10 +22,10 @@ struct RopeGradArgs {
     uint16_t *dq, *dk;
     int64_t dq_stride, dk_stride;
     float *dq_weight, *dk_weight;
-    float *partials;  // [kRopeGradBlocks][2][128]
+    float *partials;  // [kRopeGradBlocks][128]
 };
 
-constexpr int kRopeGradBlocks = 1024;  // workgroups of the gradient at most
+constexpr int kRopeGradBlocks = 512;  // workgroups of the gradient at most
 
 hipError_t launch_qk_norm_rope(const RopeArgs &a, uint16_t *q_out, uint16_t *k_out,
                                hipStream_t stream);

@@ -11,7 +11,8 @@
 // rotated pairs, in two 16-byte vectors, so a wave takes 8 rows (heads of one token) per pass and
 // the row sums are three DPP steps.  A token's 64 angles are computed once per wave, one per
 // lane, in fp64: p * inv_freq / 2pi less its nearest integer keeps full fp32 precision of the
-// turn at any int32 position.
+// turn at any int32 position; sine and cosine of a turn are one instruction each (off by at most
+// 2^-22.9 over 2^24 turns against fp64, sincospi by 2^-24.2: both far below the bf16 step).
 // Bound by HBM: 512 B per row for ~10 flops an element.
 #include "qk_norm_rope.h"
 
@@ -48,6 +49,20 @@ __device__ __forceinline__ float sum8(float x)
     return x;
 }
 
+// Sum over the lanes l, l + 8, ... l + 56 (every lane gets it): a rotation by 8 inside each 16, then
+// swaps of 16-lane rows and of halves with a copy, which leave a lane its own and its partner's.
+__device__ __forceinline__ float sum_rows(float x)
+{
+    constexpr int kRor8 = 0x128;
+    x += dpp_f<kRor8>(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 __device__ __forceinline__ void unpack8(u32x4_t v, float (&f)[8])
 {
 #pragma unroll
@@ -71,10 +86,16 @@ struct Row {
         lo = ld16_nt(p + 8 * l);
         hi = ld16_nt(p + kHalf + 8 * l);
     }
+    template <bool kStream>
     __device__ __forceinline__ void store(uint16_t *p, int l) const
     {
-        st16(p + 8 * l, lo);
-        st16(p + kHalf + 8 * l, hi);
+        if (kStream) {
+            __builtin_nontemporal_store(lo, reinterpret_cast<u32x4_t *>(p + 8 * l));
+            __builtin_nontemporal_store(hi, reinterpret_cast<u32x4_t *>(p + kHalf + 8 * l));
+        } else {
+            st16(p + 8 * l, lo);
+            st16(p + kHalf + 8 * l, hi);
+        }
     }
 };
 
@@ -84,8 +105,7 @@ __device__ __forceinline__ void angles(double inv_freq, int pos, int lane, float
 {
     const double turns = (double)pos * (inv_freq * kInvTwoPi);
     const float t = (float)(turns - __builtin_rint(turns));
-    float sv, cv;
-    sincospif(2.f * t, &sv, &cv);
+    const float cv = __builtin_amdgcn_cosf(t), sv = __builtin_amdgcn_sinf(t);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         c[j] = __shfl(cv, 8 * j + (lane & 7), 64);
@@ -104,6 +124,7 @@ __device__ __forceinline__ float inv_rms(const float (&x0)[8], const float (&x1)
 }
 
 // A wave takes one pass (8 query rows, or 8 key rows) of one token at a time.
+template <bool kStream>
 __global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope(RopeArgs a, uint16_t *q_out,
                                                                uint16_t *k_out)
 {
@@ -149,28 +170,16 @@ __global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope(RopeArgs a, uint1
         }
         if (live) {
             const Row y = {pack8(y0), pack8(y1)};
-            y.store((is_q ? q_out : k_out) + (t * heads + h) * kHeadDim, l);
+            y.store<kStream>((is_q ? q_out : k_out) + (t * heads + h) * kHeadDim, l);
         }
     }
 }
 
-// One pass of the gradient: dx of 8 rows, and the rows' parts of dw added to dw0, dw1.
-__device__ __forceinline__ void grad_rows(const uint16_t *dy, const uint16_t *x, uint16_t *dx,
-                                          int h, int heads, bool skip, int l, float eps,
-                                          const Row &w, const float (&c)[8], const float (&s)[8],
+// One pass of the gradient: dx of 8 rows into d, and the rows' parts of dw added to dw0, dw1.
+__device__ __forceinline__ void grad_rows(const Row &xr, Row &d, float eps, const Row &w,
+                                          const float (&c)[8], const float (&s)[8],
                                           float (&dw0)[8], float (&dw1)[8])
 {
-    if (h >= heads)
-        return;  // (all 8 lanes of the row)
-    Row d;
-    if (skip) {
-        d.lo = d.hi = (u32x4_t){0u, 0u, 0u, 0u};
-        d.store(dx + h * kHeadDim, l);
-        return;
-    }
-    Row xr;
-    xr.load(x + h * kHeadDim, l);
-    d.load(dy + h * kHeadDim, l);
     float x0[8], x1[8], d0[8], d1[8], w0[8], w1[8];
     unpack8(xr.lo, x0);
     unpack8(xr.hi, x1);
@@ -199,21 +208,112 @@ __device__ __forceinline__ void grad_rows(const uint16_t *dy, const uint16_t *x,
     }
     d.lo = pack8(d0);
     d.hi = pack8(d1);
-    d.store(dx + h * kHeadDim, l);
 }
 
-// The wave's sums over its 8 rows and the workgroup's over its waves: 128 floats at `out`.
-__device__ void block_dw(float (&dw0)[8], float (&dw1)[8], float *s_dw, int lane, int wave,
-                         float *out)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int m = 8; m < 64; m <<= 1) {
-            dw0[i] += __shfl_xor(dw0[i], m, 64);
-            dw1[i] += __shfl_xor(dw1[i], m, 64);
+// What a wave works through: the passes of a token one after another, then those of the token `waves`
+// further on, so that neighbouring waves read neighbouring rows.  Where there are more waves than
+// tokens a token's passes are shared out: run u is token u / runs, passes [r passes / runs, (r + 1)
+// passes / runs) with r = u % runs, and a wave takes the runs w, w + waves, ...
+struct Walk {
+    int64_t u, t;
+    int pass, stop, runs;
+    bool more, fresh;  // there is a pass; it is the first of its token here
+
+    __device__ __forceinline__ void place(int64_t tokens, int passes)
+    {
+        t = u / runs;
+        const int r = (int)(u - t * runs);
+        pass = r * passes / runs;
+        stop = (r + 1) * passes / runs;
+        more = t < tokens;
+        fresh = true;
+    }
+    __device__ __forceinline__ void start(int64_t w, int64_t waves, int64_t tokens, int passes)
+    {
+        const int64_t share = waves / (tokens > 0 ? tokens : 1);
+        runs = share < 1 ? 1 : (share < passes ? (int)share : passes);
+        u = w;
+        place(tokens, passes);
+    }
+    __device__ __forceinline__ void step(int64_t waves, int64_t tokens, int passes)
+    {
+        fresh = false;
+        if (++pass == stop) {
+            u += waves;
+            place(tokens, passes);
         }
-    __syncthreads();  // s_dw is free
+    }
+};
+
+// Workgroups [0, q_blocks) take the query heads, the others the key heads, so that a wave keeps one
+// weight's gradient.  The workgroups' sums go to `partials` and are added in a fixed order by
+// k_rope_dw, so that results do not depend on which workgroup ends first.
+template <bool kStream>
+__global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope_bwd(RopeArgs a, RopeGradArgs g,
+                                                                   int q_blocks)
+{
+    __shared__ float s_dw[kRopeWaves * kHeadDim];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l = lane & 7;
+    const bool is_q = (int)blockIdx.x < q_blocks;
+    const int heads = is_q ? a.num_q_heads : a.num_k_heads;
+    const uint16_t *x = is_q ? a.q : a.k;
+    const uint16_t *dy = is_q ? g.dq_out : g.dk_out;
+    uint16_t *dx = is_q ? g.dq : g.dk;
+    const int64_t x_stride = is_q ? a.q_stride : a.k_stride;
+    const int64_t dx_stride = is_q ? g.dq_stride : g.dk_stride;
+    const uint16_t *weight = is_q ? a.q_weight : a.k_weight;
+    const int passes = (heads + kRows - 1) / kRows;
+    const int64_t waves = (int64_t)(is_q ? q_blocks : gridDim.x - q_blocks) * kRopeWaves;
+    const int64_t w = (int64_t)(blockIdx.x - (is_q ? 0 : q_blocks)) * kRopeWaves + wave;
+    Walk k;
+    k.start(w, waves, a.tokens, passes);
+
+    const double inv_freq = a.inv_freq[8 * l + (lane >> 3)];
+    Row wt;
+    wt.lo = ld16(weight + 8 * l);
+    wt.hi = ld16(weight + kHalf + 8 * l);
+    float dw0[8] = {}, dw1[8] = {}, c[8], s[8];
+    Row xr = {}, d = {};
+    int pos = 0;
+    auto load = [&]() __attribute__((always_inline)) {
+        const int h = k.pass * kRows + (lane >> 3);
+        if (k.fresh)
+            pos = a.positions[k.t];
+        if (h < heads) {
+            xr.load(x + k.t * x_stride + h * kHeadDim, l);
+            d.load(dy + (k.t * heads + h) * kHeadDim, l);
+        }
+    };
+    if (k.more)
+        load();
+    while (k.more) {
+        const int64_t t = k.t;
+        const bool fresh = k.fresh;
+        const int h = k.pass * kRows + (lane >> 3), pos_now = pos;
+        const Row x_now = xr;
+        Row d_now = d;
+        k.step(waves, a.tokens, passes);
+        if (k.more)
+            load();
+        if (fresh)
+            angles(inv_freq, pos_now, lane, c, s);
+        if (h < heads) {  // (all 8 lanes of a row)
+            if (pos_now < 0)
+                d_now.lo = d_now.hi = (u32x4_t){0u, 0u, 0u, 0u};
+            else
+                grad_rows(x_now, d_now, a.eps, wt, c, s, dw0, dw1);
+            d_now.store<kStream>(dx + t * dx_stride + h * kHeadDim, l);
+        }
+    }
+
+    // ---- the wave's sums over its 8 rows, the workgroup's over its waves
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        dw0[i] = sum_rows(dw0[i]);
+        dw1[i] = sum_rows(dw1[i]);
+    }
     if (lane < 8)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -223,66 +323,59 @@ __device__ void block_dw(float (&dw0)[8], float (&dw1)[8], float *s_dw, int lane
     __syncthreads();
     if (threadIdx.x < kHeadDim) {
         float v = 0.f;
-        for (int w = 0; w < kRopeWaves; ++w)
-            v += s_dw[w * kHeadDim + threadIdx.x];
-        out[threadIdx.x] = v;
+        for (int k = 0; k < kRopeWaves; ++k)
+            v += s_dw[k * kHeadDim + threadIdx.x];
+        g.partials[(int64_t)blockIdx.x * kHeadDim + threadIdx.x] = v;
     }
 }
 
-// A wave walks over tokens with all their heads and keeps the weights' gradients in registers;
-// the workgroups' sums go to `partials` and are added in a fixed order by k_rope_dw, so that
-// results do not depend on which workgroup ends first.
-__global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope_bwd(RopeArgs a, RopeGradArgs g)
-{
-    __shared__ float s_dw[kRopeWaves * kHeadDim];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l = lane & 7;
-    const double inv_freq = a.inv_freq[8 * l + (lane >> 3)];
-    Row wq, wk;
-    wq.lo = ld16(a.q_weight + 8 * l);
-    wq.hi = ld16(a.q_weight + kHalf + 8 * l);
-    wk.lo = ld16(a.k_weight + 8 * l);
-    wk.hi = ld16(a.k_weight + kHalf + 8 * l);
-    float q0[8] = {}, q1[8] = {}, k0[8] = {}, k1[8] = {};
-    for (int64_t t = (int64_t)blockIdx.x * kRopeWaves + wave; t < a.tokens;
-         t += (int64_t)gridDim.x * kRopeWaves) {
-        const int pos = a.positions[t];
-        const bool skip = pos < 0;
-        float c[8], s[8];
-        angles(inv_freq, pos, lane, c, s);
-        for (int h = lane >> 3; h - (lane >> 3) < a.num_q_heads; h += kRows)
-            grad_rows(g.dq_out + t * a.num_q_heads * kHeadDim, a.q + t * a.q_stride,
-                      g.dq + t * g.dq_stride, h, a.num_q_heads, skip, l, a.eps, wq, c, s, q0, q1);
-        for (int h = lane >> 3; h - (lane >> 3) < a.num_k_heads; h += kRows)
-            grad_rows(g.dk_out + t * a.num_k_heads * kHeadDim, a.k + t * a.k_stride,
-                      g.dk + t * g.dk_stride, h, a.num_k_heads, skip, l, a.eps, wk, c, s, k0, k1);
-    }
-    float *out = g.partials + (int64_t)blockIdx.x * 2 * kHeadDim;
-    block_dw(q0, q1, s_dw, lane, wave, out);
-    block_dw(k0, k1, s_dw, lane, wave, out + kHeadDim);
-}
-
-// dw from the workgroups' sums: 8 channels a workgroup, 32 threads a channel.
+// dw from the workgroups' sums: 8 channels a workgroup, 128 threads a channel with their loads all
+// under way at once.
+constexpr int kDwThreads = 1024;
 constexpr int kDwChannels = 8;
-constexpr int kDwParts = kRopeThreads / kDwChannels;
+constexpr int kDwParts = kDwThreads / kDwChannels;
+constexpr int kDwLoads = kRopeGradBlocks / kDwParts;
 
-__global__ __launch_bounds__(kRopeThreads) void k_rope_dw(const float *partials, int blocks,
-                                                          float *dq_weight, float *dk_weight)
+__global__ __launch_bounds__(kDwThreads) void k_rope_dw(const float *partials, int q_blocks,
+                                                        int blocks, float *dq_weight,
+                                                        float *dk_weight)
 {
     __shared__ float s_sum[kDwParts][kDwChannels];
+    constexpr int kGroups = kHeadDim / kDwChannels;  // workgroups per weight
+    const bool is_q = blockIdx.x < kGroups;
     const int ch = threadIdx.x % kDwChannels, part = threadIdx.x / kDwChannels;
-    const int i = blockIdx.x * kDwChannels + ch;  // of the two weights' 256
-    float v = 0.f;
-    for (int b = part; b < blocks; b += kDwParts)
-        v += partials[(int64_t)b * 2 * kHeadDim + i];
-    s_sum[part][ch] = v;
-    __syncthreads();
-    if (part == 0) {
-        for (int p = 1; p < kDwParts; ++p)
-            v += s_sum[p][ch];
-        (i < kHeadDim ? dq_weight : dk_weight)[i & (kHeadDim - 1)] = v;
+    const int i = (is_q ? blockIdx.x : blockIdx.x - kGroups) * kDwChannels + ch;
+    const int b0 = is_q ? 0 : q_blocks, b1 = is_q ? q_blocks : blocks;
+    float v[kDwLoads];
+#pragma unroll
+    for (int k = 0; k < kDwLoads; ++k) {
+        const int b = b0 + part + k * kDwParts;
+        v[k] = b < b1 ? partials[(int64_t)b * kHeadDim + i] : 0.f;
     }
+#pragma unroll
+    for (int k = 1; k < kDwLoads; ++k)
+        v[0] += v[k];
+    s_sum[part][ch] = v[0];
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        float sum = 0.f;
+        for (int p = part; p < kDwParts; p += 8)
+            sum += s_sum[p][ch];
+#pragma unroll
+        for (int m = 8; m < 64; m <<= 1)
+            sum += __shfl_xor(sum, m, 64);
+        if (part == 0)
+            (is_q ? dq_weight : dk_weight)[i] = sum;
+    }
+}
+
+// Whether a call's rows are written past the caches.  That is faster where they would not stay in the
+// 256 MB memory-side cache anyway, and takes them from the kernel that reads them where they
+// would: 32 + 8 heads, this kernel / with a copy of q_out behind it, us, plain -> streamed stores:
+// 168 MB of rows 54 / 92 -> 56 / 103, 252 MB 79 / 167 -> 84 / 161, 671 MB 234 / 440 -> 223 / 433.
+bool stream_rows(const RopeArgs &a)
+{
+    return a.tokens * (a.num_q_heads + a.num_k_heads) * (int64_t)(kHeadDim * 2) >= 224 << 20;
 }
 
 }  // namespace
@@ -293,23 +386,27 @@ hipError_t launch_qk_norm_rope(const RopeArgs &a, uint16_t *q_out, uint16_t *k_o
     const int64_t passes = (a.num_q_heads + kRows - 1) / kRows + (a.num_k_heads + kRows - 1) / kRows;
     int64_t blocks = (a.tokens * passes + kRopeWaves - 1) / kRopeWaves;
     blocks = blocks < kRopeBlocks ? blocks : kRopeBlocks;
-    hipLaunchKernelGGL(k_qk_norm_rope, dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, a,
-                       q_out, k_out);
+    auto kernel = stream_rows(a) ? k_qk_norm_rope<true> : k_qk_norm_rope<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, a, q_out,
+                       k_out);
     return hipGetLastError();
 }
 
 hipError_t launch_qk_norm_rope_bwd(const RopeArgs &a, const RopeGradArgs &g, hipStream_t stream)
 {
-    const int64_t want = (a.tokens + kRopeWaves - 1) / kRopeWaves;
-    const int blocks = (int)(want < kRopeGradBlocks ? want : kRopeGradBlocks);
-    if (blocks > 0) {
-        hipLaunchKernelGGL(k_qk_norm_rope_bwd, dim3(blocks), dim3(kRopeThreads), 0, stream, a, g);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess)
-            return e;
-    }
-    hipLaunchKernelGGL(k_rope_dw, dim3(2 * kHeadDim / kDwChannels), dim3(kRopeThreads), 0, stream,
-                       g.partials, blocks, g.dq_weight, g.dk_weight);
+    // workgroups in proportion to the two sides' items, at least one each
+    const int64_t qp = (a.num_q_heads + kRows - 1) / kRows, kp = (a.num_k_heads + kRows - 1) / kRows;
+    const int64_t want = (a.tokens * (qp + kp) + kRopeWaves - 1) / kRopeWaves;
+    const int blocks = (int)(want < 2 ? 2 : (want < kRopeGradBlocks ? want : kRopeGradBlocks));
+    int q_blocks = (int)(blocks * qp / (qp + kp));
+    q_blocks = q_blocks < 1 ? 1 : (q_blocks > blocks - 1 ? blocks - 1 : q_blocks);
+    auto kernel = stream_rows(a) ? k_qk_norm_rope_bwd<true> : k_qk_norm_rope_bwd<false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kRopeThreads), 0, stream, a, g, q_blocks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(k_rope_dw, dim3(2 * kHeadDim / kDwChannels), dim3(kDwThreads), 0, stream,
+                       g.partials, q_blocks, blocks, g.dq_weight, g.dk_weight);
     return hipGetLastError();
 }
 
