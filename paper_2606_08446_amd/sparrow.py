@@ -350,11 +350,23 @@ def _workspace(nbytes: int, device):
     return torch.empty(max(int(nbytes), 16), dtype=torch.uint8, device=device)
 
 
-def _expect_workspace(t, device):
-    """Raise unless ``t`` is contiguous memory on ``device`` (its size is the library's check)."""
+def _given(t, name, dtype, shape, device):
+    """The caller's output ``t`` after its check, or a new one."""
+    if t is None:
+        import torch
+        return torch.empty(shape, dtype=dtype, device=device)
+    _expect(t, name, dtype, shape, device)
+    return t
+
+
+def _given_workspace(t, nbytes, device):
+    """The caller's workspace (its size is the library's check), or a new one of ``nbytes``."""
+    if t is None:
+        return _workspace(nbytes, device)
     _require_device(t)
     if t.device != device or not t.is_contiguous():
         raise ValueError(f"workspace must be contiguous memory on {device}")
+    return t
 
 
 def _require_device(t):
@@ -690,10 +702,8 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=
     import torch
     T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
     dev = q.device
-    q_out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev) if q_out is None else q_out
-    k_out = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=dev) if k_out is None else k_out
-    _expect(q_out, "q_out", torch.bfloat16, (T, Hq, D), dev)
-    _expect(k_out, "k_out", torch.bfloat16, (T, Hk, D), dev)
+    q_out = _given(q_out, "q_out", torch.bfloat16, (T, Hq, D), dev)
+    k_out = _given(k_out, "k_out", torch.bfloat16, (T, Hk, D), dev)
     if T == 0:
         return q_out, k_out
     with _on(dev):
@@ -712,26 +722,22 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positio
     dev = q.device
     _expect(dq_out, "dq_out", torch.bfloat16, (T, Hq, D), dev)
     _expect(dk_out, "dk_out", torch.bfloat16, (T, Hk, D), dev)
+    dqs = Hq * D if dq is None else _expect_rows(dq, "dq", (T, Hq, D), dev)
+    dks = Hk * D if dk is None else _expect_rows(dk, "dk", (T, Hk, D), dev)
     dq = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev) if dq is None else dq
     dk = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=dev) if dk is None else dk
-    dqs, dks = _expect_rows(dq, "dq", (T, Hq, D), dev), _expect_rows(dk, "dk", (T, Hk, D), dev)
-    dws = []
-    for name, w in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
-        w = torch.empty(D, dtype=torch.float32, device=dev) if w is None else w
-        _expect(w, name, torch.float32, (D,), dev)
-        dws.append(w)
+    dq_weight = _given(dq_weight, "dq_weight", torch.float32, (D,), dev)
+    dk_weight = _given(dk_weight, "dk_weight", torch.float32, (D,), dev)
     if T == 0:
-        return dq, dk, dws[0].zero_(), dws[1].zero_()
-    if workspace is None:
-        workspace = _workspace(SPARROW_ROPE_WORKSPACE_BYTES, dev)
-    _expect_workspace(workspace, dev)
+        return dq, dk, dq_weight.zero_(), dk_weight.zero_()
+    workspace = _given_workspace(workspace, SPARROW_ROPE_WORKSPACE_BYTES, dev)
     with _on(dev):
         _check("sparrow_qk_norm_rope_bwd", sparrow_qk_norm_rope_bwd(
             T, Hq, Hk, D, _ptr(dq_out), _ptr(dk_out), _ptr(q), qs, _ptr(k), ks, _ptr(q_weight),
             _ptr(k_weight), _ptr(inv_freq), _ptr(positions), float(eps), _ptr(dq), dqs, _ptr(dk),
-            dks, _ptr(dws[0]), _ptr(dws[1]), _ptr(workspace),
+            dks, _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream_of(dev)))
-    return dq, dk, dws[0], dws[1]
+    return dq, dk, dq_weight, dk_weight
 
 
 def new_cache_e4m3(num_phys_pages, num_kv_heads, page_size, device):
@@ -799,19 +805,16 @@ def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_t
     T = int(num_tokens)
     if cu_tokens is not None:
         _expect(cu_tokens, "cu_tokens", torch.int32, (B + 1,), dev)
-    outs = []
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        t = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=dev) if t is None else t
-        _expect(t, name, torch.bfloat16, (T, Hkv, D), dev)
-        outs.append(t)
+    k_out = _given(k_out, "k_out", torch.bfloat16, (T, Hkv, D), dev)
+    v_out = _given(v_out, "v_out", torch.bfloat16, (T, Hkv, D), dev)
     if B == 0 or T == 0:
-        return outs[0], outs[1]
+        return k_out, v_out
     shape = make_shape(B, Hkv, Hkv, ps, M, P, D)
     with _on(dev):
         _check("sparrow_read_kv_e4m3", sparrow_read_kv_e4m3(
             shape, _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens),
-            _ptr(cu_tokens), T, _ptr(outs[0]), _ptr(outs[1]), _stream_of(dev)))
-    return outs[0], outs[1]
+            _ptr(cu_tokens), T, _ptr(k_out), _ptr(v_out), _stream_of(dev)))
+    return k_out, v_out
 
 
 def _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, scale, out, out_dtype,
@@ -832,18 +835,15 @@ def _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, sc
         k_max = idx.shape[2]
         _expect(k, "k", torch.int32, (B,), dev)
         _expect(idx, "idx", torch.int32, (B, Hkv, k_max), dev)
-    if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32 if out_dtype == SPARROW_OUT_F32
-                          else torch.bfloat16, device=dev)
-    _expect_out(out, out_dtype, (B, Hq, D), dev)
+    out = _given(out, "out", torch.float32 if out_dtype == SPARROW_OUT_F32 else torch.bfloat16,
+                 (B, Hq, D), dev)
     if B == 0:
         return out
     scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
     shape = make_shape(B, Hq, Hkv, ps, M, P, D)
-    if workspace is None:
-        workspace = _workspace(sparrow_workspace_size(
-            shape, k_max, SPARROW_OP_DENSE_ATTN if idx is None else SPARROW_OP_SPARSE_ATTN), dev)
-    _expect_workspace(workspace, dev)
+    workspace = _given_workspace(workspace, None if workspace is not None else
+                                 sparrow_workspace_size(shape, k_max, SPARROW_OP_DENSE_ATTN if idx is
+                                                        None else SPARROW_OP_SPARSE_ATTN), dev)
     ws = (_ptr(workspace), workspace.numel() * workspace.element_size(), _stream_of(dev))
     head = (shape, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table),
             _ptr(seq_lens))
