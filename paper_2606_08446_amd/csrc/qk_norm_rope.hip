@@ -123,6 +123,14 @@ __device__ __forceinline__ float inv_rms(const float (&x0)[8], const float (&x1)
     return rsqrtf(sum8(ss) * (1.f / kHeadDim) + eps);
 }
 
+// The workgroup's place among `n` (a multiple of 8), counted so that each of the 8 XCDs, which take
+// workgroups in turn, works on one contiguous eighth of the rows (64K tokens of 32 + 8 heads: 233 ->
+// 225 us).
+__device__ __forceinline__ int64_t place_by_xcd(int block, int n)
+{
+    return (int64_t)(block % 8) * (n / 8) + block / 8;
+}
+
 // A wave takes one pass (8 query rows, or 8 key rows) of one token at a time.
 template <bool kStream>
 __global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope(RopeArgs a, uint16_t *q_out,
@@ -134,7 +142,7 @@ __global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope(RopeArgs a, uint1
     const int passes = q_passes + (a.num_k_heads + kRows - 1) / kRows;
     const double inv_freq = a.inv_freq[8 * l + (lane >> 3)];
     const int64_t all = a.tokens * passes;
-    for (int64_t w = (int64_t)blockIdx.x * kRopeWaves +
+    for (int64_t w = place_by_xcd(blockIdx.x, gridDim.x) * kRopeWaves +
                      __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
          w < all; w += (int64_t)gridDim.x * kRopeWaves) {
         const int64_t t = w / passes;
@@ -385,7 +393,7 @@ hipError_t launch_qk_norm_rope(const RopeArgs &a, uint16_t *q_out, uint16_t *k_o
 {
     const int64_t passes = (a.num_q_heads + kRows - 1) / kRows + (a.num_k_heads + kRows - 1) / kRows;
     int64_t blocks = (a.tokens * passes + kRopeWaves - 1) / kRopeWaves;
-    blocks = blocks < kRopeBlocks ? blocks : kRopeBlocks;
+    blocks = blocks < kRopeBlocks ? (blocks + 7) / 8 * 8 : kRopeBlocks;
     auto kernel = stream_rows(a) ? k_qk_norm_rope<true> : k_qk_norm_rope<false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, a, q_out,
                        k_out);

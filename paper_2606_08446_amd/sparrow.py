@@ -11,7 +11,6 @@ visible, the tensor-level calls raise.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -645,15 +644,18 @@ def tail_stats(alpha, positions, bin_tokens, n_bins, percentile=5.0):
     return q, m, c
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _on(device):
-    """Makes ``device`` the current one for the launches inside, where it is not."""
+def _launch(name, device, *args):
+    """Calls the entry point ``name`` on ``device``'s current stream (its last argument), with that
+    device the current one, and raises on a negative status."""
     import torch
+    fn = getattr(load(), name)
     if device.index == torch.cuda.current_device():
-        return _HERE
-    return torch.cuda.device(device)
+        rc = fn(*args, _stream_of(device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream_of(device))
+    if rc != SPARROW_OK:
+        raise SparrowError(name, rc)
 
 
 def _expect_rows(t, name, shape, device):
@@ -706,10 +708,9 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=
     k_out = _given(k_out, "k_out", torch.bfloat16, (T, Hk, D), dev)
     if T == 0:
         return q_out, k_out
-    with _on(dev):
-        _check("sparrow_qk_norm_rope", sparrow_qk_norm_rope(
-            T, Hq, Hk, D, _ptr(q), qs, _ptr(k), ks, _ptr(q_weight), _ptr(k_weight),
-            _ptr(inv_freq), _ptr(positions), float(eps), _ptr(q_out), _ptr(k_out), _stream_of(dev)))
+    _launch("sparrow_qk_norm_rope", dev, T, Hq, Hk, D, q.data_ptr(), qs, k.data_ptr(), ks,
+            q_weight.data_ptr(), k_weight.data_ptr(), inv_freq.data_ptr(), positions.data_ptr(),
+            float(eps), q_out.data_ptr(), k_out.data_ptr())
     return q_out, k_out
 
 
@@ -731,12 +732,11 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positio
     if T == 0:
         return dq, dk, dq_weight.zero_(), dk_weight.zero_()
     workspace = _given_workspace(workspace, SPARROW_ROPE_WORKSPACE_BYTES, dev)
-    with _on(dev):
-        _check("sparrow_qk_norm_rope_bwd", sparrow_qk_norm_rope_bwd(
-            T, Hq, Hk, D, _ptr(dq_out), _ptr(dk_out), _ptr(q), qs, _ptr(k), ks, _ptr(q_weight),
-            _ptr(k_weight), _ptr(inv_freq), _ptr(positions), float(eps), _ptr(dq), dqs, _ptr(dk),
-            dks, _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream_of(dev)))
+    _launch("sparrow_qk_norm_rope_bwd", dev, T, Hq, Hk, D, dq_out.data_ptr(), dk_out.data_ptr(),
+            q.data_ptr(), qs, k.data_ptr(), ks, q_weight.data_ptr(), k_weight.data_ptr(),
+            inv_freq.data_ptr(), positions.data_ptr(), float(eps), dq.data_ptr(), dqs,
+            dk.data_ptr(), dks, dq_weight.data_ptr(), dk_weight.data_ptr(), workspace.data_ptr(),
+            workspace.nbytes)
     return dq, dk, dq_weight, dk_weight
 
 
@@ -787,11 +787,9 @@ def append_kv_e4m3(k_new, v_new, k_cache, v_cache, exps, block_table, seq_lens, 
     if B == 0 or T == 0:
         return
     shape = make_shape(B, Hkv, Hkv, ps, M, P, D, landmark=landmark)
-    with _on(dev):
-        _check("sparrow_append_kv_e4m3", sparrow_append_kv_e4m3(
-            shape, _ptr(k_new), ks, _ptr(v_new), vs, _ptr(cu_tokens), T, _ptr(k_cache),
-            _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens), _ptr(meta),
-            _stream_of(dev)))
+    _launch("sparrow_append_kv_e4m3", dev, ctypes.byref(shape), k_new.data_ptr(), ks,
+            v_new.data_ptr(), vs, _ptr(cu_tokens), T, k_cache.data_ptr(), v_cache.data_ptr(),
+            exps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), meta.data_ptr())
 
 
 def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_tokens, k_out=None,
@@ -810,10 +808,9 @@ def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_t
     if B == 0 or T == 0:
         return k_out, v_out
     shape = make_shape(B, Hkv, Hkv, ps, M, P, D)
-    with _on(dev):
-        _check("sparrow_read_kv_e4m3", sparrow_read_kv_e4m3(
-            shape, _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table), _ptr(seq_lens),
-            _ptr(cu_tokens), T, _ptr(k_out), _ptr(v_out), _stream_of(dev)))
+    _launch("sparrow_read_kv_e4m3", dev, ctypes.byref(shape), k_cache.data_ptr(),
+            v_cache.data_ptr(), exps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+            _ptr(cu_tokens), T, k_out.data_ptr(), v_out.data_ptr())
     return k_out, v_out
 
 
@@ -844,16 +841,14 @@ def _attention_e4m3(q, k_cache, v_cache, exps, block_table, seq_lens, k, idx, sc
     workspace = _given_workspace(workspace, None if workspace is not None else
                                  sparrow_workspace_size(shape, k_max, SPARROW_OP_DENSE_ATTN if idx is
                                                         None else SPARROW_OP_SPARSE_ATTN), dev)
-    ws = (_ptr(workspace), workspace.numel() * workspace.element_size(), _stream_of(dev))
-    head = (shape, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(exps), _ptr(block_table),
-            _ptr(seq_lens))
-    with _on(dev):
-        if idx is None:
-            _check("sparrow_dense_decode_attn_e4m3", sparrow_dense_decode_attn_e4m3(
-                *head, scale, _ptr(out), int(out_dtype), *ws))
-        else:
-            _check("sparrow_sparse_decode_attn_e4m3", sparrow_sparse_decode_attn_e4m3(
-                *head, _ptr(k), _ptr(idx), k_max, scale, _ptr(out), int(out_dtype), *ws))
+    cache = (ctypes.byref(shape), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+             exps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr())
+    rest = (scale, out.data_ptr(), int(out_dtype), workspace.data_ptr(), workspace.nbytes)
+    if idx is None:
+        _launch("sparrow_dense_decode_attn_e4m3", dev, *cache, *rest)
+    else:
+        _launch("sparrow_sparse_decode_attn_e4m3", dev, *cache, k.data_ptr(), idx.data_ptr(),
+                k_max, *rest)
     return out
 
 
