@@ -352,9 +352,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
             a.plan_off[b] = s_off[b];
 
     const int64_t P = (int64_t)uniform(s_off[B]) * Hkv;
-    // (the rule of k_attn_stream, with tiles of twice its chunks)
-    int64_t W = P * (a.ps >> 4) / (2 * kParts);
-    W = W > a.fine_waves ? W : a.fine_waves;
+    // A wave has at least one tile, with more than 8 query heads per KV head four (the merge reads a
+    // row per head and wave), and at least one page.  A whole dense call, us, tiles 1 / 2 / 4: 8 units
+    // of 4097 tokens x 2 heads 11.6 / 12.8 / 14.3, of 2048 10.4 / 10.5 / 12.7, 16 of 4096 x 16 heads
+    // 17.7 / 17.6 / 16.0; no difference from 32 units of 8192 tokens on.
+    int64_t W = P * (a.ps >> 4) / (kParts * (G > 8 ? 4 : 1));
+    W = W > 1 ? W : 1;
     W = W < a.max_waves ? W : a.max_waves;
     W = W < P ? W : P;
     const int w = blockIdx.x * kAttnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -683,7 +686,6 @@ hipError_t launch_attention_e4m3(const sparrow_shape_t &s, const AttnPlan &plan,
     a.num_phys = s.num_phys_pages;
     a.out_bf16 = out_dtype == SPARROW_OUT_BF16 ? 1 : 0;
     a.max_waves = (int)(units * kUnitSegments < waves ? units * kUnitSegments : waves);
-    a.fine_waves = (int)(units * 64 < waves ? units * 64 : waves);
     a.scale_log2 = scale * 1.4426950408889634f;
     if (unit_path(s, idx != nullptr ? k_max : s.max_pages_per_seq)) {
         auto unit = idx != nullptr ? k_attn_unit_e4m3<true> : k_attn_unit_e4m3<false>;
