@@ -414,8 +414,9 @@ hipError_t launch_read_e4m3(const sparrow_shape_t &s, const CacheE4m3 &c,
                             hipStream_t stream)
 {
     const int waves = s.num_kv_heads * (s.page_size / 16);
+    const int per_slot = (waves + kWaves - 1) / kWaves;  // (the kernel strides over the rest)
     const dim3 grid((unsigned)page_slots(num_rows, s.batch, s.page_size),
-                    (waves + kWaves - 1) / kWaves);
+                    per_slot < 65535 ? per_slot : 65535);
     // Rows that would not stay in the 256 MB memory-side cache are written past it (67 MB of codes
     // 83 -> 60 us by itself, the same with a copy of the rows behind it; at 134 MB of rows 32 either
     // way, but the copies behind it 79 -> 91).

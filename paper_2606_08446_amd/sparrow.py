@@ -888,13 +888,26 @@ class SparseDecodeStep:
     """One layer's sparse decode step with preallocated buffers.
 
     ``run(first_pos)`` enqueues: metadata update of the pages touched since
-    ``first_pos`` (skipped when None), page scoring + top-k, sparse attention."""
+    ``first_pos`` (skipped when None), page scoring + top-k, sparse attention.
+
+    With ``exps`` the caches are e4m3 (``new_cache_e4m3``) and every method works on them: the append
+    quantises its rows and keeps the landmarks, attention reads the codes.  There the fused calls
+    are the separate ones in a row, and ``meta_update`` does not apply."""
 
     def __init__(self, q, k_cache, v_cache, block_table, seq_lens, meta, min_pages, frac_num,
                  frac_den, bin_tokens, k_max, scale=None, landmark=SPARROW_LANDMARK_MINMAX,
-                 sink_pages=0, local_pages=0):
+                 sink_pages=0, local_pages=0, exps=None):
         import torch
-        B, Hq, Hkv, ps, D, P, M = _expect_cache(q, k_cache, v_cache, block_table, seq_lens)
+        if exps is None:
+            B, Hq, Hkv, ps, D, P, M = _expect_cache(q, k_cache, v_cache, block_table, seq_lens)
+        else:
+            _require_device(q)
+            B, Hkv, ps, D, P, M = _expect_cache_e4m3(k_cache, v_cache, exps, block_table, seq_lens,
+                                                     q.device)
+            if q.dim() != 3:
+                raise ValueError("q must be [B][Hq][D]")
+            _expect(q, "q", torch.bfloat16, (B, q.shape[1], D), q.device)
+        self.exps = exps
         _expect_meta(meta, P, Hkv, D, landmark, q.device)
         _expect_tables(min_pages, frac_num, q.device)
         self.q, self.k_cache, self.v_cache = q, k_cache, v_cache
@@ -916,8 +929,8 @@ class SparseDecodeStep:
                                                          SPARROW_OP_SPARSE_ATTN), dev)
         # allocated here, not on first use, so that a first call under graph capture
         # allocates nothing
-        self.ws_step = _workspace(sparrow_workspace_size(self.shape, self.k_max,
-                                                         SPARROW_OP_DECODE_STEP), dev)
+        self.ws_step = None if exps is not None else _workspace(
+            sparrow_workspace_size(self.shape, self.k_max, SPARROW_OP_DECODE_STEP), dev)
 
     # Every method takes an optional ``seq_lens`` tensor that replaces the one given at
     # construction for that call (a decode loop advances the lengths step by step).
@@ -937,6 +950,8 @@ class SparseDecodeStep:
 
     def meta_update(self, first_pos, stream, seq_lens=None):
         import torch
+        if self.exps is not None:
+            raise ValueError("the landmarks of an e4m3 cache are kept by its append")
         if first_pos is not None:
             _expect(first_pos, "first_pos", torch.int32, tuple(self.seq_lens.shape),
                     self.q.device)
@@ -946,6 +961,15 @@ class SparseDecodeStep:
 
     def append(self, k_new, v_new, stream, seq_lens=None):
         """Write the decoded token's K/V rows and update its page's metadata."""
+        if self.exps is not None:
+            want = (self.q.shape[0], self.k_cache.shape[1], self.q.shape[2])
+            ks = _expect_rows(k_new, "k_new", want, self.q.device)
+            vs = _expect_rows(v_new, "v_new", want, self.q.device)
+            _check("sparrow_append_kv_e4m3", sparrow_append_kv_e4m3(
+                self.shape, _ptr(k_new), ks, _ptr(v_new), vs, None, want[0], _ptr(self.k_cache),
+                _ptr(self.v_cache), _ptr(self.exps), _ptr(self.block_table), self._lens(seq_lens),
+                _ptr(self.meta), stream))
+            return
         self._rows(k_new, v_new)
         _check("sparrow_append_kv", sparrow_append_kv(
             self.shape, _ptr(k_new), _ptr(v_new), _ptr(self.k_cache), _ptr(self.v_cache),
@@ -959,6 +983,10 @@ class SparseDecodeStep:
 
     def append_score_topk(self, k_new, v_new, stream, seq_lens=None):
         """Append the decoded token (k_new/v_new [B][Hkv][D]) and select pages, fused."""
+        if self.exps is not None:
+            self.append(k_new, v_new, stream, seq_lens)
+            self.score_topk(stream, seq_lens)
+            return
         self._rows(k_new, v_new)
         _check("sparrow_append_score_topk", sparrow_append_score_topk(
             self.shape, _ptr(self.q), _ptr(k_new), _ptr(v_new), _ptr(self.k_cache),
@@ -967,6 +995,13 @@ class SparseDecodeStep:
             self.ws_score.numel(), stream))
 
     def attend(self, stream, seq_lens=None):
+        if self.exps is not None:
+            _check("sparrow_sparse_decode_attn_e4m3", sparrow_sparse_decode_attn_e4m3(
+                self.shape, _ptr(self.q), _ptr(self.k_cache), _ptr(self.v_cache), _ptr(self.exps),
+                _ptr(self.block_table), self._lens(seq_lens), _ptr(self.k), _ptr(self.idx),
+                self.k_max, self.scale, _ptr(self.out), SPARROW_OUT_F32, _ptr(self.ws_attn),
+                self.ws_attn.numel(), stream))
+            return
         _check("sparrow_sparse_decode_attn", sparrow_sparse_decode_attn(
             self.shape, _ptr(self.q), _ptr(self.k_cache), _ptr(self.v_cache),
             _ptr(self.block_table), self._lens(seq_lens), _ptr(self.k), _ptr(self.idx),
@@ -979,6 +1014,12 @@ class SparseDecodeStep:
         same results as append_score_topk (or score_topk) followed by attend."""
         if (k_new is None) != (v_new is None):
             raise ValueError("k_new and v_new are both given or both None")
+        if self.exps is not None:
+            if k_new is not None:
+                self.append(k_new, v_new, stream, seq_lens)
+            self.score_topk(stream, seq_lens)
+            self.attend(stream, seq_lens)
+            return self.out
         if k_new is not None:
             self._rows(k_new, v_new)
         _check("sparrow_decode_step", sparrow_decode_step(
