@@ -138,29 +138,40 @@ __device__ __forceinline__ int64_t first_row(const int32_t *cu, int b, int64_t n
     return c < 0 ? 0 : (c > num_rows ? num_rows : c);
 }
 
-// Page slot `s` of the layout above (every lane of the wave takes part in the search).
+// Page slot `s` of the layout above (every lane of the wave takes part in the search): the last
+// sequence whose first slot is <= s.  64 candidates a round; in the last round a lane loads all that is
+// wanted of its candidate, so that up to 64 sequences cost one trip to memory.
 __device__ __forceinline__ PageRows find_page(const int32_t *cu, const int32_t *seq_lens,
                                               int64_t num_rows, int batch, int ps, int64_t s)
 {
     const int lane = threadIdx.x & 63;
-    auto slot_of = [&](int b) { return first_row(cu, b, num_rows) / ps + 2 * (int64_t)b; };
-    int lo = 0, span = batch;  // the last sequence whose first slot is <= s
-    while (span > 1) {
+    int lo = 0, span = batch;
+    while (span > 64) {
         const int step = (span + 63) >> 6;
-        const bool ok = lane * step < span && slot_of(lo + lane * step) <= s;
-        const int t = __popcll(__ballot(ok)) - 1;
-        lo += max(t, 0) * step;
-        span = min(step, span - max(t, 0) * step);
+        const int b = lo + lane * step;
+        const bool ok = lane * step < span && first_row(cu, b, num_rows) / ps + 2 * (int64_t)b <= s;
+        const int t = max(__popcll(__ballot(ok)) - 1, 0);
+        lo += t * step;
+        span = min(step, span - t * step);
     }
+    int c = 0, next = 0, len = 0;
+    bool ok = false;
+    if (lane < span) {
+        c = (int)first_row(cu, lo + lane, num_rows);
+        next = (int)first_row(cu, lo + lane + 1, num_rows);
+        len = seq_lens[lo + lane];
+        ok = c / ps + 2 * (int64_t)(lo + lane) <= s;
+    }
+    const int t = max(__popcll(__ballot(ok)) - 1, 0);
     PageRows p;
-    p.b = lo;
-    const int64_t c0 = first_row(cu, lo, num_rows);
-    int64_t n = first_row(cu, lo + 1, num_rows) - c0;
+    p.b = lo + t;
+    const int64_t c0 = __builtin_amdgcn_readlane(c, t);
+    int64_t n = __builtin_amdgcn_readlane(next, t) - c0;
     n = n < 0 ? 0 : n;
-    p.L = seq_lens[lo];
+    p.L = __builtin_amdgcn_readlane(len, t);
     const int64_t p0 = p.L - n;  // position of row c0
     const int64_t first = p0 >= 0 ? p0 / ps : -((-p0 + ps - 1) / ps);
-    p.lp = first + (s - (c0 / ps + 2 * (int64_t)lo));
+    p.lp = first + (s - (c0 / ps + 2 * (int64_t)p.b));
     const int64_t at = p.lp * ps;
     p.t0 = (int)(p0 > at ? p0 - at : 0);
     const int64_t end = p.L - at;  // (<= 0 past the sequence's end)
@@ -216,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void k_append_pages_e4m3(
         return;
     const int64_t phys = block_table[(int64_t)p.b * max_pages + p.lp];
     if (phys < 0 || phys >= num_phys)
-        return;
+        return;  // the page is outside the cache: nothing is written
     const bool head = h < num_kv_heads;
     const int64_t ph = phys * num_kv_heads + h;
 
