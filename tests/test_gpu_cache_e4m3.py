@@ -308,3 +308,44 @@ def test_bf16_bits_of_landmarks_keep_their_zero_signs():
                      cu_tokens=torch.tensor([0, 3], dtype=torch.int32, device=DEV))
     m = W.bf16_bits(c.meta[c.bt[0, 0].long()])
     assert (m[0, 0] == 0x8000).all() and (m[0, 1] == 0).all()
+
+
+def test_very_many_sequences():
+    # the search over the row offsets takes three trips; decode rows as well
+    B = 4097
+    g = np.random.default_rng(B)
+    new = g.integers(0, 4, B)
+    past = g.integers(0, 20, B)
+    c = Cache(B, 1, 16, (new + past).tolist())
+    cu = np.concatenate([[0], np.cumsum(new)]).tolist()
+    k, v = c.rows(max(1, cu[-1]))
+    c.append_and_check(k, v, cu)
+    k, v = c.rows(B)
+    c.append_and_check(k, v, None)
+    ko, _ = S.read_kv_e4m3(c.k8, c.v8, c.exps, c.bt, c.lens, None, B)
+    kv, _ = e4m3.both_values(c.k8, c.v8, c.exps)
+    np.testing.assert_array_equal(
+        f64(ko), e4m3.read(kv, list(range(B + 1)), c.bt_host, c.lens_host, B, 0))
+
+
+def test_row_offsets_past_32_bits():
+    # 2.4e9 elements of new rows and of rows read back, from two sequences
+    hkv, ps, n = 8, 128, 300
+    lens = [1200000, 1100003]
+    T = sum(lens)
+    pages = [-(-L // ps) for L in lens]
+    k8, v8, exps = S.new_cache_e4m3(sum(pages), hkv, ps, DEV)
+    meta = S.new_meta(sum(pages), hkv, DEV)
+    bt = torch.full((2, max(pages)), -1, dtype=torch.int32, device=DEV)
+    bt[0, :pages[0]] = torch.arange(pages[0], device=DEV, dtype=torch.int32)
+    bt[1, :pages[1]] = torch.arange(pages[0], sum(pages), device=DEV, dtype=torch.int32)
+    seq_lens = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    cu = torch.tensor([0, lens[0], T], dtype=torch.int32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(32)
+    rows = torch.randn((T, hkv, D), generator=g, device=DEV, dtype=torch.bfloat16)
+    S.append_kv_e4m3(rows, rows, k8, v8, exps, bt, seq_lens, meta, cu_tokens=cu)
+    ko, vo = S.read_kv_e4m3(k8, v8, exps, bt, seq_lens, cu, T)
+    for at in (slice(T - n, T), slice(lens[0] - n, lens[0] + n), slice(0, n)):
+        y, e = e4m3.quantise(f64(rows[at]))
+        np.testing.assert_array_equal(f64(ko[at]), np.ldexp(y, e[..., None]))
+        assert torch.equal(ko[at], vo[at])

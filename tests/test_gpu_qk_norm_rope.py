@@ -272,3 +272,39 @@ def test_side_stream_and_graph_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(outs, want + wg)), rep
+
+
+@pytest.mark.parametrize("T,hq,hk", [(1, 1024, 1024), (5, 1000, 3), (700, 3, 1000)])
+def test_many_heads(T, hq, hk):
+    log(f"case rope many heads T={T} heads={hq},{hk}")
+    _, q, k, w, f, pos, dy = make(T, hq, hk, 30 + T)
+    got = S.qk_norm_rope(q, k, w[0], w[1], f, pos)
+    out = S.qk_norm_rope_bwd(dy[0], dy[1], q, k, w[0], w[1], f, pos)
+    for i, (x, wt) in enumerate(((q, w[0]), (k, w[1]))):
+        check(got[i], *formula(x, wt, f, pos, 1e-6), 2.0 ** -18, "forward")
+        want, size, part, ps = formula_grad(dy[i], x, wt, f, pos, 1e-6)
+        check(out[i], want, size, 2.0 ** -17, "dx")
+        # (at most 700,000 rows over some 2000 waves of 8 rows a pass: 44 additions a lane)
+        assert bool(((wide(out[2 + i]) - part.sum((0, 1))).abs() <= 2.0 ** -16 * ps.sum((0, 1))).all())
+
+
+def test_offsets_past_32_bits():
+    # 2.3e9 elements of q and of its gradient, streamed stores; the last tokens against the formula,
+    # and rows of padding in front of them as they were
+    T, hq, hk, n = 70000, 256, 1, 40
+    f = torch.from_numpy(1e6 ** (-np.arange(0, D, 2) / D)).to(DEV)
+    w = [torch.full((D,), 1.25, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    pos[T - n - 3:T - n] = -1
+    g = torch.Generator(device=DEV).manual_seed(31)
+    q, k, dq_out, dk_out = (torch.randn((T, h, D), generator=g, device=DEV, dtype=torch.bfloat16)
+                            for h in (hq, hk, hq, hk))
+    outs = [torch.full_like(t, 7.0) for t in (q, k)]
+    S.qk_norm_rope(q, k, w[0], w[1], f, pos, q_out=outs[0], k_out=outs[1])
+    grads = S.qk_norm_rope_bwd(dq_out, dk_out, q, k, w[0], w[1], f, pos)
+    for i, (x, dy) in enumerate(((q, dq_out), (k, dk_out))):
+        check(outs[i][-n:], *formula(x[-n:], w[i], f, pos[-n:], 1e-6), 2.0 ** -18, "far rows")
+        check(grads[i][-n:], *formula_grad(dy[-n:], x[-n:], w[i], f, pos[-n:], 1e-6)[:2],
+              2.0 ** -17, "far dx")
+        assert bool((outs[i][T - n - 3:T - n] == 7).all())
+        assert bool((grads[i][T - n - 3:T - n] == 0).all())
