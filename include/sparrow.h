@@ -413,14 +413,16 @@ int sparrow_tail_stats(int64_t num_tokens, const float *alpha, const int32_t *po
  * written to q_out, k_out.  fp32 arithmetic (the angle in fp64), one rounding to bf16.  Rows of a
  * token with a negative position (padding) are left as they were.  inv_freq holds any
  * frequencies, in radians per token, scaled ones included.  The sum of squares is fp32: rows with
- * entries beyond 1e18 overflow it.
+ * entries beyond 1e18 overflow it, and with eps = 0 a row of zeros, or of entries below 1e-19, has no
+ * finite 1 / sqrt.
  *
- * Arguments: num_tokens >= 0; 1 <= num_q_heads, num_k_heads <= 1024; head_dim == 128; q, k (device
- * bf16; head j of token t starts at t * stride + j * 128 elements; the strides are multiples of 8 and
- * at least num_heads * 128, so that both may lie in one fused projection output); q_weight, k_weight
- * (device bf16 [128]); inv_freq (device fp64 [64], 8-byte aligned); positions (device int32
- * [num_tokens]); eps >= 0; q_out, k_out (device bf16 [num_tokens][num_heads][128], written; either
- * may be its input where that is contiguous); stream.
+ * Arguments: 0 <= num_tokens < 2^31; 1 <= num_q_heads, num_k_heads <= 1024; head_dim == 128; q, k
+ * (device bf16, 16-byte aligned; head j of token t starts at t * stride + j * 128 elements; the strides
+ * are multiples of 8 and at least num_heads * 128, so that both may lie in one fused projection
+ * output); q_weight, k_weight (device bf16 [128], 16-byte aligned); inv_freq (device fp64 [64], 8-byte
+ * aligned); positions (device int32 [num_tokens]); eps >= 0; q_out, k_out (device bf16
+ * [num_tokens][num_heads][128], written, 16-byte aligned; either may be its input where that is
+ * contiguous); stream.
  * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED (head_dim), SPARROW_EHIP.
  */
 int sparrow_qk_norm_rope(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
@@ -439,7 +441,8 @@ int sparrow_qk_norm_rope(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_
  * negative position get dx = 0 and add nothing to dw.
  *
  * Arguments: as above; dq_out, dk_out (device bf16 [num_tokens][num_heads][128]); workspace of at
- * least SPARROW_ROPE_WORKSPACE_BYTES (device, scratch of this call); stream.
+ * least SPARROW_ROPE_WORKSPACE_BYTES (device, 16-byte aligned, scratch of this call: calls that may
+ * overlap need one each); stream.
  * Errors: as above, plus SPARROW_EWORKSPACE.
  */
 #define SPARROW_ROPE_WORKSPACE_BYTES 1048576

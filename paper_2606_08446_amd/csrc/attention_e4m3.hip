@@ -58,17 +58,32 @@ __device__ __forceinline__ T load_nt(global_bytes p)
     return __builtin_nontemporal_load((const __attribute__((address_space(1))) T *)p);
 }
 
-// Part p from the 16 cache rows `part` (their number in the cache / 16).
-__device__ __forceinline__ void load_part(Tile &t, int p, const Args8 &x, int part, uint32_t k_lane,
-                                          uint32_t v_lane, uint32_t e_lane)
+// A lane's offsets into a part's exponents, K and V.
+struct LaneOffsets {
+    uint32_t e, k, v;
+    __device__ __forceinline__ LaneOffsets(int lr, int lg)
+        : e(8 * lg), k((lr & 7) * kHeadDim + 16 * (2 * lg + (lr >> 3))),
+          v(4 * lg * kHeadDim + 8 * lr) {}
+};
+
+// K, V and the exponents of part p from the 16 cache rows `part` (their number in the cache / 16).
+__device__ __forceinline__ void load_exps(Tile &t, int p, const Args8 &x, int part, uint32_t e_lane)
 {
-    const int64_t off = (int64_t)part * (16 * kHeadDim);
     const global_bytes ep = scalar_base(x.exps + (int64_t)part * 32);
-    const global_bytes kp = scalar_base(x.k + off);
-    const global_bytes vp = scalar_base(x.v + off);
     t.e[p] = *(const __attribute__((address_space(1))) u32x2_t *)(ep + e_lane);
+}
+
+__device__ __forceinline__ void load_keys(Tile &t, int p, const Args8 &x, int part, uint32_t k_lane)
+{
+    const global_bytes kp = scalar_base(x.k + (int64_t)part * (16 * kHeadDim));
     t.k[p][0] = load_nt<u32x4_t>(kp + k_lane);
     t.k[p][1] = load_nt<u32x4_t>(kp + k_lane + 8 * kHeadDim);
+}
+
+__device__ __forceinline__ void load_values(Tile &t, int p, const Args8 &x, int part,
+                                            uint32_t v_lane)
+{
+    const global_bytes vp = scalar_base(x.v + (int64_t)part * (16 * kHeadDim));
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         t.v[p][j] = load_nt<u32x2_t>(vp + v_lane + j * kHeadDim);
@@ -117,10 +132,12 @@ __device__ __forceinline__ void trade_rows(u32x4_t (&k)[2])
 }
 
 // A tile into the wave's online-softmax state.  v0 and v1 tokens of its parts lie inside the
-// sequence (16 or more: all; 0 or less: none); the others get weight 0 and zero V rows.
+// sequence (16 or more: all; 0 or less: none); the others get weight 0 and zero V rows.  k_done() is
+// called when the tile's K is read, v_done() when its V and exponents are: they may load the next.
+template <typename KDone, typename VDone>
 __device__ __forceinline__ void attend_tile(Tile &t, int v0, int v1, const bf16x8_t (&qf)[4],
                                             float scale_log2, int lg, float &m_run, float &l_run,
-                                            f32x4_t (&O)[8])
+                                            f32x4_t (&O)[8], KDone k_done, VDone v_done)
 {
     float z[kParts][4];
 #pragma unroll
@@ -138,6 +155,7 @@ __device__ __forceinline__ void attend_tile(Tile &t, int v0, int v1, const bf16x
         for (int j = 0; j < 4; ++j)
             z[p][j] = s[j] * (scale_log2 * byte_pow2(t.e[p][0], j));
     }
+    k_done();
     if (min(v0, v1) < 16) {  // cache slots past the length, and parts that are not there, may
                              // hold anything
 #pragma unroll
@@ -182,6 +200,7 @@ __device__ __forceinline__ void attend_tile(Tile &t, int v0, int v1, const bf16x
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             v[p][j] = values(t.v[p][j], byte_pow2(t.e[p][1], j));
+    v_done();
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const u32x4_t av = {pair_of(v[0][0], v[0][1], c), pair_of(v[0][2], v[0][3], c),
@@ -366,10 +385,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
     const int lane = threadIdx.x & 63;
     const int lr = lane & 15;
     const int lg = lane >> 4;
-    // a lane's offsets into a part
-    const uint32_t k_lane = (lr & 7) * kHeadDim + 16 * (2 * lg + (lr >> 3));
-    const uint32_t v_lane = 4 * lg * kHeadDim + 8 * lr;
-    const uint32_t e_lane = 8 * lg;
+    const LaneOffsets at(lr, lg);
     const int log_cpp = __ffs(a.ps) - 5;  // 16-token parts per page: ps / 16
     Walk walk;
     walk.start(a, s_off, (int64_t)w * P / W, (int64_t)(w + 1) * P / W, lane);
@@ -394,8 +410,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
         const int c0 = kParts * ti, c1 = c0 + 1;  // parts of the batch
         const int p0 = (c0 >> log_cpp) & 63, p1 = (c1 >> log_cpp) & 63;  // their pages
         const int u0 = c0 & ((1 << log_cpp) - 1), u1 = c1 & ((1 << log_cpp) - 1);
-        load_part(tile, 0, x, __builtin_amdgcn_readlane(pages.part, p0) + u0, k_lane, v_lane, e_lane);
-        load_part(tile, 1, x, __builtin_amdgcn_readlane(pages.part, p1) + u1, k_lane, v_lane, e_lane);
+        const int part[kParts] = {__builtin_amdgcn_readlane(pages.part, p0) + u0,
+                                  __builtin_amdgcn_readlane(pages.part, p1) + u1};
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            load_exps(tile, p, x, part[p], at.e);
+            load_keys(tile, p, x, part[p], at.k);
+            load_values(tile, p, x, part[p], at.v);
+        }
         s.v0 = __builtin_amdgcn_readlane(pages.tokens, p0) - 16 * u0;
         s.v1 = __builtin_amdgcn_readlane(pages.tokens, p1) - 16 * u1;
         s.unit = now.unit;
@@ -473,7 +495,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
 
     // ---- a tile's turn; true when the range is done
     auto turn = [&](Tile &tile, const Step &s, const Step &after) __attribute__((always_inline)) {
-        attend_tile(tile, s.v0, s.v1, qf, a.scale_log2, lg, m_run, l_run, O);
+        attend_tile(tile, s.v0, s.v1, qf, a.scale_log2, lg, m_run, l_run, O, [] {}, [] {});
         if (s.ends != 0) {
             write_unit(s.unit, from_start, s.ends & kCloses);
             if (s.ends & kLast)
@@ -511,15 +533,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
     }
 }
 
-// Short lists of few units: one workgroup per (sequence, KV head), its waves' states joined in LDS in
-// wave order, so that there are no partials in memory and no second launch.  Every wave knows the
-// whole list, a page per lane, and takes an equal share of its tiles.  Bound by what one CU can fetch,
-// and so by the longest list that the call admits: up to 256 units (a CU each) of 1024 tokens it is
-// the faster one at any lengths.  A call, streaming waves and merge -> this, us, 4 query heads each:
-// 8 units x 256 tokens 16.8 -> 14.0, 128 x 1024 16.8 -> 14.7, 256 x 1024 21.6 -> 18.1; but 8 x 2048
-// 16.8 -> 18.2, 8 x 4096 16.7 -> 29.9 and 512 x 512 21.8 -> 23.1.
-constexpr int kUnitMaxUnits = 256;
-constexpr int kUnitMaxTokens = 1024;    // list bound x page size
+// Short lists: one workgroup per (sequence, KV head), its waves' states joined in LDS in wave order, so
+// that there are no partials in memory and no second launch.  Every wave knows the whole list, a page
+// per lane, and takes an equal share of its tiles.  A call of a few microseconds waits for its code as
+// well as for its data, so the loop body is there once: it has one tile's registers, and the next
+// tile's K is loaded where this one's is read, its V and exponents where they are (1024 tokens, 4 query
+// heads, us in a graph: three tiles' registers in turn 11.9 for 8 units and 14.9 for 128; this 9.8 and
+// 12.2; with 4 waves 11.0 and 14.0).
+//
+// Against the streaming waves and their merge, us in a graph, streaming -> this, 4 query heads:
+//   units x tokens  8 x 256 10.4 -> 5.2, 8 x 1024 10.4 -> 9.8, 128 x 1024 15.8 -> 12.2, 256 x 1024
+//   20.5 -> 14.0, 512 x 1024 31.9 -> 27.3, 768 x 256 20.3 -> 16.7, 768 x 1024 45.9 -> 40.4; lists of
+//   50 to 1024 tokens, 256 units 18.5 -> 12.2, 768 32.8 -> 30.1
+// and past 3 units a CU the other way (1024 x 256 18.4 -> 21.6, x 1024 50.2 -> 53.8).  Longer lists,
+// bound by what one CU can fetch, pay where most CUs have one:
+//   192 x 2048 26.3 -> 21.4, 256 x 2048 32.5 -> 24.8 (ragged 23.9 -> 20.1); but 8 x 1536 10.6 -> 12.6,
+//   128 x 2048 20.9 -> 21.0 (ragged 16.3 -> 17.0), 384 x 2048 42.9 -> 42.5.
+constexpr int kUnitsPerCu = 3;
+constexpr int kUnitMaxTokens = 1024;    // list bound x page size; twice that, see unit_path
 constexpr int kUnitThreads = 512;
 constexpr int kUnitWaves = kUnitThreads / 64;
 constexpr int kUnitMaxGroup = 8;        // query heads per KV head (sizes the LDS)
@@ -537,9 +568,6 @@ __global__ __launch_bounds__(kUnitThreads, 2) void k_attn_unit_e4m3(Args8 x)
     const int lane = threadIdx.x & 63;
     const int lr = lane & 15;
     const int lg = lane >> 4;
-    const uint32_t k_lane = (lr & 7) * kHeadDim + 16 * (2 * lg + (lr >> 3));
-    const uint32_t v_lane = 4 * lg * kHeadDim + 8 * lr;
-    const uint32_t e_lane = 8 * lg;
     const int log_cpp = __ffs(a.ps) - 5;
 
     PageBatch t;
@@ -562,15 +590,21 @@ __global__ __launch_bounds__(kUnitThreads, 2) void k_attn_unit_e4m3(Args8 x)
     const int tiles = ((t.n << log_cpp) + kParts - 1) / kParts;
     const int end = (wv + 1) * tiles / kUnitWaves;
     int ti = wv * tiles / kUnitWaves;
-    auto issue = [&](Tile &tile, int &v0, int &v1) __attribute__((always_inline)) {
-        const int at = min(ti, tiles - 1);  // (behind the share: rows that exist)
-        const int c0 = kParts * max(at, 0), c1 = c0 + 1;
-        const int p0 = (c0 >> log_cpp) & 63, p1 = (c1 >> log_cpp) & 63;
+    // the next tile's place; behind the share all lanes take one word of the last one
+    const LaneOffsets in_part(lr, lg);
+    LaneOffsets at = in_part;
+    int part[kParts], v0, v1;
+    auto place = [&]() __attribute__((always_inline)) {
+        const int c0 = kParts * min(ti, end - 1), c1 = c0 + 1;
+        const int p0 = c0 >> log_cpp, p1 = (c1 >> log_cpp) & 63;
         const int u0 = c0 & ((1 << log_cpp) - 1), u1 = c1 & ((1 << log_cpp) - 1);
-        load_part(tile, 0, x, __builtin_amdgcn_readlane(pages.part, p0) + u0, k_lane, v_lane, e_lane);
-        load_part(tile, 1, x, __builtin_amdgcn_readlane(pages.part, p1) + u1, k_lane, v_lane, e_lane);
+        part[0] = __builtin_amdgcn_readlane(pages.part, p0) + u0;
+        part[1] = __builtin_amdgcn_readlane(pages.part, p1) + u1;
         v0 = __builtin_amdgcn_readlane(pages.tokens, p0) - 16 * u0;
         v1 = __builtin_amdgcn_readlane(pages.tokens, p1) - 16 * u1;
+        at.e = ti < end ? in_part.e : 0;
+        at.k = ti < end ? in_part.k : 0;
+        at.v = ti < end ? in_part.v : 0;
         ++ti;
     };
     float m_run = -INFINITY;
@@ -579,26 +613,31 @@ __global__ __launch_bounds__(kUnitThreads, 2) void k_attn_unit_e4m3(Args8 x)
 #pragma unroll
     for (int c = 0; c < 8; ++c)
         O[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    int left = end - ti;
-    if (left > 0) {
-        Tile t0, t1, t2;
-        int v[3][2];
-        issue(t0, v[0][0], v[0][1]);
-        issue(t1, v[1][0], v[1][1]);
-        for (;;) {
-            issue(t2, v[2][0], v[2][1]);
-            attend_tile(t0, v[0][0], v[0][1], qf, a.scale_log2, lg, m_run, l_run, O);
-            if (--left == 0)
-                break;
-            issue(t0, v[0][0], v[0][1]);
-            attend_tile(t1, v[1][0], v[1][1], qf, a.scale_log2, lg, m_run, l_run, O);
-            if (--left == 0)
-                break;
-            issue(t1, v[1][0], v[1][1]);
-            attend_tile(t2, v[2][0], v[2][1], qf, a.scale_log2, lg, m_run, l_run, O);
-            if (--left == 0)
-                break;
-        }
+    if (ti < end) {
+        Tile t;
+        auto load_k = [&]() __attribute__((always_inline)) {
+            load_keys(t, 0, x, part[0], at.k);
+            load_keys(t, 1, x, part[1], at.k);
+        };
+        auto load_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                load_exps(t, p, x, part[p], at.e);
+                load_values(t, p, x, part[p], at.v);
+            }
+        };
+        place();
+        load_k();
+        load_v();
+#pragma unroll 1
+        do {
+            attend_tile(t, v0, v1, qf, a.scale_log2, lg, m_run, l_run, O,
+                        [&]() __attribute__((always_inline)) {
+                            place();
+                            load_k();
+                        },
+                        load_v);
+        } while (ti <= end);
     }
 
     // ---- the waves' states into LDS (lane (g, r) holds head g, channels 32r .. 32r+31)
@@ -642,9 +681,11 @@ __global__ __launch_bounds__(kUnitThreads, 2) void k_attn_unit_e4m3(Args8 x)
 // Whether a call takes one workgroup per unit; list_bound: k_max, or the block table's width.
 bool unit_path(const sparrow_shape_t &s, int64_t list_bound)
 {
-    return (int64_t)s.batch * s.num_kv_heads <= kUnitMaxUnits &&
-           s.num_q_heads / s.num_kv_heads <= kUnitMaxGroup && list_bound <= kBatch &&
-           list_bound * s.page_size <= kUnitMaxTokens;
+    const int64_t units = (int64_t)s.batch * s.num_kv_heads, cus = device_cus();
+    const int64_t tokens = list_bound * s.page_size;
+    return s.num_q_heads / s.num_kv_heads <= kUnitMaxGroup && list_bound <= kBatch &&
+           ((tokens <= kUnitMaxTokens && units <= kUnitsPerCu * cus) ||
+            (tokens <= 2 * kUnitMaxTokens && units > cus / 2 && units <= cus));
 }
 
 }  // namespace

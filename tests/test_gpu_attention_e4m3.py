@@ -405,3 +405,19 @@ def test_calls_at_once_on_two_streams():
     torch.cuda.synchronize()
     for outs, w in zip(got, want):
         assert all(torch.equal(o, x) for pair in outs for o, x in zip(pair, w))
+
+
+# both sides of the sizes up to which a (sequence, KV head) is one workgroup's (256 CUs)
+@pytest.mark.parametrize("B,hkv,ps,k_max", [(96, 8, 16, 64), (97, 8, 16, 5), (32, 8, 32, 64), (33, 8, 32, 64),
+                                            (16, 8, 64, 32), (17, 8, 128, 16), (3, 8, 64, 17)])
+def test_sparse_sizes_around_the_split(B, hkv, ps, k_max):
+    log(f"case e4m3 split B={B} ps={ps} k_max={k_max}")
+    g = np.random.default_rng(B + ps)
+    lens = g.integers(1, 2 * ps * k_max // 3 + 2, B)
+    lens[:3] = [0, 1, ps * k_max + 5]
+    c = Case(B, lens[:B].tolist(), 2 * hkv, hkv, ps)
+    c.poison()
+    counts = g.integers(0, k_max + 1, B).tolist()
+    counts[B - 1] = k_max + 3
+    idx = c.lists([min(n, k_max) for n in counts], k_max)
+    c.check(sparse(c, counts, idx), c.formula(idx, counts), "split")
