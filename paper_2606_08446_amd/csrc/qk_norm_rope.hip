@@ -14,7 +14,7 @@
 // turn at any int32 position; sine and cosine of a turn are one instruction each (off by at most
 // 2^-22.9 over 2^24 turns against fp64, sincospi by 2^-24.2: both far below the bf16 step).
 // Bound by HBM: 512 B per row for ~10 flops an element, 768 B for ~30 in the gradient.  64K tokens of
-// 32 + 8 heads (1.39 GB) take 225-237 us, 5.9-6.2 TB/s; the gradient of 32K tokens (1.01 GB) 171 us, 5.9
+// 32 + 8 heads (1.39 GB) take 230 us, 6.0 TB/s; the gradient of 32K tokens (1.01 GB) 171 us, 5.9
 // (a plain copy reaches 4.8 TB/s, a sum of two arrays 6.0).
 #include "qk_norm_rope.h"
 
@@ -125,12 +125,17 @@ __device__ __forceinline__ float inv_rms(const float (&x0)[8], const float (&x1)
     return rsqrtf(sum8(ss) * (1.f / kHeadDim) + eps);
 }
 
-// The workgroup's place among `n` (a multiple of 8), counted so that each of the 8 XCDs, which take
-// workgroups in turn, works on one contiguous eighth of the rows (64K tokens of 32 + 8 heads: 233 ->
-// 225 us).
-__device__ __forceinline__ int64_t place_by_xcd(int block, int n)
+// The workgroup's place among `n`, counted so that each of the 8 XCDs, which take workgroups in turn,
+// works on 128 neighbours out of every 1024.  (64K tokens of 32 + 8 heads 234 -> 230 us, 128K of
+// 16 + 8 277 -> 270, 32K of 40 + 8 133.5 -> 133.2; with 512 neighbours, or an eighth of all, 237, 279 and
+// 140.)
+constexpr int kXcds = 8, kXcdRun = 128;
+
+__device__ __forceinline__ int place_by_xcd(int block, int n)
 {
-    return (int64_t)(block % 8) * (n / 8) + block / 8;
+    constexpr int kWindow = kXcds * kXcdRun;
+    const int first = block / kWindow * kWindow, r = block - first;
+    return first + kWindow > n ? block : first + r % kXcds * kXcdRun + r / kXcds;
 }
 
 // A wave takes one pass (8 query rows, or 8 key rows) of one token at a time.
@@ -144,7 +149,7 @@ __global__ __launch_bounds__(kRopeThreads) void k_qk_norm_rope(RopeArgs a, uint1
     const int passes = q_passes + (a.num_k_heads + kRows - 1) / kRows;
     const double inv_freq = a.inv_freq[8 * l + (lane >> 3)];
     const int64_t all = a.tokens * passes;
-    for (int64_t w = place_by_xcd(blockIdx.x, gridDim.x) * kRopeWaves +
+    for (int64_t w = (int64_t)place_by_xcd(blockIdx.x, gridDim.x) * kRopeWaves +
                      __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
          w < all; w += (int64_t)gridDim.x * kRopeWaves) {
         const int64_t t = w / passes;
@@ -395,7 +400,7 @@ hipError_t launch_qk_norm_rope(const RopeArgs &a, uint16_t *q_out, uint16_t *k_o
 {
     const int64_t passes = (a.num_q_heads + kRows - 1) / kRows + (a.num_k_heads + kRows - 1) / kRows;
     int64_t blocks = (a.tokens * passes + kRopeWaves - 1) / kRopeWaves;
-    blocks = blocks < kRopeBlocks ? (blocks + 7) / 8 * 8 : kRopeBlocks;
+    blocks = blocks < kRopeBlocks ? blocks : kRopeBlocks;
     auto kernel = stream_rows(a) ? k_qk_norm_rope<true> : k_qk_norm_rope<false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, a, q_out,
                        k_out);
