@@ -700,7 +700,8 @@ def _expect_rope(q, k, q_weight, k_weight, inv_freq, positions):
 def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=None, k_out=None):
     """RMS norm of every head of q ``[T][Hq][128]`` and k ``[T][Hk][128]`` (bf16, views of a fused
     projection welcome) with its weight, and the rotation by ``positions * inv_freq``.  Returns
-    (q_out, k_out), contiguous bf16; rows of tokens with a negative position are not written."""
+    (q_out, k_out), contiguous bf16; rows of tokens with a negative position are not written.  No
+    autograd node: ``qk_norm_rope_bwd`` is its gradient."""
     import torch
     T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
     dev = q.device
