@@ -358,6 +358,16 @@ def _given(t, name, dtype, shape, device):
     return t
 
 
+def _given_like(t, name, like):
+    """The caller's output ``t`` after its check, or a new one of ``like``'s type, shape and device
+    (0.4 us less than from those)."""
+    import torch
+    if t is None:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+    _expect(t, name, like.dtype, tuple(like.shape), like.device)
+    return t
+
+
 def _given_workspace(t, nbytes, device):
     """The caller's workspace (its size is the library's check), or a new one of ``nbytes``."""
     if t is None:
@@ -702,11 +712,10 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=
     projection welcome) with its weight, and the rotation by ``positions * inv_freq``.  Returns
     (q_out, k_out), contiguous bf16; rows of tokens with a negative position are not written.  No
     autograd node: ``qk_norm_rope_bwd`` is its gradient."""
-    import torch
     T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
     dev = q.device
-    q_out = _given(q_out, "q_out", torch.bfloat16, (T, Hq, D), dev)
-    k_out = _given(k_out, "k_out", torch.bfloat16, (T, Hk, D), dev)
+    q_out = _given_like(q_out, "q_out", q)
+    k_out = _given_like(k_out, "k_out", k)
     if T == 0:
         return q_out, k_out
     _launch("sparrow_qk_norm_rope", dev, T, Hq, Hk, D, q.data_ptr(), qs, k.data_ptr(), ks,
@@ -726,10 +735,10 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positio
     _expect(dk_out, "dk_out", torch.bfloat16, (T, Hk, D), dev)
     dqs = Hq * D if dq is None else _expect_rows(dq, "dq", (T, Hq, D), dev)
     dks = Hk * D if dk is None else _expect_rows(dk, "dk", (T, Hk, D), dev)
-    dq = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=dev) if dq is None else dq
-    dk = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=dev) if dk is None else dk
+    dq = torch.empty_like(dq_out) if dq is None else dq
+    dk = torch.empty_like(dk_out) if dk is None else dk
     dq_weight = _given(dq_weight, "dq_weight", torch.float32, (D,), dev)
-    dk_weight = _given(dk_weight, "dk_weight", torch.float32, (D,), dev)
+    dk_weight = _given_like(dk_weight, "dk_weight", dq_weight)
     if T == 0:
         return dq, dk, dq_weight.zero_(), dk_weight.zero_()
     workspace = _given_workspace(workspace, SPARROW_ROPE_WORKSPACE_BYTES, dev)
@@ -805,7 +814,7 @@ def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_t
     if cu_tokens is not None:
         _expect(cu_tokens, "cu_tokens", torch.int32, (B + 1,), dev)
     k_out = _given(k_out, "k_out", torch.bfloat16, (T, Hkv, D), dev)
-    v_out = _given(v_out, "v_out", torch.bfloat16, (T, Hkv, D), dev)
+    v_out = _given_like(v_out, "v_out", k_out)
     if B == 0 or T == 0:
         return k_out, v_out
     shape = make_shape(B, Hkv, Hkv, ps, M, P, D)
