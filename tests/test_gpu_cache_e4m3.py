@@ -183,7 +183,7 @@ def test_row_offsets_outside_the_rows_stay_inside():
 
 @pytest.mark.parametrize("B", [1, 65, 300])
 def test_many_short_prompts(B):
-    # the search over the row offsets takes one, two and three rounds
+    # the search over the row offsets takes one and two trips
     g = np.random.default_rng(B)
     new = g.integers(0, 9, B)
     past = g.integers(0, 40, B)
