@@ -511,8 +511,7 @@ int sparrow_read_kv_e4m3(const sparrow_shape_t *shape, const void *k_cache, cons
  * sparrow_dense_decode_attn with K and V as the cache's values,
  *     z_t = scale * 2^(kbyte_t - 127) * (q[b][j] . kcode_t),  w = softmax(z),
  *     out[b][j] = sum_t w_t 2^(vbyte_t - 127) vcode_t
- * with fp32 sums; the softmax numerators enter the product with V as two bf16 numbers each (17
- * bits).  Page lists, lengths, absent pages and empty sequences are those calls'; so is the
+ * with fp32 sums and fp32 softmax numerators (all of their 24 bits enter the product with V).  Page lists, lengths, absent pages and empty sequences are those calls'; so is the
  * workspace (SPARROW_OP_SPARSE_ATTN, SPARROW_OP_DENSE_ATTN).  The order of the sums depends only on the
  * shape, k_max, the page lists and the device.
  *
