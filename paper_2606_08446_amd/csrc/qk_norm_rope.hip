@@ -10,9 +10,8 @@
 // 8 lanes own a row: lane l holds channels 8l .. 8l+7 and 64+8l .. 64+8l+7, both halves of its 8
 // rotated pairs, in two 16-byte vectors, so a wave takes 8 rows (heads of one token) per pass and
 // the row sums are three DPP steps.  A token's 64 angles are computed once per wave, one per
-// lane, in fp64: p * inv_freq / 2pi less its nearest integer keeps full fp32 precision of the
-// turn at any int32 position; sine and cosine of a turn are one instruction each (off by at most
-// 2^-22.9 over 2^24 turns against fp64, sincospi by 2^-24.2: both far below the bf16 step).
+// lane: p * inv_freq / 2pi is reduced in fp64, which keeps full fp32 precision of the angle at any int32
+// position, and its sine and cosine are as exact (the weights' gradients are fp32 outputs).
 // Bound by HBM: 512 B per row for ~10 flops an element, 768 B for ~30 in the gradient.  64K tokens of
 // 32 + 8 heads (1.39 GB) take 230 us, 6.0 TB/s; the gradient of 32K tokens (1.01 GB) 171 us, 5.9
 // (a plain copy reaches 4.8 TB/s, a sum of two arrays 6.0).
@@ -101,13 +100,30 @@ struct Row {
     }
 };
 
+// Sine and cosine of a turn: its whole quarters turn the result, and what is left, at most pi / 4
+// either way, goes to fp32 in one rounding and through the Taylor series (their next terms are below
+// 2^-29).  Off by at most 2^-23.4 (2^-23.8 measured; an instruction each on the fp32 turn over 2^-23.1).
+__device__ __forceinline__ void sincos_turn(double turns, float &sine, float &cosine)
+{
+    constexpr double kHalfPi = 1.57079632679489661923;
+    const double quarters = 4. * (turns - __builtin_rint(turns)), n = __builtin_rint(quarters);
+    const float x = (float)((quarters - n) * kHalfPi), x2 = x * x;
+    const float s = x + x * x2 * (-1.f / 6 + x2 * (1.f / 120 + x2 * (-1.f / 5040 + x2 * (1.f / 362880))));
+    const float c = 1.f + x2 * (-1.f / 2 + x2 * (1.f / 24 + x2 * (-1.f / 720 + x2 * (1.f / 40320 + x2 *
+                                                                                  (-1.f / 3628800)))));
+    const int k = (int)n;  // -2 .. 2
+    sine = k & 1 ? c : s;
+    cosine = k & 1 ? s : c;
+    sine = k & 2 ? -sine : sine;
+    cosine = (k + 1) & 2 ? -cosine : cosine;
+}
+
 // Cosines and sines of a token's angles 8l .. 8l+7: lane 8j + l computes number 8l + j.
 __device__ __forceinline__ void angles(double inv_freq, int pos, int lane, float (&c)[8],
                                        float (&s)[8])
 {
-    const double turns = (double)pos * (inv_freq * kInvTwoPi);
-    const float t = (float)(turns - __builtin_rint(turns));
-    const float cv = __builtin_amdgcn_cosf(t), sv = __builtin_amdgcn_sinf(t);
+    float cv, sv;
+    sincos_turn((double)pos * (inv_freq * kInvTwoPi), sv, cv);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         c[j] = __shfl(cv, 8 * j + (lane & 7), 64);
