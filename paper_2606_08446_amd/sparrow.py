@@ -711,7 +711,13 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=
     """RMS norm of every head of q ``[T][Hq][128]`` and k ``[T][Hk][128]`` (bf16, views of a fused
     projection welcome) with its weight, and the rotation by ``positions * inv_freq``.  Returns
     (q_out, k_out), contiguous bf16; rows of tokens with a negative position are not written.  No
-    autograd node: ``qk_norm_rope_bwd`` is its gradient."""
+    autograd node: ``qk_norm_rope_bwd`` is its gradient, and inputs that a gradient is recorded for
+    are refused."""
+    import torch
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight.requires_grad or
+                                    k_weight.requires_grad):
+        raise ValueError("qk_norm_rope records no gradient: call it under torch.no_grad() or on "
+                         "detached tensors, and qk_norm_rope_bwd for the gradient")
     T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
     dev = q.device
     q_out = _given_like(q_out, "q_out", q)
