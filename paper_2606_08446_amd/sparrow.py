@@ -710,7 +710,8 @@ def _expect_rope(q, k, q_weight, k_weight, inv_freq, positions):
 def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=None, k_out=None):
     """RMS norm of every head of q ``[T][Hq][128]`` and k ``[T][Hk][128]`` (bf16, views of a fused
     projection welcome) with its weight, and the rotation by ``positions * inv_freq``.  Returns
-    (q_out, k_out), contiguous bf16; rows of tokens with a negative position are not written.  No
+    (q_out, k_out), contiguous bf16; rows of tokens with a negative position (padding) are not written:
+    they keep what a given output holds, and are undefined, possibly NaN, in a new one.  No
     autograd node: ``qk_norm_rope_bwd`` is its gradient, and inputs that a gradient is recorded for
     are refused."""
     import torch
@@ -811,7 +812,9 @@ def append_kv_e4m3(k_new, v_new, k_cache, v_cache, exps, block_table, seq_lens, 
 def read_kv_e4m3(k_cache, v_cache, exps, block_table, seq_lens, cu_tokens, num_tokens, k_out=None,
                  v_out=None):
     """The last cu_tokens[b+1] - cu_tokens[b] tokens of every sequence from an e4m3 cache: (k_out,
-    v_out) bf16 [num_tokens][Hkv][128], exactly the values that the cache holds."""
+    v_out) bf16 [num_tokens][Hkv][128], exactly the values that the cache holds.  Rows behind
+    cu_tokens[batch] are not written: they keep what a given output holds, and are undefined in a new
+    one."""
     import torch
     _require_device(k_cache)
     dev = k_cache.device
