@@ -12,6 +12,7 @@ visible, the tensor-level calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Sequence
@@ -903,6 +904,20 @@ def stream_read(buf, checksum=None):
     return checksum
 
 
+def _on_its_device(method):
+    """``method`` with ``self.q``'s device as the current one: a device's default stream has the handle
+    0, which stands for the current device's."""
+    @functools.wraps(method)
+    def call(self, *args, **kw):
+        import torch
+        device = self.q.device
+        if device.index == torch.cuda.current_device():
+            return method(self, *args, **kw)
+        with torch.cuda.device(device):
+            return method(self, *args, **kw)
+    return call
+
+
 class SparseDecodeStep:
     """One layer's sparse decode step with preallocated buffers.
 
@@ -967,6 +982,7 @@ class SparseDecodeStep:
         _expect(k_new, "k_new", torch.bfloat16, want, self.q.device)
         _expect(v_new, "v_new", torch.bfloat16, want, self.q.device)
 
+    @_on_its_device
     def meta_update(self, first_pos, stream, seq_lens=None):
         import torch
         if self.exps is not None:
@@ -978,6 +994,7 @@ class SparseDecodeStep:
             self.shape, _ptr(self.k_cache), _ptr(self.block_table), self._lens(seq_lens),
             _ptr(first_pos), _ptr(self.meta), stream))
 
+    @_on_its_device
     def append(self, k_new, v_new, stream, seq_lens=None):
         """Write the decoded token's K/V rows and update its page's metadata."""
         if self.exps is not None:
@@ -994,12 +1011,14 @@ class SparseDecodeStep:
             self.shape, _ptr(k_new), _ptr(v_new), _ptr(self.k_cache), _ptr(self.v_cache),
             _ptr(self.block_table), self._lens(seq_lens), _ptr(self.meta), stream))
 
+    @_on_its_device
     def score_topk(self, stream, seq_lens=None):
         _check("sparrow_page_score_topk", sparrow_page_score_topk(
             self.shape, _ptr(self.q), _ptr(self.meta), _ptr(self.block_table),
             self._lens(seq_lens), self.sched, self.k_max, _ptr(self.k), _ptr(self.idx),
             _ptr(self.ws_score), self.ws_score.numel(), stream))
 
+    @_on_its_device
     def append_score_topk(self, k_new, v_new, stream, seq_lens=None):
         """Append the decoded token (k_new/v_new [B][Hkv][D]) and select pages, fused."""
         if self.exps is not None:
@@ -1013,6 +1032,7 @@ class SparseDecodeStep:
             self.sched, self.k_max, _ptr(self.k), _ptr(self.idx), _ptr(self.ws_score),
             self.ws_score.numel(), stream))
 
+    @_on_its_device
     def attend(self, stream, seq_lens=None):
         if self.exps is not None:
             _check("sparrow_sparse_decode_attn_e4m3", sparrow_sparse_decode_attn_e4m3(
@@ -1027,6 +1047,7 @@ class SparseDecodeStep:
             self.k_max, self.scale, _ptr(self.out), SPARROW_OUT_F32, _ptr(self.ws_attn),
             self.ws_attn.numel(), stream))
 
+    @_on_its_device
     def decode_step(self, k_new, v_new, stream, seq_lens=None):
         """The whole step in one call (sparrow_decode_step): append the decoded token
         (k_new/v_new [B][Hkv][D], or both None for no append), select pages, attend; the
@@ -1048,6 +1069,7 @@ class SparseDecodeStep:
             SPARROW_OUT_F32, _ptr(self.ws_step), self.ws_step.numel(), stream))
         return self.out
 
+    @_on_its_device
     def run(self, first_pos=None, stream=None):
         stream = _stream(self.q.device) if stream is None else stream
         if first_pos is not None:
