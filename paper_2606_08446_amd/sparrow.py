@@ -1020,7 +1020,8 @@ class SparseDecodeStep:
 
     @_on_its_device
     def append_score_topk(self, k_new, v_new, stream, seq_lens=None):
-        """Append the decoded token (k_new/v_new [B][Hkv][D]) and select pages, fused."""
+        """Append the decoded token (k_new/v_new [B][Hkv][D]) and select pages: one fused call, over an
+        e4m3 cache the append and the selection one after the other."""
         if self.exps is not None:
             self.append(k_new, v_new, stream, seq_lens)
             self.score_topk(stream, seq_lens)
@@ -1049,9 +1050,10 @@ class SparseDecodeStep:
 
     @_on_its_device
     def decode_step(self, k_new, v_new, stream, seq_lens=None):
-        """The whole step in one call (sparrow_decode_step): append the decoded token
-        (k_new/v_new [B][Hkv][D], or both None for no append), select pages, attend; the
-        same results as append_score_topk (or score_topk) followed by attend."""
+        """The whole step in one call (sparrow_decode_step; over an e4m3 cache its three calls one after
+        the other): append the decoded token (k_new/v_new [B][Hkv][D], or both None for no
+        append), select pages, attend; the same results as append_score_topk (or score_topk)
+        followed by attend."""
         if (k_new is None) != (v_new is None):
             raise ValueError("k_new and v_new are both given or both None")
         if self.exps is not None:
