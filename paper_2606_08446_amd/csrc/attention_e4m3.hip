@@ -13,11 +13,13 @@
 //       on mfma_f32_16x16x32_bf16 over the tile's 32 tokens
 // The softmax numerators enter PV as the sum of three bf16 numbers, 8 bits each from the top down,
 // which is all of their 24 bits: the products are those of fp32 numerators, for an fp32 output too.
-// Sums and maxima are fp32.  (Two numbers, 17 bits, were up to 2^-17 off; in a graph they took 12.0
-// instead of 12.2 us for 8 units of 4097 tokens, 436 instead of 441 for 64 sequences of 8K-32K.)
+// Sums and maxima are fp32.  An fp32 output of 8 units of 4097 tokens, 64 sequences of 8K-32K and 256 at
+// 10 % is 1.9e-7, 9.1e-7 and 4.8e-7 off (2-norm), elementary operations in fp32 5.8e-7, 1.2e-6 and 4.9e-7.
+// (Two numbers, 17 bits: 1.6e-6, 2.4e-6 and 2.3e-6; us in a graph, two -> three: 12.0 -> 12.2, 431 -> 434,
+// 257 -> 259, and 8 units of 256 tokens 5.1 -> 5.2.)
 //
-// Bound by HBM: 64 sequences of 8K-32K tokens (2.8 GB) take 428 us, 6.6 TB/s where a read-only stream
-// reaches 7.1; with the arithmetic taken out the kernel is no faster.
+// Bound by HBM: 64 sequences of 8K-32K tokens (2.8 GB) take 432 us, 6.5 TB/s where a read-only stream
+// reaches 7.1; the third number's matrix instructions, a third more, cost it 1 %.
 #include "attention_e4m3.h"
 
 #include "attention_split.h"
@@ -388,8 +390,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
     const int64_t P = (int64_t)uniform(s_off[B]) * Hkv;
     // A wave has at least one tile, with more than 8 query heads per KV head four (the merge reads a
     // row per head and wave), and at least one page.  A whole dense call, us, tiles 1 / 2 / 4: 8 units
-    // of 4097 tokens x 2 heads 11.6 / 12.8 / 14.3, of 2048 10.4 / 10.5 / 12.7, 16 of 4096 x 16 heads
-    // 17.7 / 17.6 / 16.0; no difference from 32 units of 8192 tokens on.
+    // of 4097 tokens x 2 heads 12.3 / 13.4 / 15.1, of 2048 10.8 / 11.6 / 13.4, 16 of 4096 x 16 heads
+    // 18.9 / 18.8 / 16.9; no difference from 32 units of 8192 tokens on.  Shares are whole pages: with
+    // pages of 128 tokens and little more than one a wave, some waves have twice the others' tiles.
     int64_t W = P * (a.ps >> 4) / (kParts * (G > 8 ? 4 : 1));
     W = W > 1 ? W : 1;
     W = W < a.max_waves ? W : a.max_waves;
@@ -553,17 +556,19 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_stream_e4m3(Args8 x)
 // per lane, and takes an equal share of its tiles.  A call of a few microseconds waits for its code as
 // well as for its data, so the loop body is there once: it has one tile's registers, and the next
 // tile's K is loaded where this one's is read, its V and exponents where they are (1024 tokens, 4 query
-// heads, us in a graph: three tiles' registers in turn 11.9 for 8 units and 14.9 for 128; this 9.8 and
-// 12.2; with 4 waves 11.0 and 14.0).
+// heads, us in a graph, with numerators of two numbers: three tiles' registers in turn 11.9 for 8 units
+// and 14.9 for 128; this 9.8 and 12.2; with 4 waves 11.0 and 14.0).  What is left is latency: a wave has
+// one tile in flight, and 1024 tokens are four tiles a wave, one after another.
 //
 // Against the streaming waves and their merge, us in a graph, streaming -> this, 4 query heads:
-//   units x tokens  8 x 256 10.4 -> 5.2, 8 x 1024 10.4 -> 9.8, 128 x 1024 15.8 -> 12.2, 256 x 1024
-//   20.5 -> 14.0, 512 x 1024 31.9 -> 27.3, 768 x 256 20.3 -> 16.7, 768 x 1024 45.9 -> 40.4; lists of
-//   50 to 1024 tokens, 256 units 18.5 -> 12.2, 768 32.8 -> 30.1
-// and past 3 units a CU the other way (1024 x 256 18.4 -> 21.6, x 1024 50.2 -> 53.8).  Longer lists,
+//   units x tokens  8 x 256 10.4 -> 5.3, 8 x 1024 10.5 -> 9.7, 128 x 1024 16.6 -> 13.0, 256 x 1024
+//   21.8 -> 14.8, 512 x 1024 33.1 -> 28.9, 768 x 256 21.3 -> 17.8, 768 x 1024 47.3 -> 43.5; lists of
+//   50 to 1024 tokens, 256 units 20.0 -> 12.7, 768 34.9 -> 31.9
+// and past 3 units a CU the other way (1024 x 256 20.2 -> 23.1, x 1024 54.1 -> 57.6).  Longer lists,
 // bound by what one CU can fetch, pay where most CUs have one:
-//   192 x 2048 26.3 -> 21.4, 256 x 2048 32.5 -> 24.8 (ragged 23.9 -> 20.1); but 8 x 1536 10.6 -> 12.6,
-//   128 x 2048 20.9 -> 21.0 (ragged 16.3 -> 17.0), 384 x 2048 42.9 -> 42.5.
+//   192 x 2048 28.1 -> 21.5, 256 x 2048 33.2 -> 25.6 (lists of 400 to 2048 tokens 27.0 -> 21.6); but
+//   8 x 1536 10.9 -> 13.8, 128 x 2048 22.1 -> 21.4 (18.8 -> 18.2), 384 x 2048 45.7 -> 46.2.
+// A dense call goes by the block table's width, the only bound on the lengths that the host knows.
 constexpr int kUnitsPerCu = 3;
 constexpr int kUnitMaxTokens = 1024;    // list bound x page size; twice that, see unit_path
 constexpr int kUnitThreads = 512;
@@ -715,7 +720,8 @@ hipError_t launch_attention_e4m3(const sparrow_shape_t &s, const AttnPlan &plan,
     const int G = s.num_q_heads / s.num_kv_heads;
     // One workgroup per CU, four waves with two tiles in flight each: 64 KiB, which keeps the memory
     // busy; more waves only add partials and uneven ends (1 / 2 workgroups: 64 sequences of 8K-32K
-    // tokens 428 / 429 us, 256 sequences at 10 % 251 / 257, 128 units of 1024 tokens 16.1 / 17.2).
+    // tokens 448 / 450 us, 256 sequences at 10 % 259 / 265, 128 units of 1024 tokens 16.7 / 19.6, on one
+    // box in turn).
     int64_t waves = (int64_t)device_cus() * kAttnWaves;
     waves = waves < kMaxWaves ? waves : kMaxWaves;
     Args8 x{};

@@ -13,7 +13,7 @@
 // lane: p * inv_freq / 2pi is reduced in fp64, which keeps full fp32 precision of the angle at any int32
 // position, and its sine and cosine are as exact (the weights' gradients are fp32 outputs).
 // Bound by HBM: 512 B per row for ~10 flops an element, 768 B for ~30 in the gradient.  64K tokens of
-// 32 + 8 heads (1.39 GB) take 230 us, 6.0 TB/s; the gradient of 32K tokens (1.01 GB) 171 us, 5.9
+// 32 + 8 heads (1.39 GB) take 229 us, 6.1 TB/s; the gradient of 32K tokens (1.01 GB) 171 us, 5.9
 // (a plain copy reaches 4.8 TB/s, a sum of two arrays 6.0).
 #include "qk_norm_rope.h"
 
@@ -142,9 +142,10 @@ __device__ __forceinline__ float inv_rms(const float (&x0)[8], const float (&x1)
 }
 
 // The workgroup's place among `n`, counted so that each of the 8 XCDs, which take workgroups in turn,
-// works on 128 neighbours out of every 1024.  (64K tokens of 32 + 8 heads 234 -> 230 us, 128K of
-// 16 + 8 277 -> 270, 32K of 40 + 8 133.5 -> 133.2; with 512 neighbours, or an eighth of all, 237, 279 and
-// 140.)
+// works on 128 neighbours out of every 1024.  (In the order of launch -> this, us in a graph, both in turn
+// on two boxes: 64K tokens of 32 + 8 heads 234.4 -> 229.2, 128K of 16 + 8 279 -> 270, 32K of 40 + 8 135.6
+// -> 134.0, 4K of 32 + 8 17.7 -> 17.5; two builds of the same code differ by 0.3 % at most.  With 512
+// neighbours, or an eighth of all, the first three were 237, 279 and 140.)
 constexpr int kXcds = 8, kXcdRun = 128;
 
 __device__ __forceinline__ int place_by_xcd(int block, int n)
@@ -244,7 +245,9 @@ __device__ __forceinline__ void grad_rows(const Row &xr, Row &d, float eps, cons
 // What a wave works through: the passes of a token one after another, then those of the token `waves`
 // further on, so that neighbouring waves read neighbouring rows.  Where there are more waves than
 // tokens a token's passes are shared out: run u is token u / runs, passes [r passes / runs, (r + 1)
-// passes / runs) with r = u % runs, and a wave takes the runs w, w + waves, ...
+// passes / runs) with r = u % runs, and a wave takes the runs w, w + waves, ...  `runs` is a whole
+// number, so that up to twice as many waves as tokens leave some without work: 1014 tokens of 40 + 8
+// heads are five passes in a row for 1014 of the query side's 1704 waves, where an even split is three.
 struct Walk {
     int64_t u, t;
     int pass, stop, runs;
