@@ -98,6 +98,9 @@ extern "C" {
 #define SPARROW_LOGITS_F32 0
 #define SPARROW_LOGITS_BF16 1
 
+#define SPARROW_STREAM_F32 0
+#define SPARROW_STREAM_BF16 1
+
 #define SPARROW_OP_SCORE_TOPK 0
 #define SPARROW_OP_SPARSE_ATTN 1
 #define SPARROW_OP_DENSE_ATTN 2
@@ -453,6 +456,64 @@ int sparrow_qk_norm_rope_bwd(int64_t num_tokens, int32_t num_q_heads, int32_t nu
                              const int32_t *positions, float eps, void *dq, int64_t dq_stride,
                              void *dk, int64_t dk_stride, float *dq_weight, float *dk_weight,
                              void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * The residual stream after a block and the norm before the next one, in one pass: what stands between
+ * two blocks of a layer, for models with a norm on one side of a block or on both, a gate and a
+ * residual scale.
+ *
+ * For every token t < num_tokens, with rows of `channels` values:
+ *     n = x r_x post_weight,  r_x = 1 / sqrt(mean(x^2) + eps)      (post_weight NULL: n = x)
+ *     h' = h + scale * sigmoid(gate) * n                           (gate NULL: h + scale * n)
+ *     y = h' r weight,  r = 1 / sqrt(mean(h'^2) + eps)
+ * h' goes to h_out in the stream's type and y to y, each rounded once from fp32 (y comes from h' as
+ * it is before that rounding).  With x == NULL there is no block yet: y = h r weight, and gate,
+ * post_weight and h_out are NULL too.  The sums of squares are fp32: entries beyond 1e18 overflow
+ * them, and with eps = 0 a row of zeros, or of entries below 1e-19, has no finite 1 / sqrt.
+ *
+ * Arguments: 0 <= num_tokens < 2^31; channels a multiple of 8, at most 16384; stream_dtype
+ * (SPARROW_STREAM_*: the type of h and h_out); h (device [num_tokens][channels]); x, gate (device
+ * bf16, rows of x_stride and gate_stride elements, multiples of 8 and at least channels, so that
+ * both may lie in one projection's output); weight, post_weight (device bf16 [channels]); scale
+ * finite; eps >= 0; h_out (device, like h, written; may be h); y (device bf16
+ * [num_tokens][channels], written); all 16-byte aligned; stream.
+ * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED (channels, stream_dtype), SPARROW_EHIP.
+ */
+int sparrow_residual_norm(int64_t num_tokens, int32_t channels, int32_t stream_dtype, const void *h,
+                          const void *x, int64_t x_stride, const void *gate, int64_t gate_stride,
+                          const void *weight, const void *post_weight, float scale, float eps,
+                          void *h_out, void *y, void *stream);
+
+/*
+ * Gradient of sparrow_residual_norm, from the stream behind the block (h_out, as it was written).
+ * With dy the gradient of y, dh_out that of h_out from everything behind (NULL: zero), u = dy weight,
+ * k = h_out r, s = sigmoid(gate):
+ *     dh = dh_out + r (u - k mean(u k)),              dweight = sum over the tokens of dy k
+ *     d = scale dh,  e = d s,  dgate = d n s (1 - s)  (without a gate e = d)
+ *     dx = r_x (v - k_x mean(v k_x)),  v = e post_weight,  k_x = x r_x,  dpost_weight = sum of e k_x
+ *     (without post_weight dx = e)
+ * fp32 arithmetic; dh is rounded to the stream's type, dx and dgate to bf16; dweight and dpost_weight
+ * are fp32 [channels], overwritten, summed in an order that depends on the sizes alone.
+ *
+ * Arguments: as above; dy (device bf16 [num_tokens][channels]); dh_out (like h_out, or NULL); x may
+ * be NULL where neither gate nor post_weight is given; dh (like h_out, written; may be dh_out); dx,
+ * dgate (device bf16 rows of dx_stride and dgate_stride elements, written; dx NULL: there is no
+ * block; dgate NULL exactly where gate is); dweight; dpost_weight (NULL exactly where post_weight is);
+ * workspace of at least sparrow_residual_norm_workspace_size(num_tokens, channels) bytes (device,
+ * 16-byte aligned, scratch of this call: calls that may overlap need one each); stream.  With
+ * num_tokens == 0 nothing is written.
+ * Errors: as above, plus SPARROW_EWORKSPACE.
+ */
+int sparrow_residual_norm_bwd(int64_t num_tokens, int32_t channels, int32_t stream_dtype,
+                              const void *dy, const void *dh_out, const void *h_out, const void *x,
+                              int64_t x_stride, const void *gate, int64_t gate_stride,
+                              const void *weight, const void *post_weight, float scale, float eps,
+                              void *dh, void *dx, int64_t dx_stride, void *dgate,
+                              int64_t dgate_stride, float *dweight, float *dpost_weight,
+                              void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of sparrow_residual_norm_bwd; 0 for sizes that it refuses (and for no tokens). */
+size_t sparrow_residual_norm_workspace_size(int64_t num_tokens, int32_t channels);
 
 /*
  * The e4m3 cache: K and V in 8 bits, half the bytes that a decode step streams.

@@ -6,6 +6,7 @@
 #include "cache_e4m3.h"
 #include "common.h"
 #include "qk_norm_rope.h"
+#include "residual_norm.h"
 
 using namespace sparrow;
 
@@ -82,6 +83,44 @@ int rope_args(int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads, int3
                  inv_freq,                                positions,
                  num_tokens,                              num_q_heads,
                  num_k_heads,                             eps};
+    return SPARROW_OK;
+}
+
+// Rows of `channels` bf16 values at any stride of whole 16-byte vectors.
+bool rows_ok(const void *p, int64_t stride, int channels)
+{
+    return p && al16(p) && stride % 8 == 0 && stride >= channels;
+}
+
+// Shared by sparrow_residual_norm and its gradient (h: the stream that it reads); fills `a` where the
+// arguments are fine.
+int norm_args(int64_t num_tokens, int32_t channels, int32_t stream_dtype, const void *h,
+              const void *x, int64_t x_stride, const void *gate, int64_t gate_stride,
+              const void *weight, const void *post_weight, float scale, float eps, NormArgs &a)
+{
+    if (num_tokens < 0 || num_tokens > 0x7fffffff || channels < 8)
+        return SPARROW_EINVAL;
+    if (channels % 8 || channels > kNormMaxChannels ||
+        (stream_dtype != SPARROW_STREAM_F32 && stream_dtype != SPARROW_STREAM_BF16))
+        return SPARROW_EUNSUPPORTED;
+    if (!h || !weight || !al16(h) || !al16(weight) || !al16(post_weight))
+        return SPARROW_EINVAL;
+    if ((x && !rows_ok(x, x_stride, channels)) || (gate && !rows_ok(gate, gate_stride, channels)))
+        return SPARROW_EINVAL;
+    if (!std::isfinite(scale) || !(eps >= 0.f) || !std::isfinite(eps))
+        return SPARROW_EINVAL;
+    a = NormArgs{h,
+                 static_cast<const uint16_t *>(x),
+                 static_cast<const uint16_t *>(gate),
+                 x_stride,
+                 gate_stride,
+                 static_cast<const uint16_t *>(weight),
+                 static_cast<const uint16_t *>(post_weight),
+                 num_tokens,
+                 channels,
+                 stream_dtype == SPARROW_STREAM_F32,
+                 scale,
+                 eps};
     return SPARROW_OK;
 }
 
@@ -501,6 +540,75 @@ int sparrow_qk_norm_rope_bwd(int64_t num_tokens, int32_t num_q_heads, int32_t nu
                          dk_weight,
                          static_cast<float *>(workspace)};
     return status_of(launch_qk_norm_rope_bwd(a, g, static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_residual_norm(int64_t num_tokens, int32_t channels, int32_t stream_dtype, const void *h,
+                          const void *x, int64_t x_stride, const void *gate, int64_t gate_stride,
+                          const void *weight, const void *post_weight, float scale, float eps,
+                          void *h_out, void *y, void *stream)
+{
+    NormArgs a;
+    const int rc = norm_args(num_tokens, channels, stream_dtype, h, x, x_stride, gate, gate_stride,
+                             weight, post_weight, scale, eps, a);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!y || !al16(y) || !al16(h_out) || (x != nullptr) != (h_out != nullptr) ||
+        (!x && (gate || post_weight)))
+        return SPARROW_EINVAL;
+    if (num_tokens == 0)
+        return SPARROW_OK;
+    return status_of(launch_residual_norm(a, h_out, static_cast<uint16_t *>(y),
+                                          static_cast<hipStream_t>(stream)));
+}
+
+size_t sparrow_residual_norm_workspace_size(int64_t num_tokens, int32_t channels)
+{
+    if (num_tokens < 0 || num_tokens > 0x7fffffff || channels < 8 || channels % 8 ||
+        channels > kNormMaxChannels)
+        return 0;
+    return norm_grad_workspace(num_tokens, channels);
+}
+
+int sparrow_residual_norm_bwd(int64_t num_tokens, int32_t channels, int32_t stream_dtype,
+                              const void *dy, const void *dh_out, const void *h_out, const void *x,
+                              int64_t x_stride, const void *gate, int64_t gate_stride,
+                              const void *weight, const void *post_weight, float scale, float eps,
+                              void *dh, void *dx, int64_t dx_stride, void *dgate,
+                              int64_t dgate_stride, float *dweight, float *dpost_weight,
+                              void *workspace, size_t ws_bytes, void *stream)
+{
+    NormArgs a;
+    const int rc = norm_args(num_tokens, channels, stream_dtype, h_out, x, x_stride, gate,
+                             gate_stride, weight, post_weight, scale, eps, a);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!dy || !dh || !dweight || !al16(dy) || !al16(dh_out) || !al16(dh) || !al4(dweight) ||
+        !al4(dpost_weight) || !al16(workspace))
+        return SPARROW_EINVAL;
+    if ((dx && !rows_ok(dx, dx_stride, channels)) ||
+        (dgate && !rows_ok(dgate, dgate_stride, channels)))
+        return SPARROW_EINVAL;
+    if ((gate != nullptr) != (dgate != nullptr) ||
+        (post_weight != nullptr) != (dpost_weight != nullptr) ||
+        ((gate || post_weight) && (!x || !dx)))
+        return SPARROW_EINVAL;
+    if (num_tokens == 0)
+        return SPARROW_OK;
+    if (!workspace || ws_bytes < norm_grad_workspace(num_tokens, channels))
+        return SPARROW_EWORKSPACE;
+    if (!gate && !post_weight)
+        a.x = nullptr;  // dx is then a multiple of dh
+    const NormGradArgs g{static_cast<const uint16_t *>(dy),
+                         dh_out,
+                         dh,
+                         static_cast<uint16_t *>(dx),
+                         static_cast<uint16_t *>(dgate),
+                         dx_stride,
+                         dgate_stride,
+                         dweight,
+                         dpost_weight,
+                         static_cast<float *>(workspace)};
+    return status_of(launch_residual_norm_bwd(a, g, static_cast<hipStream_t>(stream)));
 }
 
 int sparrow_append_kv_e4m3(const sparrow_shape_t *shape, const void *k_new, int64_t k_stride,

@@ -36,6 +36,8 @@ SPARROW_LANDMARK_MINMAX = 0
 SPARROW_LANDMARK_MEAN = 1
 SPARROW_LOGITS_F32 = 0
 SPARROW_LOGITS_BF16 = 1
+SPARROW_STREAM_F32 = 0
+SPARROW_STREAM_BF16 = 1
 SPARROW_OP_SCORE_TOPK = 0
 SPARROW_OP_SPARSE_ATTN = 1
 SPARROW_OP_DENSE_ATTN = 2
@@ -49,7 +51,8 @@ EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_
            "sparrow_stream_read", "sparrow_sparse_decode_attn_noalloc", "sparrow_decode_step",
            "sparrow_qk_norm_rope", "sparrow_qk_norm_rope_bwd", "sparrow_append_kv_e4m3",
            "sparrow_read_kv_e4m3", "sparrow_sparse_decode_attn_e4m3",
-           "sparrow_dense_decode_attn_e4m3",
+           "sparrow_dense_decode_attn_e4m3", "sparrow_residual_norm", "sparrow_residual_norm_bwd",
+           "sparrow_residual_norm_workspace_size",
            "sparrow_budget_bound", "sparrow_workspace_size", "sparrow_status_string")
 
 
@@ -125,8 +128,18 @@ def load():
                                                     ctypes.c_size_t, _p]
     lib.sparrow_dense_decode_attn_e4m3.argtypes = [sp, _p, _p, _p, _p, _p, _p, ctypes.c_float, _p,
                                                    _i32, _p, ctypes.c_size_t, _p]
+    lib.sparrow_residual_norm.argtypes = [ctypes.c_int64, _i32, _i32, _p, _p, ctypes.c_int64, _p,
+                                          ctypes.c_int64, _p, _p, ctypes.c_float, ctypes.c_float,
+                                          _p, _p, _p]
+    lib.sparrow_residual_norm_bwd.argtypes = [ctypes.c_int64, _i32, _i32, _p, _p, _p, _p,
+                                              ctypes.c_int64, _p, ctypes.c_int64, _p, _p,
+                                              ctypes.c_float, ctypes.c_float, _p, _p,
+                                              ctypes.c_int64, _p, ctypes.c_int64, _p, _p, _p,
+                                              ctypes.c_size_t, _p]
     for fn in EXPORTS[:-3]:
         getattr(lib, fn).restype = ctypes.c_int
+    lib.sparrow_residual_norm_workspace_size.argtypes = [ctypes.c_int64, _i32]
+    lib.sparrow_residual_norm_workspace_size.restype = ctypes.c_size_t
     lib.sparrow_budget_bound.argtypes = [_p, ctypes.c_int64, _i32, _i32, _i32, _p, _p, _i32, _p]
     lib.sparrow_budget_bound.restype = ctypes.c_int32
     lib.sparrow_workspace_size.argtypes = [sp, _i32, _i32]
@@ -225,6 +238,27 @@ def sparrow_qk_norm_rope_bwd(num_tokens, num_q_heads, num_k_heads, head_dim, dq_
                                            dk_out, q, q_stride, k, k_stride, q_weight, k_weight,
                                            inv_freq, positions, eps, dq, dq_stride, dk, dk_stride,
                                            dq_weight, dk_weight, workspace, ws_bytes, stream)
+
+
+def sparrow_residual_norm(num_tokens, channels, stream_dtype, h, x, x_stride, gate, gate_stride,
+                          weight, post_weight, scale, eps, h_out, y, stream):
+    return load().sparrow_residual_norm(num_tokens, channels, stream_dtype, h, x, x_stride, gate,
+                                        gate_stride, weight, post_weight, scale, eps, h_out, y,
+                                        stream)
+
+
+def sparrow_residual_norm_bwd(num_tokens, channels, stream_dtype, dy, dh_out, h_out, x, x_stride,
+                              gate, gate_stride, weight, post_weight, scale, eps, dh, dx, dx_stride,
+                              dgate, dgate_stride, dweight, dpost_weight, workspace, ws_bytes,
+                              stream):
+    return load().sparrow_residual_norm_bwd(num_tokens, channels, stream_dtype, dy, dh_out, h_out, x,
+                                            x_stride, gate, gate_stride, weight, post_weight, scale,
+                                            eps, dh, dx, dx_stride, dgate, dgate_stride, dweight,
+                                            dpost_weight, workspace, ws_bytes, stream)
+
+
+def sparrow_residual_norm_workspace_size(num_tokens, channels) -> int:
+    return int(load().sparrow_residual_norm_workspace_size(num_tokens, channels))
 
 
 def sparrow_append_kv_e4m3(shape, k_new, k_stride, v_new, v_stride, cu_tokens, num_tokens, k_cache,
@@ -756,6 +790,120 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, positio
             dk.data_ptr(), dks, dq_weight.data_ptr(), dk_weight.data_ptr(), workspace.data_ptr(),
             workspace.nbytes)
     return dq, dk, dq_weight, dk_weight
+
+
+def _expect_matrix(t, name, shape, device):
+    """Raise unless ``t`` is bf16 ``[T][C]`` on ``device`` with contiguous channels; returns its row
+    stride in elements (a view into a fused projection's output has a larger one)."""
+    import torch
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != device or not t.is_cuda:
+        _require_device(t)
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected {torch.bfloat16} {shape}")
+    row, one = t.stride()
+    if shape[0] <= 1:  # (a size of one has any stride)
+        row = shape[1]
+    if one != 1 or row < shape[1] or row % 8:
+        raise ValueError(f"{name}: strides {t.stride()}, expected contiguous channels and a row "
+                         f"stride that is a multiple of 8 and at least {shape[1]}")
+    return row
+
+
+def _expect_norm(h, x, weight, post_weight, gate):
+    """(tokens, channels, the stream's type, row strides of x and gate) of checked arguments."""
+    import torch
+    _require_device(h)
+    if h.dim() != 2:
+        raise ValueError("h must be [T][C]")
+    if h.dtype is not torch.bfloat16 and h.dtype is not torch.float32:
+        raise ValueError(f"h: dtype {h.dtype}, expected {torch.bfloat16} or {torch.float32}")
+    dev = h.device
+    T, C = h.shape
+    if not h.is_contiguous():
+        raise ValueError("h must be contiguous")
+    _expect(weight, "weight", torch.bfloat16, (C,), dev)
+    xs = C if x is None else _expect_matrix(x, "x", (T, C), dev)
+    gs = C if gate is None else _expect_matrix(gate, "gate", (T, C), dev)
+    if post_weight is not None:
+        _expect(post_weight, "post_weight", torch.bfloat16, (C,), dev)
+    return T, C, SPARROW_STREAM_F32 if h.dtype is torch.float32 else SPARROW_STREAM_BF16, xs, gs
+
+
+def residual_norm(h, x, weight, post_weight=None, gate=None, scale=1.0, eps=1e-6, h_out=None,
+                  y=None):
+    """The residual stream behind a block and the norm before the next one:
+    ``h' = h + scale * sigmoid(gate) * norm(x) * post_weight`` and ``y = norm(h') * weight``, with h
+    ``[T][C]`` (bf16 or fp32), x and gate ``[T][C]`` bf16 (views of a fused projection welcome).
+    Without post_weight x is not normed, without gate not gated, and without x (a model's first norm)
+    h' is h itself.  Returns (h', y); h_out may be h.  No autograd node: ``residual_norm_bwd`` is its
+    gradient, and inputs that a gradient is recorded for are refused."""
+    import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
+                                       for t in (h, x, weight, post_weight, gate)):
+        raise ValueError("residual_norm records no gradient: call it under torch.no_grad() or on "
+                         "detached tensors, and residual_norm_bwd for the gradient")
+    T, C, dt, xs, gs = _expect_norm(h, x, weight, post_weight, gate)
+    dev = h.device
+    if x is None:
+        if gate is not None or post_weight is not None or h_out is not None:
+            raise ValueError("gate, post_weight and h_out go with x")
+    else:
+        h_out = _given_like(h_out, "h_out", h)
+    y = _given(y, "y", torch.bfloat16, (T, C), dev)
+    if T > 0:
+        _launch("sparrow_residual_norm", dev, T, C, dt, h.data_ptr(), _ptr(x), xs, _ptr(gate), gs,
+                weight.data_ptr(), _ptr(post_weight), float(scale), float(eps), _ptr(h_out),
+                y.data_ptr())
+    return (h if x is None else h_out), y
+
+
+def residual_norm_bwd(dy, dh_out, h_out, x, weight, post_weight=None, gate=None, scale=1.0, eps=1e-6,
+                      dh=None, dx=None, dgate=None, dweight=None, dpost_weight=None, block=True,
+                      workspace=None):
+    """Gradient of ``residual_norm`` from the stream behind the block (its h_out): (dh, dx, dgate,
+    dweight, dpost_weight), dh in the stream's type, dx and dgate bf16 (they may be views into one
+    buffer), the weights' fp32 ``[C]``; None for what the call has no input of.  dh_out None is zero.
+    ``block=False`` says that there was no x: dx is None.  x may be None where it is not needed, with
+    neither post_weight nor gate.  dh may be dh_out."""
+    import torch
+    T, C, dt, xs, gs = _expect_norm(h_out, x, weight, post_weight, gate)
+    dev = h_out.device
+    if (post_weight is not None or gate is not None) and (x is None or not block):
+        raise ValueError("gate and post_weight go with x")
+    _expect(dy, "dy", torch.bfloat16, (T, C), dev)
+    if dh_out is not None:
+        _expect(dh_out, "dh_out", h_out.dtype, (T, C), dev)
+    if (not block and dx is not None) or (gate is None and dgate is not None) or \
+            (post_weight is None and dpost_weight is not None):
+        raise ValueError("a gradient is given for an input that the call does not have")
+    dxs = dgs = C
+    dh = _given_like(dh, "dh", h_out)
+    if dx is not None:
+        dxs = _expect_matrix(dx, "dx", (T, C), dev)
+    elif block:
+        dx = torch.empty_like(dy)
+    if dgate is not None:
+        dgs = _expect_matrix(dgate, "dgate", (T, C), dev)
+    elif gate is not None:
+        dgate = torch.empty_like(dy)
+    dweight = _given(dweight, "dweight", torch.float32, (C,), dev)
+    if post_weight is not None:
+        dpost_weight = _given_like(dpost_weight, "dpost_weight", dweight)
+    if T == 0:
+        dweight.zero_()
+        if dpost_weight is not None:
+            dpost_weight.zero_()
+        return dh, dx, dgate, dweight, dpost_weight
+    if workspace is None:
+        workspace = _workspace(sparrow_residual_norm_workspace_size(T, C), dev)
+    else:
+        workspace = _given_workspace(workspace, None, dev)
+    _launch("sparrow_residual_norm_bwd", dev, T, C, dt, dy.data_ptr(), _ptr(dh_out),
+            h_out.data_ptr(), _ptr(x), xs, _ptr(gate), gs, weight.data_ptr(), _ptr(post_weight),
+            float(scale), float(eps), dh.data_ptr(), _ptr(dx), dxs, _ptr(dgate), dgs,
+            dweight.data_ptr(), _ptr(dpost_weight), workspace.data_ptr(), workspace.nbytes)
+    return dh, dx, dgate, dweight, dpost_weight
 
 
 def new_cache_e4m3(num_phys_pages, num_kv_heads, page_size, device):
