@@ -382,6 +382,42 @@ int sparrow_acceptance_rate_topk(int64_t num_tokens, int32_t k, const float *lp_
                                  const float *lp_draft, float *alpha, void *stream);
 
 /*
+ * The next token of every row of logits, drawn with a given random number.
+ *
+ * For every row t < num_rows, z = logits[t][:], T = temperature[t], m = max z, x_i = (z_i - m) / T,
+ * w_i = exp(x_i), tokens ordered by z descending, equal ones by index ascending (-0 equals +0):
+ *     top-k   (1 <= top_k[t] < vocab)  keeps the first top_k[t] tokens of that order;
+ *     top-p   (top_p[t] < 1)   keeps of these each one whose predecessors' w add up to less than
+ *                              top_p[t] times the sum of w over all of these, the first one always;
+ *     min-p   (min_p[t] > 0)   keeps of these those with w_i >= min(min_p[t], 1).
+ *     tokens[t]   = the first kept token, by index, at which the running sum of the kept w exceeds
+ *                   uniform[t] times their whole sum
+ *     logprobs[t] = log of its w over that sum: the log-probability that it was drawn with
+ * Other values of top_k, top_p and min_p leave a filter off, as NULL arrays do; temperature NULL is 1.
+ * T <= 0 (or NaN) takes the largest logit, the lowest index of equal ones, with logprobs[t] = 0; so do
+ * top_k[t] == 1 and top_p[t] <= 0.  uniform[t] is clamped to [0, 1 - 2^-24].  -inf and NaN logits are
+ * masked tokens, never drawn; +inf counts as the largest finite number.  A row with no other gets
+ * tokens[t] = -1 and logprobs[t] = -inf.  Weights and their sums are held to 1e-13 of the sum, so that
+ * the token is the definition's unless a border lies closer; results do not depend on the launch.
+ *
+ * Arguments: 0 <= num_rows < 2^31; 1 <= vocab <= SPARROW_SAMPLE_MAX_VOCAB; logits_dtype
+ * (SPARROW_LOGITS_*); logits (device, element-aligned, rows of row_stride >= vocab elements: any
+ * stride); temperature, top_p, min_p (device fp32 [num_rows] or NULL), top_k (device int32 [num_rows]
+ * or NULL); uniform (device fp32 [num_rows]); tokens (device int32 [num_rows], written); logprobs
+ * (device fp32 [num_rows], written, or NULL); workspace of at least sparrow_sample_workspace_size
+ * bytes (device, 16-byte aligned, scratch of this call: calls that may overlap need one each); stream.
+ * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED (vocab, dtype), SPARROW_EWORKSPACE, SPARROW_EHIP.
+ */
+#define SPARROW_SAMPLE_MAX_VOCAB 524288
+int sparrow_sample(int64_t num_rows, int32_t vocab, int32_t logits_dtype, const void *logits,
+                   int64_t row_stride, const float *temperature, const int32_t *top_k,
+                   const float *top_p, const float *min_p, const float *uniform, int32_t *tokens,
+                   float *logprobs, void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of sparrow_sample; 0 for sizes that it refuses (and for no rows). */
+size_t sparrow_sample_workspace_size(int64_t num_rows, int32_t vocab, int32_t logits_dtype);
+
+/*
  * Lower-tail statistic of the acceptance rate per length bin (Sec. 3.1 Method:
  * the 5-percentile of the per-token rate; Sec. 3.2: tokens grouped by position
  * in 2K-token bins).

@@ -7,6 +7,7 @@
 #include "common.h"
 #include "qk_norm_rope.h"
 #include "residual_norm.h"
+#include "sample.h"
 
 using namespace sparrow;
 
@@ -466,6 +467,39 @@ int sparrow_acceptance_rate_topk(int64_t num_tokens, int32_t k, const float *lp_
         return SPARROW_OK;
     return status_of(launch_acceptance_topk(num_tokens, k, lp_target, lp_draft, alpha,
                                             static_cast<hipStream_t>(stream)));
+}
+
+int sparrow_sample(int64_t num_rows, int32_t vocab, int32_t logits_dtype, const void *logits,
+                   int64_t row_stride, const float *temperature, const int32_t *top_k,
+                   const float *top_p, const float *min_p, const float *uniform, int32_t *tokens,
+                   float *logprobs, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (num_rows < 0 || num_rows > 0x7fffffff || vocab < 1 || row_stride < vocab)
+        return SPARROW_EINVAL;
+    if (vocab > kSampleMaxVocab ||
+        (logits_dtype != SPARROW_LOGITS_F32 && logits_dtype != SPARROW_LOGITS_BF16))
+        return SPARROW_EUNSUPPORTED;
+    const bool bf16 = logits_dtype == SPARROW_LOGITS_BF16;
+    if (!logits || !uniform || !tokens ||
+        (reinterpret_cast<uintptr_t>(logits) % (bf16 ? 2 : 4)) != 0 || !al4(temperature) ||
+        !al4(top_k) || !al4(top_p) || !al4(min_p) || !al4(uniform) || !al4(tokens) ||
+        !al4(logprobs) || !al16(workspace))
+        return SPARROW_EINVAL;
+    if (num_rows == 0)
+        return SPARROW_OK;
+    if (!workspace || ws_bytes < sample_workspace(num_rows, vocab, bf16))
+        return SPARROW_EWORKSPACE;
+    const SampleArgs a{logits, row_stride, num_rows, vocab,   bf16,   temperature,
+                       top_k,  top_p,      min_p,    uniform, tokens, logprobs};
+    return status_of(launch_sample(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t sparrow_sample_workspace_size(int64_t num_rows, int32_t vocab, int32_t logits_dtype)
+{
+    if (num_rows < 0 || num_rows > 0x7fffffff || vocab < 1 || vocab > kSampleMaxVocab ||
+        (logits_dtype != SPARROW_LOGITS_F32 && logits_dtype != SPARROW_LOGITS_BF16))
+        return 0;
+    return sample_workspace(num_rows, vocab, logits_dtype == SPARROW_LOGITS_BF16);
 }
 
 int sparrow_tail_stats(int64_t num_tokens, const float *alpha, const int32_t *positions,

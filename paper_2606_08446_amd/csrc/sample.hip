@@ -1,0 +1,973 @@
+// The next token of every row of logits: temperature, top-k, top-p, min-p and one given uniform number.
+//
+// With x_i = (z_i - max z) / T and w_i = e^x_i, tokens in the order (z descending, index ascending):
+//   top-k keeps the first k; top-p of those each one whose predecessors' w add up to less than p times
+//   the sum over top-k's; min-p those with w >= q; and the token is the first kept one, by index,
+//   whose running sum of w exceeds u times the sum over the kept.
+// The outcome is a whole number, so what decides it is held far finer than the logits: weights and
+// sums in fp64 (an exponential of 18 operations, off by 1e-14), histograms in 64-bit fixed point, in
+// orders that depend on the sizes alone.
+//
+// k_sample_stats reads the rows once: the maximum of every 64 vectors, and where it may be asked for
+// the sum of the weights of every 256, relative to their own maximum.  k_sample_pick, one workgroup per
+// row, finds from them which of those blocks can hold a kept token and reads only these: the k-th
+// largest block maximum bounds top-k's last logit from below, (1 - p) / vocab of the whole sum
+// top-p's last weight.  Up to kSampleSort tokens above the bound are sorted in LDS; more are narrowed down
+// by digits of their keys.  Without a filter one span's 256 vectors are all it reads.
+#include "common.h"
+#include "sample.h"
+#include "wave.h"
+
+#include <cfloat>
+
+namespace sparrow {
+namespace {
+
+constexpr int kStatThreads = 256;
+constexpr int kStatWaves = kStatThreads / 64;
+constexpr int kBlockVecs = 64;  // a wave's load
+constexpr int kSpanBlocks = 4;
+constexpr int kSpanVecs = kBlockVecs * kSpanBlocks;
+constexpr int kPickThreads = 1024;
+constexpr int kPickWaves = kPickThreads / 64;
+constexpr int kSampleSort = 2048;
+constexpr int kDigitBits = 11;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kMaxSpans = (kSampleMaxVocab / 4 + 1 + kSpanVecs - 1) / kSpanVecs;
+constexpr int kMaxBlocks = kMaxSpans * kSpanBlocks;
+constexpr int kSampleGrid = 1 << 20;  // workgroups at most
+static_assert(kMaxSpans <= kPickThreads, "a thread holds one span");
+static_assert(kSampleSort == 2 * kPickThreads && kDigits == 2 * kPickThreads, "two per thread");
+constexpr double kLog2e = 1.44269504088896340736;
+
+template <bool kBf16> constexpr int kElems = kBf16 ? 8 : 4;  // of a 16-byte vector
+
+// A row as 16-byte vectors from the boundary at or before its start; elements outside are masked.
+template <bool kBf16>
+struct Row {
+    const char *base;  // of vector 0
+    int off;           // its elements before the row
+    int vocab;
+
+    __device__ __forceinline__ Row(const SampleArgs &a, int64_t row)
+    {
+        constexpr int kSize = kBf16 ? 2 : 4;
+        const char *p = static_cast<const char *>(a.logits) + row * a.row_stride * kSize;
+        const int mis = (int)(reinterpret_cast<uintptr_t>(p) & 15u);
+        base = p - mis;
+        off = mis / kSize;
+        vocab = a.vocab;
+    }
+    __device__ __forceinline__ int vecs() const
+    {
+        return (vocab + off + kElems<kBf16> - 1) / kElems<kBf16>;
+    }
+    __device__ __forceinline__ int index(int v, int e) const { return v * kElems<kBf16> + e - off; }
+    // vector v, nothing past the row's ends being read (-inf there)
+    __device__ __forceinline__ u32x4_t load(int v) const
+    {
+        const int i = index(v, 0);
+        if (i >= 0 && i + kElems<kBf16> <= vocab)
+            return ld16(base + (int64_t)v * 16);
+        constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;
+        u32x4_t x = {kNone, kNone, kNone, kNone};
+#pragma unroll
+        for (int e = 0; e < kElems<kBf16>; ++e)
+            if (i + e >= 0 && i + e < vocab) {
+                if (kBf16) {
+                    const uint32_t b = *reinterpret_cast<const uint16_t *>(base + (int64_t)v * 16 + 2 * e);
+                    x[e >> 1] = e & 1 ? (x[e >> 1] & 0xffffu) | b << 16 : (x[e >> 1] & 0xffff0000u) | b;
+                } else {
+                    x[e & 3] = *reinterpret_cast<const uint32_t *>(base + (int64_t)v * 16 + 4 * e);
+                }
+            }
+        return x;
+    }
+    // its logits: NaN counts as masked, +inf as the largest number, -0 as 0
+    __device__ static __forceinline__ void unpack(u32x4_t v, float (&z)[kElems<kBf16>])
+    {
+#pragma unroll
+        for (int e = 0; e < kElems<kBf16>; ++e) {
+            float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
+                            : __uint_as_float(v[e & 3]);
+            f = f != f ? -INFINITY : f;
+            z[e] = fminf(f, FLT_MAX) + 0.f;
+        }
+    }
+};
+
+// 2^t for t <= 0 (NaN: 0): the nearest whole power and the Taylor series of what is left, at most 1/2
+// either way (the next term is 6e-15).
+__device__ __forceinline__ double exp2_64(double t)
+{
+    constexpr double kLn2 = 0.69314718055994530942;
+    constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4,
+                     c5 = c4 * kLn2 / 5, c6 = c5 * kLn2 / 6, c7 = c6 * kLn2 / 7, c8 = c7 * kLn2 / 8,
+                     c9 = c8 * kLn2 / 9, c10 = c9 * kLn2 / 10, c11 = c10 * kLn2 / 11;
+    t = fmax(t, -2000.);
+    const double n = __builtin_rint(t), f = t - n;
+    double p = fma(c11, f, c10);
+    p = fma(p, f, c9);
+    p = fma(p, f, c8);
+    p = fma(p, f, c7);
+    p = fma(p, f, c6);
+    p = fma(p, f, c5);
+    p = fma(p, f, c4);
+    p = fma(p, f, c3);
+    p = fma(p, f, c2);
+    p = fma(p, f, c1);
+    p = fma(p, f, 1.);
+    return __builtin_ldexp(p, (int)n);
+}
+
+// w of a logit relative to the maximum m, with c = log2(e) / T.
+__device__ __forceinline__ double weight_of(float z, double m, double c)
+{
+    return exp2_64(((double)z - m) * c);
+}
+
+__device__ __forceinline__ uint32_t key_of(float z)
+{
+    const uint32_t b = __float_as_uint(z);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+
+__device__ __forceinline__ float logit_of(uint32_t key)
+{
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+__device__ __forceinline__ double shfl_up_64(double x, int d)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __shfl_up((uint32_t)b, d, 64), hi = __shfl_up((uint32_t)(b >> 32), d, 64);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+__device__ __forceinline__ double shfl_64(double x, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __shfl((uint32_t)b, lane, 64), hi = __shfl((uint32_t)(b >> 32), lane, 64);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+__device__ __forceinline__ double wave_scan_64(double x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double y = shfl_up_64(x, d);
+        if (lane >= d)
+            x += y;
+    }
+    return x;
+}
+
+__device__ __forceinline__ double wave_sum_64(double x) { return shfl_64(wave_scan_64(x), 63); }
+
+// A row's settings; off is k = 0, p = 1, q = 0.
+struct Filters {
+    double c;  // log2(e) / T
+    double t;
+    int k;
+    float p, q;
+    bool greedy;
+
+    __device__ __forceinline__ Filters(const SampleArgs &a, int64_t row)
+    {
+        const float temp = a.temperature ? a.temperature[row] : 1.f;
+        t = temp;
+        c = kLog2e / t;
+        k = a.top_k ? a.top_k[row] : 0;
+        k = k > 0 && k < a.vocab ? k : 0;
+        p = a.top_p ? a.top_p[row] : 1.f;
+        p = p < 1.f ? p : 1.f;  // (NaN: off)
+        q = a.min_p ? a.min_p[row] : 0.f;
+        q = q > 0.f ? fminf(q, 1.f) : 0.f;
+        greedy = !(temp > 0.f) || k == 1 || !(p > 0.f);
+    }
+    __device__ __forceinline__ bool sums() const { return !greedy && k == 0; }
+};
+
+struct Stats {
+    double *sums;  // [rows][spans] weights of a span relative to its maximum
+    float *maxima; // [rows][spans][kSpanBlocks]
+    int spans;     // of a row, at most
+};
+
+template <bool kBf16>
+__global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Stats st)
+{
+    constexpr int kE = kElems<kBf16>;
+    const int lane = threadIdx.x & 63;
+    const int64_t all = a.rows * st.spans;
+    for (int64_t w = (int64_t)blockIdx.x * kStatWaves +
+                     __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+         w < all; w += (int64_t)gridDim.x * kStatWaves) {
+        const int64_t row = w / st.spans;
+        const int span = (int)(w - row * st.spans);
+        const Row<kBf16> r(a, row);
+        const int vecs = r.vecs();
+        u32x4_t v[kSpanBlocks];
+#pragma unroll
+        for (int b = 0; b < kSpanBlocks; ++b)
+            v[b] = r.load(min(span * kSpanVecs + b * kBlockVecs + lane, vecs));  // (vecs: nothing)
+        const Filters f(a, row);
+        float z[kSpanBlocks][kE], top[kSpanBlocks], m = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < kSpanBlocks; ++b) {
+            Row<kBf16>::unpack(v[b], z[b]);
+            top[b] = z[b][0];
+#pragma unroll
+            for (int e = 1; e < kE; ++e)
+                top[b] = fmaxf(top[b], z[b][e]);
+            top[b] = wave_max_f(top[b]);
+            m = fmaxf(m, top[b]);
+        }
+        if (lane < kSpanBlocks) {
+            float t = top[0];
+#pragma unroll
+            for (int b = 1; b < kSpanBlocks; ++b)
+                t = lane == b ? top[b] : t;
+            st.maxima[w * kSpanBlocks + lane] = t;
+        }
+        if (f.sums()) {
+            double sum = 0.;
+            if (m > -INFINITY) {
+                const double md = m;
+#pragma unroll
+                for (int b = 0; b < kSpanBlocks; ++b)
+#pragma unroll
+                    for (int e = 0; e < kE; ++e)
+                        sum += weight_of(z[b][e], md, f.c);
+            }
+            sum = wave_sum_64(sum);
+            if (lane == 0)
+                st.sums[w] = sum;
+        }
+    }
+}
+
+struct PickLds {
+    float max[kMaxBlocks];       // the blocks' maxima
+    uint16_t list[kMaxBlocks];   // blocks that may hold a kept token
+    double red[kPickWaves];
+    uint32_t cnt[kPickWaves];
+    uint32_t n;                  // a counter, a result
+    uint32_t found;
+    double total, before;
+    uint64_t d0;
+    union {
+        struct {
+            uint64_t key[kSampleSort];  // ~key of the logit and index, ascending: the filters' order
+            double w[kSampleSort];
+        } sort;
+        struct {
+            unsigned long long w[kDigits];
+            uint32_t n[kDigits];
+        } hist;
+        struct {
+            double sum[kMaxBlocks];
+            uint32_t ties[kMaxBlocks];
+        } draw;
+    };
+};
+static_assert(sizeof(PickLds) <= 64 << 10, "LDS of a workgroup");
+
+// Sums over the workgroup's threads in their order: inclusive scan and the total.  The LDS is free
+// again after the caller's next barrier.
+__device__ __forceinline__ double block_scan_64(double x, double *red, double &total)
+{
+    const int wave = threadIdx.x >> 6;
+    x = wave_scan_64(x);
+    if ((threadIdx.x & 63) == 63)
+        red[wave] = x;
+    __syncthreads();
+    double base = 0., t = 0.;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) {
+        base = w == wave ? t : base;
+        t += red[w];
+    }
+    total = t;
+    return base + x;
+}
+
+__device__ __forceinline__ uint32_t block_scan_32(uint32_t x, uint32_t *cnt, uint32_t &total)
+{
+    const int wave = threadIdx.x >> 6;
+    x = wave_scan_add(x);
+    if ((threadIdx.x & 63) == 63)
+        cnt[wave] = x;
+    __syncthreads();
+    uint32_t base = 0, t = 0;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) {
+        base = w == wave ? t : base;
+        t += cnt[w];
+    }
+    total = t;
+    return base + x;
+}
+
+// Ascending bitonic sort of size (a power of two, at most kSampleSort) keys.
+__device__ __forceinline__ void sort_keys(uint64_t *key, int size)
+{
+    const int t = threadIdx.x;
+    for (int k = 2; k <= size; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            if (t < size >> 1) {
+                const int i = 2 * t - (t & (j - 1));
+                const uint64_t a = key[i], b = key[i + j];
+                if ((a > b) == ((i & k) == 0)) {
+                    key[i] = b;
+                    key[i + j] = a;
+                }
+            }
+            __syncthreads();
+        }
+}
+
+__device__ __forceinline__ int pow2_from(int n)
+{
+    return n <= 2 ? 2 : 1 << (32 - __builtin_clz(n - 1));
+}
+
+// Which tokens are kept: those above `key`, the first `ties` of those at it, and of both w >= q.
+struct Rule {
+    uint32_t key, ties;
+    double q;
+};
+
+template <bool kBf16>
+struct Picker {
+    static constexpr int kE = kElems<kBf16>;
+    const SampleArgs &a;
+    PickLds &s;
+    const Row<kBf16> r;
+    const Filters f;
+    const int64_t row;
+    int vecs, blocks;
+    float m;
+    double md;
+
+    __device__ __forceinline__ Picker(const SampleArgs &args, PickLds &lds, int64_t row_)
+        : a(args), s(lds), r(args, row_), f(args, row_), row(row_)
+    {
+        vecs = r.vecs();
+        blocks = (vecs + kBlockVecs - 1) / kBlockVecs;
+    }
+
+    __device__ __forceinline__ void answer(int token, double logprob)
+    {
+        if (threadIdx.x == 0) {
+            a.tokens[row] = token;
+            if (a.logprobs)
+                a.logprobs[row] = (float)logprob;
+        }
+    }
+
+    __device__ __forceinline__ void load_block(int b, float (&z)[kE]) const
+    {
+        Row<kBf16>::unpack(r.load(min(b * kBlockVecs + (int)(threadIdx.x & 63), vecs)), z);
+    }
+    __device__ __forceinline__ int index_in(int b, int e) const
+    {
+        return r.index(b * kBlockVecs + (int)(threadIdx.x & 63), e);
+    }
+
+    // Calls use(j, z) with the 64 vectors of every listed block j, in the waves' turns.
+    template <typename Use>
+    __device__ __forceinline__ void each_block(int n, Use use)
+    {
+        constexpr int kAhead = 4;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        for (int j0 = wave; j0 < n; j0 += kAhead * kPickWaves) {
+            u32x4_t v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int j = min(j0 + i * kPickWaves, n - 1);
+                v[i] = r.load(min((int)s.list[j] * kBlockVecs + lane, vecs));
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int j = j0 + i * kPickWaves;
+                if (j < n) {
+                    float z[kE];
+                    Row<kBf16>::unpack(v[i], z);
+                    use(j, z);
+                }
+            }
+        }
+    }
+
+    // The blocks whose maximum reaches tau (and holds a token at all), in order; their number.
+    __device__ __forceinline__ int list_blocks(float tau)
+    {
+        uint32_t n = 0;
+        for (int b0 = 0; b0 < blocks; b0 += kPickThreads) {
+            const int b = b0 + threadIdx.x;
+            const bool in = b < blocks && s.max[b] >= tau && s.max[b] > -INFINITY;
+            uint32_t total;
+            const uint32_t at = block_scan_32(in ? 1u : 0u, s.cnt, total);
+            if (in)
+                s.list[n + at - 1] = (uint16_t)b;
+            n += total;
+            __syncthreads();
+        }
+        return (int)n;
+    }
+
+    __device__ __forceinline__ void greedy()
+    {
+        if (threadIdx.x == 0)
+            s.found = 0xffffffffu;
+        __syncthreads();
+        for (int b = threadIdx.x; b < blocks; b += kPickThreads)
+            if (s.max[b] == m)
+                atomicMin(&s.found, (uint32_t)b);
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            const int b = (int)s.found;
+            float z[kE];
+            load_block(b, z);
+            uint32_t at = 0xffffffffu;
+#pragma unroll
+            for (int e = kE - 1; e >= 0; --e)
+                at = z[e] == m ? (uint32_t)index_in(b, e) : at;
+            answer((int)wave_min(at), 0.);
+        }
+    }
+
+    // A lower bound of the k-th largest block maximum, exact to its upper 16 key bits (k <= blocks).
+    __device__ __forceinline__ float kth_maximum(int k)
+    {
+        if (threadIdx.x < 64) {
+            uint32_t key = 0;
+            for (int bit = 31; bit >= 16; --bit) {
+                const uint32_t t = key | 1u << bit;
+                int n = 0;
+                for (int b0 = 0; b0 < blocks; b0 += 64) {
+                    const int b = b0 + (int)threadIdx.x;
+                    n += __popcll(__ballot(b < blocks && key_of(s.max[b < blocks ? b : 0]) >= t));
+                }
+                key = n >= k ? t : key;
+            }
+            if (threadIdx.x == 0)
+                s.n = key;
+        }
+        __syncthreads();
+        const uint32_t key = s.n;
+        __syncthreads();
+        // (keys below that of -inf belong to no number)
+        return key <= key_of(-INFINITY) ? -INFINITY : logit_of(key);
+    }
+
+    // Tokens of at least tau into the sorting LDS, any order; their number (more than fit: not all).
+    __device__ __forceinline__ int collect(int n_list, float tau)
+    {
+        if (threadIdx.x == 0)
+            s.n = 0;
+        __syncthreads();
+        each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
+            const int b = s.list[j];
+            uint32_t mine = 0;
+#pragma unroll
+            for (int e = 0; e < kE; ++e)
+                mine += z[e] >= tau && z[e] > -INFINITY ? 1u : 0u;
+            if (__ballot(mine != 0) == 0)
+                return;
+            const uint32_t incl = wave_scan_add(mine);
+            uint32_t at = 0;
+            if ((threadIdx.x & 63) == 63)
+                at = atomicAdd(&s.n, incl);
+            at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + incl - mine;
+#pragma unroll
+            for (int e = 0; e < kE; ++e)
+                if (z[e] >= tau && z[e] > -INFINITY) {
+                    if (at < (uint32_t)kSampleSort)
+                        s.sort.key[at] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(b, e);
+                    ++at;
+                }
+        });
+        __syncthreads();
+        return (int)s.n;
+    }
+
+    // The whole rest on n collected tokens; whole: the sum over all tokens (without top-k).
+    __device__ __forceinline__ void finish_sorted(int n, double whole)
+    {
+        const int t = threadIdx.x;
+        int size = pow2_from(n);
+        for (int i = n + t; i < size; i += kPickThreads)
+            s.sort.key[i] = ~0ull;
+        __syncthreads();
+        sort_keys(s.sort.key, size);
+        double w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = 2 * t + i;
+            w[i] = j < n ? weight_of(logit_of(~(uint32_t)(s.sort.key[j] >> 32)), md, f.c) : 0.;
+        }
+        double total;
+        const double incl = block_scan_64(w[0] + w[1], s.red, total);
+        const double before[2] = {incl - w[1] - w[0], incl - w[1]};
+        int keep = f.k && f.k < n ? f.k : n;
+        __syncthreads();
+        if (f.k) {  // the sum over top-k's
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (2 * t + i == keep - 1)
+                    s.total = before[i] + w[i];
+            __syncthreads();
+            whole = s.total;
+        }
+        const double most = (double)f.p * whole;
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = 2 * t + i;
+            if (j < keep && (j == 0 || f.p >= 1.f || before[i] < most) && w[i] >= (double)f.q)
+                ++mine;
+            if (j < n)
+                s.sort.w[j] = w[i];
+        }
+        uint32_t kept;
+        block_scan_32(mine, s.cnt, kept);
+        keep = (int)kept;  // (the conditions hold for a first part of the order)
+        // ---- the kept by index
+        uint64_t key[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            key[i] = s.sort.key[2 * t + i < size ? 2 * t + i : 0];
+        __syncthreads();
+        size = pow2_from(keep);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = 2 * t + i;
+            if (j < size)
+                s.sort.key[j] = j < keep ? key[i] << 32 | (uint32_t)j : ~0ull;
+        }
+        if (t == 0)
+            s.found = (uint32_t)keep - 1;
+        __syncthreads();
+        sort_keys(s.sort.key, size);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = 2 * t + i;
+            w[i] = j < keep ? s.sort.w[(uint32_t)s.sort.key[j]] : 0.;
+        }
+        const double run = block_scan_64(w[0] + w[1], s.red, total);
+        const double at = uniform() * total;
+        if (2 * t < keep && run - w[1] > at)
+            atomicMin(&s.found, (uint32_t)(2 * t));
+        else if (2 * t + 1 < keep && run > at)
+            atomicMin(&s.found, (uint32_t)(2 * t + 1));
+        __syncthreads();
+        if (t == 0) {
+            const uint64_t k = s.sort.key[s.found];
+            answer((int)(k >> 32), log(s.sort.w[(uint32_t)k] / total));
+        }
+    }
+
+    __device__ __forceinline__ double uniform() const
+    {
+        const float u = a.uniform[row];
+        return u > 0.f ? fminf(u, 1.f - FLT_EPSILON / 2) : 0.;
+    }
+
+    // The draw among the listed blocks' kept tokens.  whole > 0: the sum over all kept tokens, of which
+    // `skip` lie before the list.
+    __device__ __forceinline__ void draw(int n, const Rule &rule, double whole, double skip)
+    {
+        const double tie_w = weight_of(logit_of(rule.key), md, f.c);
+        each_block(n, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
+            double sum = 0.;
+            uint32_t ties = 0;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) {
+                const uint32_t key = key_of(z[e]);
+                const double w = weight_of(z[e], md, f.c);
+                sum += key > rule.key && w >= rule.q ? w : 0.;
+                ties += key == rule.key ? 1u : 0u;
+            }
+            sum = wave_sum_64(sum);
+            ties = wave_scan_add(ties);
+            if ((threadIdx.x & 63) == 63) {
+                s.draw.sum[j] = sum;
+                s.draw.ties[j] = ties;
+            }
+        });
+        __syncthreads();
+        const int per = (n + kPickThreads - 1) / kPickThreads;
+        const int j0 = min(n, (int)threadIdx.x * per), j1 = min(n, j0 + per);
+        if (threadIdx.x == 0)
+            s.found = 0xffffffffu;
+        uint32_t mine = 0, ties;
+        for (int j = j0; j < j1; ++j)
+            mine += s.draw.ties[j];
+        uint32_t first = block_scan_32(mine, s.cnt, ties) - mine;
+        double part = 0.;
+        const bool tie_in = tie_w >= rule.q;
+        for (int j = j0; j < j1; ++j) {
+            const uint32_t c = s.draw.ties[j];
+            const uint32_t in = tie_in && first < rule.ties ? min(c, rule.ties - first) : 0u;
+            s.draw.sum[j] += in * tie_w;
+            s.draw.ties[j] = in;  // (from here on: the ties of the block that are kept)
+            first += c;
+            part += s.draw.sum[j];
+        }
+        double total;
+        double run = block_scan_64(part, s.red, total) - part;
+        const double at = whole > 0. ? uniform() * whole - skip : uniform() * total;
+        uint32_t hit = 0xffffffffu;
+        double hit_run = 0.;
+        for (int j = j0; j < j1; ++j) {
+            if (hit == 0xffffffffu && run + s.draw.sum[j] > at && s.draw.sum[j] > 0.) {
+                hit = (uint32_t)j;
+                hit_run = run;
+            }
+            run += s.draw.sum[j];
+        }
+        if (hit != 0xffffffffu)
+            atomicMin(&s.found, hit);
+        __syncthreads();
+        if (s.found == hit && hit != 0xffffffffu)
+            s.before = hit_run;
+        __syncthreads();
+        bool last = false;
+        if (s.found == 0xffffffffu) {  // rounding: the last kept token
+            last = true;
+            __syncthreads();
+            if (threadIdx.x == 0)
+                s.found = 0;
+            __syncthreads();
+            for (int j = j0; j < j1; ++j)
+                if (s.draw.sum[j] > 0.)
+                    atomicMax(&s.found, (uint32_t)j);
+            __syncthreads();
+        }
+        if (threadIdx.x >= 64)
+            return;
+        const int j = (int)s.found, b = s.list[j];
+        float z[kE];
+        double w[kE], sum = 0.;
+        load_block(b, z);
+        uint32_t c = 0;
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+            c += key_of(z[e]) == rule.key ? 1u : 0u;
+        uint32_t rank = wave_scan_add(c) - c;
+        uint32_t at_e = 0xffffffffu, last_e = 0;
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const uint32_t key = key_of(z[e]);
+            const double x = weight_of(z[e], md, f.c);
+            const bool keep = key == rule.key ? rank < s.draw.ties[j] : key > rule.key && x >= rule.q;
+            rank += key == rule.key ? 1u : 0u;
+            w[e] = keep ? x : 0.;
+            sum += w[e];
+            last_e = w[e] > 0. ? (uint32_t)e : last_e;
+            any = any || w[e] > 0.;
+        }
+        double here = s.before + (wave_scan_64(sum) - sum);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            here += w[e];
+            if (at_e == 0xffffffffu && w[e] > 0. && here > at)
+                at_e = (uint32_t)e;
+        }
+        const uint64_t hits = last ? 0 : __ballot(at_e != 0xffffffffu);
+        const uint64_t some = __ballot(any);  // (the block's sum is above 0)
+        const int lane = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(some);
+        const uint32_t el = hits ? at_e : last_e;
+        float zt = z[0];
+#pragma unroll
+        for (int e = 1; e < kE; ++e)
+            zt = el == (uint32_t)e ? z[e] : zt;
+        zt = __shfl(zt, lane, 64);
+        const int token = __shfl(index_in(b, (int)el), lane, 64);
+        answer(token, ((double)zt - md) / f.t - log(whole > 0. ? whole : total));
+    }
+
+    // ---- thresholds by digits of the keys, for more candidates than are sorted
+    struct Cut {
+        uint32_t key, ties;
+        uint64_t w;   // fixed-point weight of the kept
+        bool all;     // fewer than asked for: every candidate is kept
+    };
+
+    // The cut behind which `want` tokens (by_count), or the fixed-point weight `want`, are reached.
+    __device__ __forceinline__ Cut cut(int n, uint32_t low, bool by_count, uint64_t want, double unit)
+    {
+        const uint32_t top = key_of(m);
+        const uint32_t range = top - low;
+        int bits = range ? 32 - __builtin_clz(range) : 0;
+        uint32_t d0 = 0;
+        uint64_t width = 1ull << bits, seen_n = 0, seen_w = 0;
+        for (;;) {
+            const int shift = bits > kDigitBits ? bits - kDigitBits : 0;
+            for (int i = threadIdx.x; i < kDigits; i += kPickThreads) {
+                s.hist.w[i] = 0;
+                s.hist.n[i] = 0;
+            }
+            if (threadIdx.x == 0)
+                s.found = 0xffffffffu;
+            __syncthreads();
+            each_block(n, [&](int, const float(&z)[kE]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < kE; ++e) {
+                    const uint32_t key = key_of(z[e]);
+                    const uint64_t d = (uint64_t)(top - key) - d0;  // (below d0: wraps, out of width)
+                    if (key >= low && key <= top && d < width) {
+                        const int bin = (int)(d >> shift);
+                        atomicAdd(&s.hist.w[bin], (unsigned long long)__builtin_rint(
+                                                      weight_of(z[e], md, f.c) * unit));
+                        atomicAdd(&s.hist.n[bin], 1u);
+                    }
+                }
+            });
+            __syncthreads();
+            // two digits a thread, in order
+            const int i = 2 * threadIdx.x;
+            const uint64_t w0 = s.hist.w[i], w1 = s.hist.w[i + 1];
+            const uint32_t n0 = s.hist.n[i], n1 = s.hist.n[i + 1];
+            uint32_t total_n;
+            const uint32_t incl_n = block_scan_32(n0 + n1, s.cnt, total_n);
+            const uint64_t incl_w = scan_u64(w0 + w1);
+            const uint64_t bn = seen_n + incl_n - n1 - n0, bw = seen_w + incl_w - w1 - w0;
+            if (n0 && (by_count ? bn + n0 >= want : bw + w0 >= want))
+                atomicMin(&s.found, (uint32_t)i);
+            else if (n1 && (by_count ? bn + n0 + n1 >= want : bw + w0 + w1 >= want))
+                atomicMin(&s.found, (uint32_t)i + 1);
+            __syncthreads();
+            const uint32_t bin = s.found;
+            if (bin == 0xffffffffu) {
+                const uint64_t w = seen_w + s.d0;  // (the scan's total)
+                __syncthreads();
+                return Cut{low, 0xffffffffu, w, true};
+            }
+            __syncthreads();
+            if (bin >> 1 == threadIdx.x) {
+                s.hist.w[0] = bin & 1 ? bw + w0 : bw;
+                s.hist.n[0] = (uint32_t)(bin & 1 ? bn + n0 : bn);
+                s.hist.n[1] = bin & 1 ? n1 : n0;
+            }
+            __syncthreads();
+            seen_w = s.hist.w[0];
+            seen_n = s.hist.n[0];
+            const uint32_t here = s.hist.n[1];
+            __syncthreads();
+            d0 += bin << shift;
+            if (shift == 0) {
+                const uint32_t key = top - d0;
+                const uint64_t w = (uint64_t)__builtin_rint(weight_of(logit_of(key), md, f.c) * unit);
+                uint64_t ties = by_count ? want - seen_n
+                                         : (w ? (want - seen_w + w - 1) / w : here);
+                ties = ties < 1 ? 1 : (ties < here ? ties : here);
+                return Cut{key, (uint32_t)ties, seen_w + ties * w, false};
+            }
+            bits = shift;
+            width = 1ull << bits;
+        }
+    }
+
+    // Inclusive scan of 64-bit whole numbers over the threads; the total stays in s.d0.
+    __device__ __forceinline__ uint64_t scan_u64(uint64_t x)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t lo = __shfl_up((uint32_t)x, d, 64), hi = __shfl_up((uint32_t)(x >> 32), d, 64);
+            if (lane >= d)
+                x += (uint64_t)hi << 32 | lo;
+        }
+        __syncthreads();
+        uint64_t *red = reinterpret_cast<uint64_t *>(s.red);
+        if (lane == 63)
+            red[wave] = x;
+        __syncthreads();
+        uint64_t base = 0, t = 0;
+#pragma unroll
+        for (int w = 0; w < kPickWaves; ++w) {
+            base = w == wave ? t : base;
+            t += red[w];
+        }
+        if (threadIdx.x == 0)
+            s.d0 = t;
+        return base + x;
+    }
+
+    __device__ __forceinline__ Rule cut_by_digits(int n, float tau, double whole)
+    {
+        const uint32_t low = key_of(fmaxf(tau, -FLT_MAX));
+        if (f.k) {  // the candidates' sum, for the fixed point's unit
+            double sum = 0.;
+            each_block(n, [&](int, const float(&z)[kE]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < kE; ++e)
+                    sum += key_of(z[e]) >= low ? weight_of(z[e], md, f.c) : 0.;
+            });
+            block_scan_64(sum, s.red, whole);
+            __syncthreads();
+        }
+        // a power of two that brings the sum to 2^60 .. 2^61: weights lose 2^-61 of it each
+        const int exponent = (int)(__builtin_bit_cast(uint64_t, whole) >> 52) - 1023;
+        const double unit = __builtin_ldexp(1., 60 - exponent);
+        Rule rule{low, 0xffffffffu, (double)f.q};
+        double most = whole * unit;
+        for (int by_count = f.k ? 1 : 0; by_count >= (f.p < 1.f ? 0 : 1); --by_count) {
+            const uint64_t want = by_count ? (uint64_t)f.k : (uint64_t)__builtin_ceil((double)f.p * most);
+            const Cut c = cut(n, low, by_count != 0, want, unit);
+            most = (double)c.w;
+            if (!c.all && (c.key > rule.key || (c.key == rule.key && c.ties < rule.ties)))
+                rule = Rule{c.key, c.ties, (double)f.q};
+        }
+        return rule;
+    }
+
+    __device__ __forceinline__ void run(const Stats &st)
+    {
+        const int64_t first = row * st.spans;
+        float top = -INFINITY;
+        for (int b = threadIdx.x; b < blocks; b += kPickThreads) {
+            const float x = st.maxima[first * kSpanBlocks + b];
+            s.max[b] = x;
+            top = fmaxf(top, x);
+        }
+        top = wave_max_f(top);
+        if ((threadIdx.x & 63) == 0)
+            s.cnt[threadIdx.x >> 6] = __float_as_uint(top);
+        __syncthreads();
+        m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kPickWaves; ++w)
+            m = fmaxf(m, __uint_as_float(s.cnt[w]));
+        md = m;
+        __syncthreads();
+        if (!(m > -INFINITY)) {  // every token is masked
+            answer(-1, -INFINITY);
+            return;
+        }
+        if (f.greedy) {
+            greedy();
+            return;
+        }
+        int n_list = 0;
+        double whole = 0.;
+        const bool plain = f.k == 0 && f.p >= 1.f && !(f.q > 0.f);
+        if (f.k == 0) {
+            // ---- a span's sum per thread, brought to the row's maximum
+            const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
+            double x = 0.;
+            if (t < spans) {
+                float sm = s.max[kSpanBlocks * t];
+                for (int b = 1; b < kSpanBlocks; ++b)
+                    if (kSpanBlocks * t + b < blocks)
+                        sm = fmaxf(sm, s.max[kSpanBlocks * t + b]);
+                if (sm > -INFINITY)
+                    x = st.sums[first + t] * weight_of(sm, md, f.c);
+            }
+            const double incl = block_scan_64(x, s.red, whole);
+            if (plain) {  // one span holds the token
+                const double at = uniform() * whole;
+                if (t == 0) {
+                    s.found = 0xffffffffu;
+                    s.n = 0;
+                }
+                __syncthreads();
+                if (x > 0.) {
+                    if (incl > at)
+                        atomicMin(&s.found, (uint32_t)t);
+                    atomicMax(&s.n, (uint32_t)t);
+                }
+                __syncthreads();
+                const uint32_t hit = s.found == 0xffffffffu ? s.n : s.found;
+                if ((uint32_t)t == hit)
+                    s.total = incl - x;
+                if (t < kSpanBlocks)
+                    s.list[t] = (uint16_t)(kSpanBlocks * hit + t);
+                n_list = min(kSpanBlocks, blocks - kSpanBlocks * (int)hit);
+            }
+            __syncthreads();
+        }
+        Rule rule{0u, 0xffffffffu, (double)f.q};
+        if (!plain) {
+            // ---- a bound that every kept token reaches (and what top-p's sum is over)
+            float tau = -INFINITY;
+            if (f.k) {
+                if (f.k <= blocks)
+                    tau = kth_maximum(f.k);
+            } else if (f.p < 1.f) {
+                tau = below(md + log((1. - (double)f.p) * whole / a.vocab) * f.t);
+            }
+            if (f.q > 0.f && !(f.k && f.p < 1.f))
+                tau = fmaxf(tau, below(md + log((double)f.q) * f.t));
+            n_list = list_blocks(tau);
+            if (f.k || f.p < 1.f) {
+                const int n = collect(n_list, tau);
+                if (n <= kSampleSort) {
+                    finish_sorted(n, whole);
+                    return;
+                }
+                __syncthreads();
+                rule = cut_by_digits(n_list, tau, whole);
+            }
+        }
+        draw(n_list, rule, plain ? whole : 0., plain ? s.total : 0.);
+    }
+
+    // A float below a bound by more than the bound's own error (NaN: none).
+    __device__ __forceinline__ float below(double x) const
+    {
+        x -= 1e-6 * (fabs(x) + fabs(md));
+        return x == x ? fminf((float)x, m) : -INFINITY;
+    }
+};
+
+template <bool kBf16>
+__global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a, Stats st)
+{
+    __shared__ PickLds s;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        Picker<kBf16> p(a, s, row);
+        p.run(st);
+        if (row + gridDim.x < a.rows)
+            __syncthreads();  // the LDS is written again
+    }
+}
+
+int sample_spans(int vocab, bool bf16)
+{
+    const int e = bf16 ? 8 : 4;
+    return ((vocab + 2 * (e - 1)) / e + kSpanVecs - 1) / kSpanVecs;
+}
+
+}  // namespace
+
+size_t sample_workspace(int64_t rows, int vocab, bool bf16)
+{
+    return (size_t)rows * sample_spans(vocab, bf16) * (sizeof(double) + kSpanBlocks * sizeof(float));
+}
+
+hipError_t launch_sample(const SampleArgs &a, void *workspace, hipStream_t stream)
+{
+    const int spans = sample_spans(a.vocab, a.bf16);
+    const Stats st{static_cast<double *>(workspace),
+                   reinterpret_cast<float *>(static_cast<double *>(workspace) + a.rows * spans),
+                   spans};
+    int64_t blocks = (a.rows * spans + kStatWaves - 1) / kStatWaves;
+    blocks = blocks < kSampleGrid ? blocks : kSampleGrid;
+    hipLaunchKernelGGL(a.bf16 ? k_sample_stats<true> : k_sample_stats<false>, dim3((unsigned)blocks),
+                       dim3(kStatThreads), 0, stream, a, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return e;
+    blocks = a.rows < kSampleGrid ? a.rows : kSampleGrid;
+    hipLaunchKernelGGL(a.bf16 ? k_sample_pick<true> : k_sample_pick<false>, dim3((unsigned)blocks),
+                       dim3(kPickThreads), 0, stream, a, st);
+    return hipGetLastError();
+}
+
+}  // namespace sparrow

@@ -44,6 +44,7 @@ SPARROW_OP_DENSE_ATTN = 2
 SPARROW_OP_DECODE_STEP = 3
 SPARROW_NOALLOC_SCRATCH_BYTES = 32 << 20
 SPARROW_ROPE_WORKSPACE_BYTES = 1 << 20
+SPARROW_SAMPLE_MAX_VOCAB = 524288
 
 EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_topk",
            "sparrow_append_score_topk", "sparrow_sparse_decode_attn", "sparrow_dense_decode_attn",
@@ -52,7 +53,7 @@ EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_
            "sparrow_qk_norm_rope", "sparrow_qk_norm_rope_bwd", "sparrow_append_kv_e4m3",
            "sparrow_read_kv_e4m3", "sparrow_sparse_decode_attn_e4m3",
            "sparrow_dense_decode_attn_e4m3", "sparrow_residual_norm", "sparrow_residual_norm_bwd",
-           "sparrow_residual_norm_workspace_size",
+           "sparrow_residual_norm_workspace_size", "sparrow_sample", "sparrow_sample_workspace_size",
            "sparrow_budget_bound", "sparrow_workspace_size", "sparrow_status_string")
 
 
@@ -136,8 +137,12 @@ def load():
                                               ctypes.c_float, ctypes.c_float, _p, _p,
                                               ctypes.c_int64, _p, ctypes.c_int64, _p, _p, _p,
                                               ctypes.c_size_t, _p]
+    lib.sparrow_sample.argtypes = [ctypes.c_int64, _i32, _i32, _p, ctypes.c_int64, _p, _p, _p, _p,
+                                   _p, _p, _p, _p, ctypes.c_size_t, _p]
     for fn in EXPORTS[:-3]:
         getattr(lib, fn).restype = ctypes.c_int
+    lib.sparrow_sample_workspace_size.argtypes = [ctypes.c_int64, _i32, _i32]
+    lib.sparrow_sample_workspace_size.restype = ctypes.c_size_t
     lib.sparrow_residual_norm_workspace_size.argtypes = [ctypes.c_int64, _i32]
     lib.sparrow_residual_norm_workspace_size.restype = ctypes.c_size_t
     lib.sparrow_budget_bound.argtypes = [_p, ctypes.c_int64, _i32, _i32, _i32, _p, _p, _i32, _p]
@@ -221,6 +226,17 @@ def sparrow_tail_stats(num_tokens, alpha, positions, bin_tokens, n_bins, percent
                        mean, count, stream):
     return load().sparrow_tail_stats(num_tokens, alpha, positions, bin_tokens, n_bins, percentile,
                                      quantile, mean, count, stream)
+
+
+def sparrow_sample(num_rows, vocab, logits_dtype, logits, row_stride, temperature, top_k, top_p,
+                   min_p, uniform, tokens, logprobs, workspace, ws_bytes, stream):
+    return load().sparrow_sample(num_rows, vocab, logits_dtype, logits, row_stride, temperature,
+                                 top_k, top_p, min_p, uniform, tokens, logprobs, workspace, ws_bytes,
+                                 stream)
+
+
+def sparrow_sample_workspace_size(num_rows, vocab, logits_dtype) -> int:
+    return int(load().sparrow_sample_workspace_size(num_rows, vocab, logits_dtype))
 
 
 def sparrow_qk_norm_rope(num_tokens, num_q_heads, num_k_heads, head_dim, q, q_stride, k, k_stride,
@@ -701,6 +717,46 @@ def _launch(name, device, *args):
             rc = fn(*args, _stream_of(device))
     if rc != SPARROW_OK:
         raise SparrowError(name, rc)
+
+
+def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None,
+           logprobs=None, workspace=None):
+    """The next token of every row of logits ``[T][V]`` (fp32 or bf16, rows at any stride): drawn by
+    the row's uniform number (fp32 ``[T]``) from what temperature, top-k, top-p and min-p (``[T]``,
+    fp32; top_k int32) leave of its distribution.  Returns (tokens int32 ``[T]``, logprobs fp32
+    ``[T]``: the log-probability that each was drawn with); a row with every token masked gives -1 and
+    -inf."""
+    import torch
+    _require_device(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T][V]")
+    dt = SPARROW_LOGITS_F32 if logits.dtype is torch.float32 else SPARROW_LOGITS_BF16
+    if logits.dtype is not torch.float32 and logits.dtype is not torch.bfloat16:
+        raise ValueError(f"logits: dtype {logits.dtype}, expected {torch.float32} or {torch.bfloat16}")
+    T, V = logits.shape
+    dev = logits.device
+    row, one = logits.stride()
+    row = V if T <= 1 else row
+    if V < 1 or (V > 1 and one != 1) or row < V:
+        raise ValueError(f"logits: shape {tuple(logits.shape)} with strides {logits.stride()}, expected "
+                         "contiguous vocabulary entries and rows that do not overlap")
+    _expect(uniform, "uniform", torch.float32, (T,), dev)
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is not None:
+            _expect(t, name, dtype, (T,), dev)
+    logprobs = _given_like(logprobs, "logprobs", uniform)
+    tokens = _given(tokens, "tokens", torch.int32, (T,), dev)
+    if T == 0:
+        return tokens, logprobs
+    if workspace is None:
+        workspace = _workspace(sparrow_sample_workspace_size(T, V, dt), dev)
+    else:
+        workspace = _given_workspace(workspace, None, dev)
+    _launch("sparrow_sample", dev, T, V, dt, logits.data_ptr(), row, _ptr(temperature), _ptr(top_k),
+            _ptr(top_p), _ptr(min_p), uniform.data_ptr(), tokens.data_ptr(), logprobs.data_ptr(),
+            workspace.data_ptr(), workspace.nbytes)
+    return tokens, logprobs
 
 
 def _expect_rows(t, name, shape, device):

@@ -1,0 +1,357 @@
+"""Token sampling against its definition in 64 bits on the CPU.
+
+Tokens have to be equal: the definition's sums are off by at most some 1e-11 of the whole (a running sum of
+half a million terms in 64 bits), and no case here has a border that close except rows of equal logits,
+whose weights and sums are whole numbers on both sides.  A log-probability is rounded to fp32 once:
+2^-24 of its value, and the weights' 1e-13."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_08446_amd import sparrow as S
+
+from parity import log
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu(gpu_device):
+    S.load()
+    yield
+
+
+def reference(z, u, t=1.0, k=0, p=1.0, q=0.0):
+    """(token, log-probability) of one row of float64 logits; f32 settings as float64."""
+    z = np.where(np.isnan(z), -np.inf, np.minimum(z, np.finfo(np.float32).max)) + 0.0
+    top = z.max()
+    if top == -np.inf:
+        return -1, -math.inf
+    if not t > 0 or k == 1 or p <= 0:
+        return int(np.argmax(z)), 0.0
+    ids = np.nonzero(z > -np.inf)[0]
+    with np.errstate(under="ignore"):
+        x = (z[ids] - top) / t if np.isfinite(t) else np.zeros(len(ids))
+        w = np.exp(x)
+        order = np.lexsort((ids, -z[ids]))
+        if 0 < k < len(z):
+            order = order[:k]
+        if p < 1:
+            c = np.cumsum(w[order])
+            before = np.concatenate([[0.0], c[:-1]])
+            keep = before < p * c[-1]
+            keep[0] = True
+            order = order[keep]
+        if q > 0:
+            order = order[w[order] >= min(q, 1.0)]
+        at = np.sort(order)
+        c = np.cumsum(w[at])
+        u = min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
+        j = int(np.searchsorted(c, u * c[-1], side="right"))
+    return int(ids[at[j]]), float(x[at[j]] - math.log(c[-1]))
+
+
+def check(z, u, t=None, k=None, p=None, q=None, got=None):
+    got = S.sample(z, u, temperature=t, top_k=k, top_p=p, min_p=q) if got is None else got
+    tok, lp = got[0].cpu().numpy(), got[1].cpu().numpy().astype(np.float64)
+    zs = z.float().cpu().numpy().astype(np.float64)
+
+    def col(x, default):
+        return [default] * len(zs) if x is None else x.cpu().numpy().astype(np.float64).tolist()
+    for i, row in enumerate(zip(zs, col(u, 0), col(t, 1.0), col(k, 0), col(p, 1.0), col(q, 0.0))):
+        want, want_lp = reference(row[0], row[1], row[2], int(row[3]), row[4], row[5])
+        assert tok[i] == want, (i, row[1:], tok[i], want)
+        if math.isinf(want_lp):
+            assert lp[i] == want_lp
+        else:
+            assert abs(lp[i] - want_lp) <= 2.0 ** -24 * abs(want_lp) + 1e-12, (i, lp[i], want_lp)
+
+
+def logits(T, V, seed, dtype=F32, spread=2.0, hot=True, pad=0, off=0):
+    """Rows of a padded buffer, `off` elements behind its start."""
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn((T, V), generator=g) * spread
+    if hot:
+        at = torch.randint(0, V, (T, min(V, 40)), generator=g)
+        z.scatter_add_(1, at, 12 * torch.rand(at.shape, generator=g))
+    buf = torch.full((T * (V + pad) + off,), 99.0).to(dtype).to(DEV)  # (padding would win)
+    v = buf[off:].view(T, V + pad)[:, :V]
+    v.copy_(z.to(dtype))
+    return v
+
+
+def rand(T, seed, lo=0.0, hi=1.0):
+    g = torch.Generator().manual_seed(1000 + seed)
+    return (lo + (hi - lo) * torch.rand(T, generator=g)).to(DEV)
+
+
+def ints(T, seed, lo, hi):
+    g = torch.Generator().manual_seed(2000 + seed)
+    return torch.randint(lo, hi + 1, (T,), generator=g, dtype=torch.int32).to(DEV)
+
+
+SIZES = [(3, 1), (4, 2), (5, 7), (9, 64), (33, 1000), (8, 4099), (6, 50021), (5, 151936), (2, 524288)]
+KINDS = ["none", "t", "k", "p", "q", "kp", "kq", "pq", "kpq"]
+
+
+@pytest.mark.parametrize("T,V", SIZES)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype,pad,off", [(F32, 0, 0), (F32, 3, 1), (BF, 0, 0), (BF, 5, 3)])
+def test_filters(T, V, kind, dtype, pad, off):
+    log(f"case sample T={T} V={V} {kind} {dtype} pad={pad} off={off}")
+    z = logits(T, V, T + V, dtype, pad=pad, off=off)
+    check(z, rand(T, V), None if kind == "none" else rand(T, 1, 0.5, 1.3),
+          ints(T, 2, 1, 70) if "k" in kind else None, rand(T, 3, 0.5, 0.99) if "p" in kind else None,
+          rand(T, 4, 0.01, 0.2) if "q" in kind else None)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("kind", ["k", "p", "kp", "kpq"])
+def test_wide_sets(dtype, kind):
+    # more kept tokens than are sorted: flat rows, thousands of top-k's
+    T, V = 12, 60013
+    z = logits(T, V, 5, dtype, spread=1.0, hot=False, pad=1)
+    check(z, rand(T, 6), rand(T, 7, 0.7, 3.0), ints(T, 8, 2000, 50000) if "k" in kind else None,
+          rand(T, 9, 0.3, 0.999) if "p" in kind else None,
+          rand(T, 10, 1e-4, 1e-2) if "q" in kind else None)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [1, 5, 300, 2048, 2049, 20001])
+def test_equal_logits(dtype, V):
+    # every weight is 1: the borders are hit exactly, the lowest indices are kept
+    T = 16
+    z = torch.full((T, V), -3.25, dtype=dtype, device=DEV)
+    u = torch.tensor([0.0, 0.25, 0.5, 0.75] * 4, device=DEV)
+    check(z, u)
+    k = torch.full((T,), max(1, V // 2), dtype=torch.int32, device=DEV)
+    check(z, u, k=k)
+    p = torch.tensor([0.5] * 8 + [0.25] * 8, device=DEV)
+    check(z, u, p=p)
+    check(z, u, k=k, p=p, q=torch.ones(T, device=DEV))
+
+
+def test_few_values():
+    # ties at the border of top-k and of top-p, over many tokens, and signed zeros among them
+    g = torch.Generator().manual_seed(3)
+    T, V = 24, 9001
+    z = torch.randint(-2, 3, (T, V), generator=g).float()
+    z[z == 0] = -0.0
+    z[:, ::2] += 0.0
+    z = z.to(DEV)
+    for k, p in ((ints(T, 1, 2, 9000), None), (None, rand(T, 2, 0.1, 0.99)),
+                 (ints(T, 3, 2, 9000), rand(T, 4, 0.1, 0.99))):
+        check(z, rand(T, 5), None, k, p)
+        check(z.to(BF), rand(T, 6), rand(T, 7, 0.5, 2.0), k, p)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_masks_and_special_values(dtype):
+    T, V = 12, 5003
+    low = torch.finfo(dtype).min
+    z = logits(T, V, 11, dtype)
+    z[0] = -math.inf                      # nothing is left
+    z[1] = math.nan
+    z[2, :] = -math.inf
+    z[2, 4001] = -70.0                    # one token is left
+    z[3, ::2] = -math.inf
+    z[4, 100:] = math.nan
+    z[5, ::3] = low                       # a mask of the type's lowest value
+    z[6, :] = low                         # and nothing else: all are equal
+    z[7, 17] = math.inf
+    z[7, 4000] = math.inf
+    z[8, :] = -math.inf
+    z[8, 30:33] = low                     # masked both ways
+    z[9, :1000] = -math.inf
+    z[9, 1000:] = -1e30
+    z[10, 5] = 1e30
+    u = rand(T, 12)
+    check(z, u)
+    check(z, u, rand(T, 13, 0.5, 2.0), ints(T, 14, 2, 50))
+    check(z, u, None, None, rand(T, 15, 0.5, 0.99))
+    check(z, u, None, None, None, rand(T, 16, 0.01, 0.5))
+    check(z, u, None, ints(T, 17, 3000, 5002), rand(T, 18, 0.5, 0.99), rand(T, 19, 1e-6, 1e-3))
+    check(z, u, torch.zeros(T, device=DEV))
+
+
+def test_settings_that_leave_a_filter_off():
+    T, V = 8, 3001
+    z, u = logits(T, V, 20), rand(T, 21)
+    want = S.sample(z, u)
+    f = torch.tensor([1.0, 1.5, math.nan, math.inf] * 2, device=DEV)
+    i = torch.tensor([0, -1, V, V + 7, 2 ** 31 - 1, -2 ** 31, 0, 0], dtype=torch.int32, device=DEV)
+    q = torch.tensor([0.0, -1.0, math.nan, -math.inf] * 2, device=DEV)
+    for kw in (dict(top_p=f), dict(top_k=i), dict(min_p=q), dict(top_p=f, top_k=i, min_p=q)):
+        got = S.sample(z, u, **kw)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), kw
+
+
+def test_greedy_forms():
+    T, V = 10, 40009
+    z = torch.round(logits(T, V, 22, spread=1.0, hot=False) * 2)    # (many equal largest ones)
+    want = torch.from_numpy(np.argmax(z.cpu().numpy(), 1).astype(np.int32))
+    u = rand(T, 23)
+    for kw in (dict(temperature=torch.zeros(T, device=DEV)),
+               dict(temperature=torch.full((T,), -1.0, device=DEV)),
+               dict(temperature=torch.full((T,), math.nan, device=DEV)),
+               dict(top_k=torch.ones(T, dtype=torch.int32, device=DEV)),
+               dict(top_p=torch.zeros(T, device=DEV)),
+               dict(top_p=torch.full((T,), -0.5, device=DEV))):
+        tok, lp = S.sample(z, u, **kw)
+        assert torch.equal(tok.cpu(), want) and bool((lp == 0).all()), kw
+
+
+def test_far_temperatures():
+    T, V = 8, 20011
+    z, u = logits(T, V, 24), rand(T, 25)
+    for t in (1e-30, 1e-3, 50.0, 1e30, math.inf):
+        t = torch.full((T,), t, device=DEV)
+        check(z, u, t)
+        check(z, u, t, ints(T, 26, 2, 100), rand(T, 27, 0.3, 0.95))
+        check(z, u, t, None, rand(T, 28, 0.3, 0.95))
+
+
+def test_ends_of_the_random_numbers():
+    T, V = 8, 10007
+    z = logits(T, V, 29)
+    z[:, -40:] = -math.inf
+    z[:, :40] = -math.inf
+    u = torch.tensor([0.0, 1 - 2.0 ** -24, 1.0, 2.0, -1.0, math.nan, math.inf, 1e-30], device=DEV)
+    check(z, u)
+    check(z, u, None, ints(T, 30, 3, 60), rand(T, 31, 0.5, 0.9))
+    check(z, u, None, ints(T, 32, 3000, 6000))
+    check(z, u, None, None, None, rand(T, 33, 0.01, 0.1))
+
+
+def test_shares_of_the_draws():
+    # a grid of random numbers over one row: every token is drawn as often as its share, within the
+    # two grid points at its borders
+    V, N = 50, 20000
+    z = logits(1, V, 34, spread=1.0, hot=False).expand(N, V)
+    with pytest.raises(ValueError):
+        S.sample(z, rand(N, 0))                                    # (rows of stride 0)
+    z = z.contiguous()
+    u = ((torch.arange(N, dtype=torch.float64) + 0.5) / N).float().to(DEV)
+    k = torch.full((N,), 20, dtype=torch.int32, device=DEV)
+    tok, lp = S.sample(z, u, top_k=k)
+    n = torch.bincount(tok.long(), minlength=V).cpu().double() / N
+    w = z[0].double().cpu().exp()
+    w[torch.argsort(w, descending=True)[20:]] = 0
+    w /= w.sum()
+    assert float((n - w).abs().max()) <= 2.0 / N
+    assert float((lp.cpu().double() - w.log()[tok.cpu().long()]).abs().max()) <= 1e-6
+
+
+def test_long_rows_far_apart():
+    # the last row starts beyond 2^32 elements
+    V, stride = 1009, 1 << 30
+    buf = torch.empty(4 * stride + V, dtype=BF, device=DEV)
+    z = buf.as_strided((5, V), (stride, 1))
+    z.copy_(logits(5, V, 35, BF))
+    check(z, rand(5, 36))
+    check(z, rand(5, 37), None, ints(5, 38, 2, 9), rand(5, 39, 0.4, 0.9))
+
+
+def test_many_rows_and_repeated_calls_are_equal():
+    T, V = 3001, 517
+    z, u = logits(T, V, 40, BF, pad=2), rand(T, 41)
+    kw = dict(temperature=rand(T, 42, 0.5, 1.5), top_k=ints(T, 43, 0, 300), top_p=rand(T, 44, 0.4, 1.2),
+              min_p=rand(T, 45, -0.1, 0.1))
+    a = S.sample(z, u, **kw)
+    check(z, u, kw["temperature"], kw["top_k"], kw["top_p"], kw["min_p"], got=a)
+    T, V = 64, 90001
+    z, u = logits(T, V, 46, spread=1.0, hot=False), rand(T, 47)
+    p = rand(T, 48, 0.5, 0.99)
+    a, b = S.sample(z, u, top_p=p), S.sample(z, u, top_p=p)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_no_rows_and_given_outputs():
+    tok, lp = S.sample(torch.zeros((0, 5), device=DEV), torch.zeros(0, device=DEV))
+    assert tok.shape == lp.shape == (0,) and tok.dtype == torch.int32 and lp.dtype == F32
+    z, u = logits(4, 100, 49), rand(4, 50)
+    tok, lp = torch.empty(4, dtype=torch.int32, device=DEV), torch.empty(4, device=DEV)
+    out = S.sample(z, u, tokens=tok, logprobs=lp)
+    assert out[0] is tok and out[1] is lp
+    check(z, u, got=out)
+
+
+def test_wrapper_refusals():
+    z, u = logits(4, 100, 51), rand(4, 52)
+    k = ints(4, 53, 1, 9)
+
+    def bad(*a, **kw):
+        with pytest.raises((ValueError, RuntimeError)):
+            S.sample(*a, **kw)
+    bad(z.double(), u)
+    bad(z.half(), u)
+    bad(z[0], u)
+    bad(z[:, ::2], u)
+    bad(z.t().contiguous().t(), u)
+    bad(z[:, :0], u)
+    bad(z, u[:3])
+    bad(z, u.double())
+    bad(z, u.cpu())
+    bad(z, u, temperature=u.double())
+    bad(z, u, temperature=u[:2])
+    bad(z, u, top_k=k.long())
+    bad(z, u, top_k=k.cpu())
+    bad(z, u, top_p=u.to(BF))
+    bad(z, u, min_p=0.1 * u[:, None])
+    bad(z, u, tokens=k.long())
+    bad(z, u, logprobs=u.double())
+    bad(z, u, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    bad(torch.zeros((1, S.SPARROW_SAMPLE_MAX_VOCAB + 1), device=DEV), u[:1])
+
+
+def test_side_stream_and_graph_replays():
+    T, V = 20, 30011
+    z, u = logits(T, V, 54, BF, pad=1), rand(T, 55)
+    kw = dict(temperature=rand(T, 56, 0.5, 1.5), top_k=ints(T, 57, 0, 300), top_p=rand(T, 58, 0.4, 1.2))
+    want = S.sample(z, u, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    ws = torch.empty(S.sparrow_sample_workspace_size(T, V, S.SPARROW_LOGITS_BF16), dtype=torch.uint8,
+                     device=DEV)
+    outs = [torch.zeros_like(t) for t in want]
+    with torch.cuda.stream(side):
+        a = S.sample(z, u, **kw)
+        assert all(torch.equal(x, y) for x, y in zip(a, want))
+        with torch.cuda.graph(graph, stream=side):
+            S.sample(z, u, **kw, tokens=outs[0], logprobs=outs[1], workspace=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    for rep in range(3):
+        if rep == 2:                                               # other numbers, the same graph
+            u.copy_(rand(T, 59))
+            want = S.sample(z, u, **kw)
+        for o in outs:
+            o.fill_(7)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want)), rep
+
+
+def test_two_calls_at_once():
+    T, V = 64, 151936
+    z, u = [logits(T, V, 60 + i) for i in range(2)], rand(T, 61)
+    p = rand(T, 62, 0.5, 0.95)
+    want = [S.sample(x, u, top_p=p) for x in z]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(S.sample(z[i], u, top_p=p))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(x, y) for x, y in zip(g, want[i]))
