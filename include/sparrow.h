@@ -345,6 +345,43 @@ int sparrow_dense_decode_attn(const sparrow_shape_t *shape, const void *q, const
                               void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * Dense decode attention for sequences in groups whose first tokens are the same - the samples of one
+ * prompt - with the shared pages read once per group instead of once per sequence.
+ *
+ * Group g holds the sequences cu_groups[g] .. cu_groups[g+1] - 1 and shares the s = prefix_lens[g] /
+ * page_size whole pages (rounded down) at the start of its sequences: token t < s * page_size of each is read
+ * from the pages that the block-table row of the group's FIRST sequence lists, whatever that
+ * sequence's own length; the sequences' other tokens from their own rows, whose first s entries are
+ * not read.  (A prompt that ends inside a page leaves its last tokens in every sequence's own copy of
+ * that page.)  A sequence shorter than the prefix attends to its own seq_lens[b] tokens of it.
+ * Groups of one sequence, and sequences in no group, share nothing.  With that the result is
+ * sparrow_dense_decode_attn's,
+ *     out[b][j] = sum_t w_t V[t],  w = softmax(scale * q[b][j] . K[t]) over t < seq_lens[b]
+ * with fp32 sums; the softmax numerators enter the product with V as bf16 for SPARROW_OUT_BF16 and
+ * with all of their 24 bits for SPARROW_OUT_F32.  An empty sequence gives a zero row.  The order of the
+ * sums depends only on the shape, the groups, the lengths and the device.
+ *
+ * Arguments: as for sparrow_dense_decode_attn, batch * num_kv_heads <= 65535; 0 <= num_groups <=
+ * SPARROW_MAX_GROUPS; cu_groups (device int32 [num_groups + 1], non-decreasing; entries outside [0,
+ * batch] count as the nearer end, one below an earlier entry as that one), prefix_lens (device int32
+ * [num_groups]; what the block table cannot hold, or is negative, counts as the nearer end), both
+ * NULL allowed without groups; scale finite; workspace of at least
+ * sparrow_shared_prefix_workspace_size(shape, num_groups) bytes.
+ * Errors: SPARROW_EINVAL, SPARROW_EUNSUPPORTED, SPARROW_EWORKSPACE, SPARROW_EHIP.
+ */
+#define SPARROW_MAX_GROUPS 4096
+int sparrow_shared_prefix_decode_attn(const sparrow_shape_t *shape, const void *q,
+                                      const void *k_cache, const void *v_cache,
+                                      const int32_t *block_table, const int32_t *seq_lens,
+                                      int32_t num_groups, const int32_t *cu_groups,
+                                      const int32_t *prefix_lens, float scale, void *out,
+                                      int32_t out_dtype, void *workspace, size_t ws_bytes,
+                                      void *stream);
+
+/* Workspace bytes of sparrow_shared_prefix_decode_attn; 0 for a shape that it refuses. */
+size_t sparrow_shared_prefix_workspace_size(const sparrow_shape_t *shape, int32_t num_groups);
+
+/*
  * Per-token acceptance rate between the dense policy and the sparse rollout
  * (Sec. 3.1, Eq. 1: the expectation under the draft of min(p/q, 1), which equals
  * the sum over the vocabulary of min(p(x), q(x))).

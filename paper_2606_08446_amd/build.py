@@ -22,7 +22,7 @@ LIB = os.path.join(PKG, "libsparrow.so")
 SOURCES = ["api.hip", "meta.hip", "append.hip", "score_topk.hip", "attention.hip",
            "acceptance.hip", "measure.hip", "qk_norm_rope.hip",
            "cache_e4m3.hip", "attention_e4m3.hip", "residual_norm.hip",
-           "sample.hip"]
+           "sample.hip", "attention_shared.hip"]
 ARCH = "gfx950"
 # Packed fp32 VALU ops are switched off for every device compile.
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

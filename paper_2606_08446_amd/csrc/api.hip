@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "attention_e4m3.h"
+#include "attention_shared.h"
 #include "cache_e4m3.h"
 #include "common.h"
 #include "qk_norm_rope.h"
@@ -429,6 +430,47 @@ int sparrow_decode_step(const sparrow_shape_t *shape, const void *q, const void 
     return status_of(launch_attention(*shape, plan_attention(*shape), q, k_cache, v_cache,
                                       block_table, seq_lens, out_k, out_idx, k_max, scale, out,
                                       out_dtype, attn_ws, st));
+}
+
+int sparrow_shared_prefix_decode_attn(const sparrow_shape_t *shape, const void *q,
+                                      const void *k_cache, const void *v_cache,
+                                      const int32_t *block_table, const int32_t *seq_lens,
+                                      int32_t num_groups, const int32_t *cu_groups,
+                                      const int32_t *prefix_lens, float scale, void *out,
+                                      int32_t out_dtype, void *workspace, size_t ws_bytes,
+                                      void *stream)
+{
+    const int rc = check_shape(shape);
+    if (rc != SPARROW_OK)
+        return rc;
+    if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !out || num_groups < 0 ||
+        (num_groups > 0 && (!cu_groups || !prefix_lens)) || !std::isfinite(scale))
+        return SPARROW_EINVAL;
+    if (!al16(q) || !al16(k_cache) || !al16(v_cache) || !al4(block_table) || !al4(seq_lens) ||
+        !al4(cu_groups) || !al4(prefix_lens) || !al16(out) || !al16(workspace))
+        return SPARROW_EINVAL;
+    if (out_dtype != SPARROW_OUT_F32 && out_dtype != SPARROW_OUT_BF16)
+        return SPARROW_EUNSUPPORTED;
+    if (shape->batch == 0)
+        return SPARROW_OK;
+    if ((int64_t)shape->batch * shape->num_kv_heads > 65535)
+        return SPARROW_EINVAL;
+    if (shape->batch > kMaxBatch || num_groups > kMaxGroups)
+        return SPARROW_EUNSUPPORTED;
+    if (!workspace || ws_bytes < shared_attention_workspace(*shape, num_groups))
+        return SPARROW_EWORKSPACE;
+    const Groups g{cu_groups, prefix_lens, num_groups};
+    return status_of(launch_shared_attention(*shape, g, q, k_cache, v_cache, block_table, seq_lens,
+                                             scale, out, out_dtype, workspace,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+size_t sparrow_shared_prefix_workspace_size(const sparrow_shape_t *shape, int32_t num_groups)
+{
+    if (check_shape(shape) != SPARROW_OK || shape->batch > kMaxBatch || num_groups < 0 ||
+        num_groups > kMaxGroups || (int64_t)shape->batch * shape->num_kv_heads > 65535)
+        return 0;
+    return shared_attention_workspace(*shape, num_groups);
 }
 
 int sparrow_acceptance_rate(int64_t num_tokens, int32_t vocab, int32_t logits_dtype,

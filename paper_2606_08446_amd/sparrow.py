@@ -45,6 +45,7 @@ SPARROW_OP_DECODE_STEP = 3
 SPARROW_NOALLOC_SCRATCH_BYTES = 32 << 20
 SPARROW_ROPE_WORKSPACE_BYTES = 1 << 20
 SPARROW_SAMPLE_MAX_VOCAB = 524288
+SPARROW_MAX_GROUPS = 4096
 
 EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_topk",
            "sparrow_append_score_topk", "sparrow_sparse_decode_attn", "sparrow_dense_decode_attn",
@@ -54,6 +55,7 @@ EXPORTS = ("sparrow_page_meta_update", "sparrow_append_kv", "sparrow_page_score_
            "sparrow_read_kv_e4m3", "sparrow_sparse_decode_attn_e4m3",
            "sparrow_dense_decode_attn_e4m3", "sparrow_residual_norm", "sparrow_residual_norm_bwd",
            "sparrow_residual_norm_workspace_size", "sparrow_sample", "sparrow_sample_workspace_size",
+           "sparrow_shared_prefix_decode_attn", "sparrow_shared_prefix_workspace_size",
            "sparrow_budget_bound", "sparrow_workspace_size", "sparrow_status_string")
 
 
@@ -139,8 +141,13 @@ def load():
                                               ctypes.c_size_t, _p]
     lib.sparrow_sample.argtypes = [ctypes.c_int64, _i32, _i32, _p, ctypes.c_int64, _p, _p, _p, _p,
                                    _p, _p, _p, _p, ctypes.c_size_t, _p]
+    lib.sparrow_shared_prefix_decode_attn.argtypes = [sp, _p, _p, _p, _p, _p, _i32, _p, _p,
+                                                      ctypes.c_float, _p, _i32, _p,
+                                                      ctypes.c_size_t, _p]
     for fn in EXPORTS[:-3]:
         getattr(lib, fn).restype = ctypes.c_int
+    lib.sparrow_shared_prefix_workspace_size.argtypes = [sp, _i32]
+    lib.sparrow_shared_prefix_workspace_size.restype = ctypes.c_size_t
     lib.sparrow_sample_workspace_size.argtypes = [ctypes.c_int64, _i32, _i32]
     lib.sparrow_sample_workspace_size.restype = ctypes.c_size_t
     lib.sparrow_residual_norm_workspace_size.argtypes = [ctypes.c_int64, _i32]
@@ -210,6 +217,19 @@ def sparrow_dense_decode_attn(shape, q, k_cache, v_cache, block_table, seq_lens,
     return load().sparrow_dense_decode_attn(ctypes.byref(shape), q, k_cache, v_cache,
                                             block_table, seq_lens, scale, out, out_dtype,
                                             workspace, ws_bytes, stream)
+
+
+def sparrow_shared_prefix_decode_attn(shape, q, k_cache, v_cache, block_table, seq_lens, num_groups,
+                                      cu_groups, prefix_lens, scale, out, out_dtype, workspace,
+                                      ws_bytes, stream):
+    return load().sparrow_shared_prefix_decode_attn(ctypes.byref(shape), q, k_cache, v_cache,
+                                                    block_table, seq_lens, num_groups, cu_groups,
+                                                    prefix_lens, scale, out, out_dtype, workspace,
+                                                    ws_bytes, stream)
+
+
+def sparrow_shared_prefix_workspace_size(shape, num_groups) -> int:
+    return int(load().sparrow_shared_prefix_workspace_size(ctypes.byref(shape), num_groups))
 
 
 def sparrow_acceptance_rate(num_tokens, vocab, logits_dtype, target, draft, inv_temperature,
@@ -641,6 +661,36 @@ def dense_decode_attn(q, k_cache, v_cache, block_table, seq_lens, scale=None, ou
                                    workspace.numel() * workspace.element_size(),
                                    _stream(q.device))
     _check("sparrow_dense_decode_attn", rc)
+    return out
+
+
+def shared_prefix_decode_attn(q, k_cache, v_cache, block_table, seq_lens, cu_groups, prefix_lens,
+                              scale=None, out=None, out_dtype=SPARROW_OUT_F32, workspace=None):
+    """Dense paged decode attention for groups of sequences with the same first tokens.  Group g is the
+    sequences ``cu_groups[g] .. cu_groups[g+1]-1`` (int32 ``[groups + 1]``) and shares the whole pages of
+    its ``prefix_lens[g]`` first tokens (int32 ``[groups]``), which are read once, from the pages of its
+    first sequence.  Returns out [B][Hq][D] (fp32 or bf16)."""
+    import torch
+    B, Hq, Hkv, ps, D, P, M = _expect_cache(q, k_cache, v_cache, block_table, seq_lens)
+    if prefix_lens.dim() != 1:
+        raise ValueError("prefix_lens must be [groups]")
+    dev, n = q.device, prefix_lens.shape[0]
+    _expect(cu_groups, "cu_groups", torch.int32, (n + 1,), dev)
+    _expect(prefix_lens, "prefix_lens", torch.int32, (n,), dev)
+    if out_dtype not in (SPARROW_OUT_F32, SPARROW_OUT_BF16):
+        raise ValueError(f"out_dtype: {out_dtype}, expected SPARROW_OUT_F32 or SPARROW_OUT_BF16")
+    out = _given(out, "out", torch.float32 if out_dtype == SPARROW_OUT_F32 else torch.bfloat16,
+                 (B, Hq, D), dev)
+    if B == 0:
+        return out
+    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    shape = make_shape(B, Hq, Hkv, ps, M, P, D)
+    workspace = _given_workspace(workspace, None if workspace is not None else
+                                 sparrow_shared_prefix_workspace_size(shape, n), dev)
+    _launch("sparrow_shared_prefix_decode_attn", dev, ctypes.byref(shape), q.data_ptr(),
+            k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), n,
+            _ptr(cu_groups) if n else None, _ptr(prefix_lens) if n else None, scale, out.data_ptr(),
+            int(out_dtype), workspace.data_ptr(), workspace.nbytes)
     return out
 
 
