@@ -5,16 +5,15 @@
 //   z_t = scale q . K[t],  m = max z,  l = sum e^(z - m),  o = sum e^(z - m) V[t]   of each part,
 //   out = sum o e^(m - M) / sum l e^(m - M),  M the largest m.
 //
-// Work split.  Query rows are taken 16 at a time: a group has (group, KV head, row block) units over its
-// shared tokens, a sequence one unit per KV head over its own.  All units' 32-token tiles are laid
-// end to end and every wave takes one equal, contiguous range of them.  A group's units are cut into
-// segments of as many tiles as a wave takes and laid out segment by segment, row block by row block
-// inside: neighbouring waves, which run side by side on one compute unit, then go through the same
-// tiles for different rows at the same time, and the tiles come from memory once.  Each part of a
-// segment or unit that a wave finds in its range leaves (m, l, o) in the workspace, in slot wave + a
-// number that grows along the order; k_shared_merge joins what belongs to a query head.
+// Work split.  A group has (group, KV head, block of 64 query rows) units over its shared tokens, a sequence
+// one unit per KV head over its own.  The groups' units are laid end to end in 32-token tiles and a part of
+// the workgroups takes an equal, contiguous range of them each; so are the sequences' for the waves of the
+// other workgroups.  Each part of a unit that falls into a range leaves (m, l, o) in the workspace, in a
+// slot that grows along the order; k_shared_merge joins what belongs to a query head.
 //
-// Per 32-token tile a wave reads K and V straight into MFMA operands:
+// A workgroup on a group's tiles (Team) brings each tile into LDS once, a fourth of it per wave, three
+// tiles ahead in registers, and every wave attends with 16 of the rows.  A wave on a sequence's (Stream)
+// reads its tiles straight into MFMA operands, the next one always under way.  Per tile and 16 rows:
 //   logits  D[t][row] = sum_d K[t][d] q[row][d]  - 2 x 4 x mfma_f32_16x16x32_bf16: lane (row lr, lg)
 //           then holds tokens 4 lg .. 4 lg + 3 of both halves;
 //   O^T[d][row] += sum_t V[t][d] p[t][row]       - 8 x mfma_f32_16x16x32_bf16, whose 32 terms are
@@ -36,7 +35,8 @@ namespace {
 constexpr int kSharedThreads = 256;
 constexpr int kSharedWaves = kSharedThreads / 64;
 constexpr int kTileTokens = 32;
-constexpr int kRows = 16;  // query rows of a unit at most
+constexpr int kRows = 16;       // query rows of a wave
+constexpr int kTeamRows = kRows * kSharedWaves;
 constexpr float kNoLogit = -FLT_MAX;  // a part's maximum before its first token
 
 struct SharedArgs {
@@ -44,89 +44,77 @@ struct SharedArgs {
     const int32_t *block_table, *seq_lens, *cu_groups, *prefix_lens;
     int32_t *plan_off;   // [groups + batch + 1] positions before each entry, groups' first
     int32_t *seq_group;  // [batch] its group, -1: none
-    int32_t *plan_waves; // [2] waves of the groups, of the sequences
+    int32_t *plan_takers; // [2] workgroups of the groups, waves of the sequences
     int32_t *plan_cu;    // [groups + 1] the groups' first sequences as the plan took them
-    float *o_group, *ml_group;  // [slots][kRows] rows
+    float *o_group, *ml_group;  // [slots][kRows] rows: a slot for each 16 rows of a part
     float *o_seq, *ml_seq;      // [slots][G] rows
     void *out;
     int64_t num_phys;
     int groups, batch, num_q_heads, num_kv_heads, ps, ps_log2, max_pages, out_bf16;
-    int max_waves, min_tiles;
+    int min_tiles;
     int step_log2;  // a position is 2^step_log2 tiles (more than one only where 2^31 would not do)
     float scale_log2;
 };
 
-// Which of the launch's waves take the groups' positions (P1 of them) and which the sequences' (P2): all of
-// them in proportion, in whole workgroups, or where that would be less than min_tiles each, fewer.
+// How many workgroups take the groups' positions (P1 of them) and how many waves the sequences' (P2): all of
+// the launch's, or where that would be less than min_tiles each, fewer.  A workgroup on a group has half the
+// bytes under way that four waves on sequences have, so its positions count double.
 struct Sides {
     uint32_t w1, w2;
-    __device__ __forceinline__ Sides(const SharedArgs &a, uint32_t P1, uint32_t P2, uint32_t waves)
+    __device__ __forceinline__ Sides(const SharedArgs &a, uint32_t P1, uint32_t P2, uint32_t blocks)
     {
         w1 = (P1 + a.min_tiles - 1) / a.min_tiles;
         w2 = (P2 + a.min_tiles - 1) / a.min_tiles;
-        const uint32_t blocks = waves / kSharedWaves;
-        if ((w1 + kSharedWaves - 1) / kSharedWaves + (w2 + kSharedWaves - 1) / kSharedWaves > blocks) {
-            const float part = (float)P1 / ((float)P1 + (float)P2);
-            uint32_t n = (uint32_t)(part * blocks + 0.5f);
+        if (w1 + (w2 + kSharedWaves - 1) / kSharedWaves > blocks) {
+            const float c1 = 2.f * (float)P1;
+            uint32_t n = (uint32_t)(c1 / (c1 + (float)P2) * blocks + 0.5f);
             n = P1 ? max(n, 1u) : 0u;
             n = P2 ? min(n, blocks - 1) : blocks;
-            w1 = min(w1, n * kSharedWaves);
+            w1 = min(w1, n);
             w2 = min(w2, (blocks - n) * kSharedWaves);
         }
     }
 };
 
-// One side's positions shared out over W waves: the first r take q + 1 of them, the others q.
+// One side's positions shared out over W takers: the first r take q + 1 of them, the others q.
 struct Share {
     uint32_t W, q, r;
-    __device__ __forceinline__ Share(uint32_t P, uint32_t waves) : W(waves)
+    __device__ __forceinline__ Share(uint32_t P, uint32_t takers) : W(takers)
     {
         q = W ? P / W : 1;
         r = P - W * q;
     }
     __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * q + min(w, r); }
-    __device__ __forceinline__ uint32_t wave_of(uint32_t pos) const
+    __device__ __forceinline__ uint32_t taker_of(uint32_t pos) const
     {
         const uint32_t big = r * (q + 1);
         return pos < big ? pos / (q + 1) : r + (pos - big) / q;
     }
-    // positions of a segment: what a wave takes at most
-    __device__ __forceinline__ uint32_t segment() const { return q + (r ? 1 : 0); }
 };
 
-// One segment's row block: where it lies, and a number for its slots that grows along the order (whole
-// segments count by their positions, a unit's last one by its row block).
-struct Segment {
-    uint32_t pos, len, number;
-};
-
-// Segment `seg` (of `size` positions) of row block rb, of a group's KV head; begin: the group's first
-// sequence, first: its first position, unit: positions of one of its units.
-__device__ __forceinline__ Segment segment_at(const SharedArgs &a, int g, int begin, uint32_t first,
-                                              uint32_t unit, uint32_t blocks, uint32_t size, int h,
-                                              uint32_t seg, uint32_t rb)
+// Row blocks of 16 of the units before one of a group that begins with sequence `begin`, in steps that leave
+// room for each group's (at most begin * G / kRows + g of them for a KV head).
+__device__ __forceinline__ uint32_t blocks_before(const SharedArgs &a, int g, int begin, int rows, int h,
+                                                  int row0)
 {
     const int G = a.num_q_heads / a.num_kv_heads;
-    const uint32_t at = seg * size;
-    const bool last = unit - at <= size;
-    Segment s;
-    s.len = last ? unit - at : size;
-    s.pos = first + (h * unit + at) * blocks + rb * s.len;
-    // (row blocks of the groups before: at most begin * G / kRows + g)
-    s.number = s.pos / size + a.num_kv_heads * (begin * G / kRows + g) + h * blocks + (last ? rb : 0);
-    return s;
+    return a.num_kv_heads * (begin * G / kRows + g) + h * ((rows + kRows - 1) / kRows) + row0 / kRows;
 }
 
 // LDS of a workgroup's plan: the positions before each entry (groups, then sequences), each sequence's first
-// own page with its own positions, each group's shared tokens, first sequence and shared pages.
+// own page with its own positions, each group's shared tokens and first sequence.
 struct Plan {
-    int32_t *off, *seq, *lim, *cu, *pages;
+    int32_t *off, *seq, *lim, *cu;
     __device__ __forceinline__ Plan(int32_t *lds, const SharedArgs &a)
-        : off(lds), seq(off + a.groups + a.batch + 1), lim(seq + a.batch), cu(lim + a.groups),
-          pages(cu + a.groups + 1)
+        : off(lds), seq(off + a.groups + a.batch + 1), lim(seq + a.batch), cu(lim + a.groups)
     {
     }
 };
+
+constexpr size_t plan_lds(size_t batch, size_t groups)
+{
+    return sizeof(int32_t) * (3 * groups + 2 * batch + 2);
+}
 
 // seq entries: own positions (16 bits) under the first own page.
 constexpr int kSeqTileBits = 16;
@@ -140,14 +128,15 @@ __device__ __forceinline__ int positions_of(const SharedArgs &a, int tokens)
 }
 static_assert(kTileTokens == 1 << 5, "positions_of");
 
-__device__ void make_plan(const SharedArgs &a, const Plan &p, int32_t *s_tmp)
+// pages: LDS of the groups' size, scratch.
+__device__ void make_plan(const SharedArgs &a, const Plan &p, int32_t *pages, int32_t *s_tmp)
 {
     const int tid = threadIdx.x;
     const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv;
     for (int g = tid; g <= a.groups; g += kSharedThreads) {
         p.cu[g] = a.groups ? min(max(a.cu_groups[g], 0), a.batch) : 0;
         if (g < a.groups) {
-            p.pages[g] = min(max(a.prefix_lens[g], 0) >> a.ps_log2, a.max_pages);
+            pages[g] = min(max(a.prefix_lens[g], 0) >> a.ps_log2, a.max_pages);
             p.lim[g] = 0;
         }
     }
@@ -176,7 +165,7 @@ __device__ void make_plan(const SharedArgs &a, const Plan &p, int32_t *s_tmp)
         int first = 0, group = -1;
         if (a.groups && p.cu[lo] <= b && b < p.cu[lo + 1] && p.cu[lo + 1] - p.cu[lo] > 1) {
             group = lo;
-            first = p.pages[lo];
+            first = pages[lo];
             atomicMax(&p.lim[lo], min(L, first << a.ps_log2));
         }
         p.seq[b] = first << kSeqTileBits | positions_of(a, max(0, L - (first << a.ps_log2)));
@@ -189,7 +178,8 @@ __device__ void make_plan(const SharedArgs &a, const Plan &p, int32_t *s_tmp)
     auto positions = [&](int e) -> int {
         if (e >= a.groups)
             return Hkv * (p.seq[e - a.groups] & ((1 << kSeqTileBits) - 1));
-        return Hkv * positions_of(a, p.lim[e]) * (((p.cu[e + 1] - p.cu[e]) * G + kRows - 1) / kRows);
+        return Hkv * positions_of(a, p.lim[e]) *
+               (((p.cu[e + 1] - p.cu[e]) * G + kTeamRows - 1) / kTeamRows);
     };
     const int per = (n + kSharedThreads - 1) / kSharedThreads;
     const int e0 = min(n, tid * per), e1 = min(n, e0 + per);
@@ -223,26 +213,23 @@ struct Half {
     u32x4_t k[4], v[4];
 };
 
-// kOnce: streamed past the caches.
-template <bool kOnce>
 __device__ __forceinline__ void load_half(Half &c, const uint16_t *kbase, const uint16_t *vbase, int lr,
                                           int lg)
 {
     const uint16_t *kp = kbase + lr * kHeadDim + 8 * lg;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        c.k[i] = kOnce ? ld16_nt(kp + 32 * i) : ld16(kp + 32 * i);
+        c.k[i] = ld16_nt(kp + 32 * i);
     const uint16_t *vp = vbase + 4 * lg * kHeadDim + 8 * lr;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        c.v[j] = kOnce ? ld16_nt(vp + j * kHeadDim) : ld16(vp + j * kHeadDim);
+        c.v[j] = ld16_nt(vp + j * kHeadDim);
 }
 
 struct Tile {
     Half h[2];
     int tok;        // its first token
     bool live[2];   // a half inside the unit's tokens, on a page that is there
-    bool first, last;  // of its part
 };
 
 // The last of n entries whose positions begin at or before pos (empty ones share their place).
@@ -260,36 +247,34 @@ __device__ __forceinline__ int entry_at(const int32_t *off, int n, uint32_t pos)
     return __builtin_amdgcn_readfirstlane(e);
 }
 
-// A wave's part of a unit.
+// A taker's part of a unit.
 struct Part {
     const int32_t *table;  // the block-table row that its pages are read from
     int h, lim;            // KV head; its tokens end here
-    int rows, row0;        // query rows of this block, and the first one's number in its entry
+    int rows, row0;        // query rows of this unit, and the first one's number in its entry
     int b0;                // the entry's first sequence
     uint32_t slot;
-    int tok, tiles;        // its first token, its tiles that are left to load
+    int tok, tiles;        // its first token, its tiles
 };
 
-// The parts of a wave's range, one after another.
+// The parts of a range, one after another.
+template <bool kTeam>
 struct Walk {
     const SharedArgs &a;
     const Plan &plan;
-    const bool shared;
     const int w, Hkv, G;
     const int32_t *off;
-    uint32_t size, pos, end;
+    uint32_t pos, end;
     int e;
 
-    __device__ __forceinline__ Walk(const SharedArgs &args, const Plan &p, bool shared_, int w_,
-                                    const Share &s)
-        : a(args), plan(p), shared(shared_), w(w_), Hkv(args.num_kv_heads),
-          G(args.num_q_heads / args.num_kv_heads), off(p.off + (shared_ ? 0 : args.groups))
+    __device__ __forceinline__ Walk(const SharedArgs &args, const Plan &p, int w_, const Share &s)
+        : a(args), plan(p), w(w_), Hkv(args.num_kv_heads), G(args.num_q_heads / args.num_kv_heads),
+          off(p.off + (kTeam ? 0 : args.groups))
     {
         const uint32_t before = __builtin_amdgcn_readfirstlane(off[0]);
-        size = s.segment();
         pos = before + s.begin(w);
         end = before + s.begin(w + 1);
-        e = entry_at(off, shared ? a.groups : a.batch, pos);
+        e = entry_at(off, kTeam ? a.groups : a.batch, pos);
     }
 
     __device__ __forceinline__ bool next(Part &u)
@@ -300,37 +285,34 @@ struct Walk {
             ++e;
         const uint32_t first = __builtin_amdgcn_readfirstlane(off[e]);
         const int step = kTileTokens << a.step_log2;
-        uint32_t at, left;
-        if (shared) {
+        uint32_t at, unit;
+        if (kTeam) {
             u.b0 = __builtin_amdgcn_readfirstlane(plan.cu[e]);
             u.lim = __builtin_amdgcn_readfirstlane(plan.lim[e]);
             const int rows = (__builtin_amdgcn_readfirstlane(plan.cu[e + 1]) - u.b0) * G;
-            const uint32_t blocks = (rows + kRows - 1) / kRows, unit = positions_of(a, u.lim);
-            u.h = (pos - first) / (unit * blocks);
-            at = pos - first - u.h * unit * blocks;
-            const uint32_t seg = at / (min(size, unit) * blocks);
-            at -= seg * size * blocks;
-            left = min(size, unit - seg * size);
-            const uint32_t rb = at / left;
-            at -= rb * left;
-            u.slot = w + segment_at(a, e, u.b0, first, unit, blocks, size, u.h, seg, rb).number;
-            u.row0 = rb * kRows;
-            u.rows = min(kRows, rows - u.row0);
-            u.tok = (int)(seg * size + at) * step;
+            const uint32_t blocks = (rows + kTeamRows - 1) / kTeamRows;
+            unit = positions_of(a, u.lim);
+            const uint32_t n = (pos - first) / unit;
+            at = pos - first - n * unit;
+            u.h = n / blocks;
+            u.row0 = (n - u.h * blocks) * kTeamRows;
+            u.rows = min(kTeamRows, rows - u.row0);
+            u.slot = w * kSharedWaves + blocks_before(a, e, u.b0, rows, u.h, u.row0);
+            u.tok = (int)at * step;
         } else {
             const int packed = __builtin_amdgcn_readfirstlane(plan.seq[e]);
-            left = packed & ((1 << kSeqTileBits) - 1);
+            unit = packed & ((1 << kSeqTileBits) - 1);
             u.b0 = e;
             u.lim = clamp_len(a.seq_lens[e], a.ps, a.max_pages);
-            u.h = (pos - first) / left;
-            at = pos - first - u.h * left;
+            u.h = (pos - first) / unit;
+            at = pos - first - u.h * unit;
             u.slot = w + e * Hkv + u.h;
             u.row0 = 0;
             u.rows = G;
             u.tok = (packed >> kSeqTileBits << a.ps_log2) + (int)at * step;
         }
         u.table = a.block_table + (int64_t)u.b0 * a.max_pages;
-        const uint32_t take = min(left - at, end - pos);
+        const uint32_t take = min(unit - at, end - pos);
         // (tiles of the last position may lie behind the unit's tokens)
         u.tiles = min((int)take << a.step_log2, (u.lim - u.tok + kTileTokens - 1) / kTileTokens);
         pos += take;
@@ -343,142 +325,91 @@ struct Walk {
 // 64 entries of a block-table row from `page0` on and the 64 behind them, one a lane.
 struct Window {
     int page0, phys, phys_next;
+
+    __device__ __forceinline__ static int entry(const SharedArgs &a, const Part &u, int page)
+    {
+        return page << a.ps_log2 < u.lim ? u.table[page] : -1;
+    }
+    __device__ __forceinline__ void begin(const SharedArgs &a, const Part &u, int lane)
+    {
+        page0 = u.tok >> a.ps_log2;
+        phys = entry(a, u, page0 + lane);
+        phys_next = entry(a, u, page0 + 64 + lane);
+    }
+    // Moves on to token `tok`, at most a window further than the one before.
+    __device__ __forceinline__ void reach(const SharedArgs &a, const Part &u, int tok, int lane)
+    {
+        if ((tok >> a.ps_log2) >= page0 + 64) {
+            page0 += 64;
+            phys = phys_next;
+            phys_next = entry(a, u, page0 + 64 + lane);
+        }
+    }
+    // Where the 16 tokens from `at` on lie in the caches, in elements; 0 and false: nowhere.
+    __device__ __forceinline__ int64_t place(const SharedArgs &a, const Part &u, int at, bool &live) const
+    {
+        const int ph = __builtin_amdgcn_readlane(phys, ((at >> a.ps_log2) - page0) & 63);
+        live = ph >= 0 && ph < a.num_phys && at < u.lim;
+        return live ? (((int64_t)ph * a.num_kv_heads + u.h) * a.ps + (at & (a.ps - 1))) * kHeadDim : 0;
+    }
 };
 
-// A wave's way through its parts: the loads of the next tile, the next part's first one too, are always
-// under way, and the next part's block-table entries with them.
+// A row's value over its four lanes (a row is in lanes lr, 16 + lr, 32 + lr, 48 + lr): swaps of 16-lane rows
+// and of halves with a copy, which leave a lane its own and its partner's.
+template <typename Op>
+__device__ __forceinline__ float over_groups(float x, Op op)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// 16 query rows of a part at work, by one wave.
 template <int kTerms>
-struct Streamer {
+struct Rows {
     const SharedArgs &a;
     const int lane, lr, lg, G;
-    Walk &walk;
-    Part load, next;  // the part whose tiles are being loaded, the one behind it
-    bool have_next;
-    Window win, win_next;
-    bf16x8_t q_load[4];  // the loaded part's query rows, tokens of their sequences
-    int len_load;
-    // ---- the part at work
     bf16x8_t q[4];
     int len;   // tokens of the row's sequence
     int full;  // tokens that every row has
     int lim, rows;
-    uint32_t slot;
     float m, l;
     f32x4_t O[8];
 
-    __device__ __forceinline__ Streamer(const SharedArgs &args, Walk &wk)
+    __device__ __forceinline__ Rows(const SharedArgs &args)
         : a(args), lane(threadIdx.x & 63), lr(lane & 15), lg(lane >> 4),
-          G(args.num_q_heads / args.num_kv_heads), walk(wk)
+          G(args.num_q_heads / args.num_kv_heads)
     {
-        load.tiles = 0;
-        have_next = walk.next(next);  // (a wave has a position at least)
-        window(next, win_next);
     }
 
-    __device__ __forceinline__ int entry(const Part &u, int page) const
+    // The query rows from row0 of the part on and the lengths of their sequences (lanes beyond its rows take
+    // the first one again: nothing is made of them).
+    __device__ __forceinline__ void load(const Part &u, int row0, bf16x8_t (&x)[4], int &tokens) const
     {
-        return page << a.ps_log2 < u.lim ? u.table[page] : -1;
-    }
-    __device__ __forceinline__ void window(const Part &u, Window &x) const
-    {
-        x.page0 = u.tok >> a.ps_log2;
-        x.phys = entry(u, x.page0 + lane);
-        x.phys_next = entry(u, x.page0 + 64 + lane);
-    }
-
-    // The loads of the next tile; false: there is none.  They are issued whatever the tile holds (from the
-    // cache's first page where there is none), so that the wait for an earlier tile can count the
-    // loads behind it.
-    __device__ __forceinline__ bool issue(Tile &t)
-    {
-        bool there = true;
-        t.first = load.tiles == 0;
-        if (t.first && have_next) {
-            load = next;
-            win = win_next;
-            // (lanes beyond the block's rows hold its first one again: nothing is made of them)
-            const bool in = lr < load.rows;
-            const int r = load.row0 + (in ? lr : 0), b = load.b0 + r / G, j = r % G;
-            const uint16_t *row = a.q + ((int64_t)b * a.num_q_heads + load.h * G + j) * kHeadDim + 8 * lg;
+        const int at = row0 + lr < u.rows ? row0 + lr : 0;
+        const int r = u.row0 + at, b = u.b0 + r / G, j = r % G;
+        const uint16_t *row = a.q + ((int64_t)b * a.num_q_heads + u.h * G + j) * kHeadDim + 8 * lg;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                q_load[i] = __builtin_bit_cast(bf16x8_t, ld16(row + 32 * i));
-            len_load = a.seq_lens[b];
-            have_next = walk.next(next);
-            if (have_next)
-                window(next, win_next);
-        } else if (t.first) {
-            there = false;
-            load.lim = 0;
-        }
-        const int tok = load.tok;
-        t.tok = tok;
-        if ((tok >> a.ps_log2) >= win.page0 + 64) {
-            win.page0 += 64;
-            win.phys = win.phys_next;
-            win.phys_next = entry(load, win.page0 + 64 + lane);
-        }
-        int64_t off[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = tok + 16 * i;
-            const int ph = __builtin_amdgcn_readlane(win.phys, ((at >> a.ps_log2) - win.page0) & 63);
-            t.live[i] = ph >= 0 && ph < a.num_phys && at < load.lim;
-            off[i] = t.live[i] ? (((int64_t)ph * a.num_kv_heads + load.h) * a.ps + (at & (a.ps - 1))) *
-                                     kHeadDim
-                               : 0;
-        }
-        if (walk.shared) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                load_half<false>(t.h[i], a.k_cache + off[i], a.v_cache + off[i], lr, lg);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                load_half<true>(t.h[i], a.k_cache + off[i], a.v_cache + off[i], lr, lg);
-        }
-        load.tok += kTileTokens;
-        --load.tiles;
-        t.last = load.tiles == 0;
-        return there;
+        for (int i = 0; i < 4; ++i)
+            x[i] = __builtin_bit_cast(bf16x8_t, ld16(row + 32 * i));
+        tokens = a.seq_lens[b];
     }
 
-    // The part whose first tile was issued last becomes the one at work.
-    __device__ __forceinline__ void begin()
+    __device__ __forceinline__ void begin(const Part &u, int row0, const bf16x8_t (&x)[4], int tokens)
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            q[i] = q_load[i];
-        lim = load.lim;
-        rows = load.rows;
-        slot = load.slot;
-        len = lr < rows ? clamp_len(len_load, a.ps, a.max_pages) : 0x7fffffff;
+            q[i] = x[i];
+        lim = u.lim;
+        rows = min(max(u.rows - row0, 0), kRows);
+        len = lr < rows ? clamp_len(tokens, a.ps, a.max_pages) : 0x7fffffff;
         full = min((int)wave_min((uint32_t)len), lim);
         m = kNoLogit;
         l = 0.f;
 #pragma unroll
         for (int c = 0; c < 8; ++c)
             O[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
-
-    // One tile of the part at work, with the next one's loads issued in front; false: it was the last.
-    __device__ __forceinline__ bool step(Tile &t, Tile &behind)
-    {
-        if (t.first)
-            begin();
-        const bool more = issue(behind);
-        attend(t);
-        if (t.last)
-            write();
-        return more;
-    }
-
-    __device__ __forceinline__ void run()
-    {
-        Tile x, y;
-        issue(x);
-        while (step(x, y) && step(y, x)) {
-        }
     }
 
     __device__ __forceinline__ void attend(Tile &t)
@@ -507,16 +438,15 @@ struct Streamer {
         }
         float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])),
                           fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = over_groups(top, [](float x, float y) { return fmaxf(x, y); });
         const float m_new = fmaxf(m, top);
-        const float alpha = exp2f(m - m_new);
+        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
         m = m_new;
         float sum = 0.f;
         u32x4_t p[kTerms];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            float x0 = exp2f(z[e] - m_new), x1 = exp2f(z[e + 1] - m_new);
+            float x0 = __builtin_amdgcn_exp2f(z[e] - m_new), x1 = __builtin_amdgcn_exp2f(z[e + 1] - m_new);
             if (kTerms > 1)
                 sum += x0 + x1;
 #pragma unroll
@@ -550,15 +480,14 @@ struct Streamer {
         }
     }
 
-    // (m, l, o) of the part's rows to its slot.
-    __device__ __forceinline__ void write()
+    // (m, l, o) of the rows to slot `slot` of slots of `stride` rows.
+    __device__ __forceinline__ void write(float *o, float *ml, uint32_t slot, int stride) const
     {
-        float sum = l + __shfl_xor(l, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
+        const float sum = over_groups(l, [](float x, float y) { return x + y; });
         if (lr >= rows)
             return;
-        const int64_t row = (int64_t)slot * (walk.shared ? kRows : G) + lr;
-        float *op = (walk.shared ? a.o_group : a.o_seq) + row * kHeadDim + 32 * lg;
+        const int64_t row = (int64_t)slot * stride + lr;
+        float *op = o + row * kHeadDim + 32 * lg;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             st16(op + 8 * i, __builtin_bit_cast(u32x4_t, (f32x4_t){O[0][i], O[1][i], O[2][i], O[3][i]}));
@@ -566,9 +495,231 @@ struct Streamer {
                  __builtin_bit_cast(u32x4_t, (f32x4_t){O[4][i], O[5][i], O[6][i], O[7][i]}));
         }
         if (lg == 0) {
-            float *ml = (walk.shared ? a.ml_group : a.ml_seq) + 2 * row;
-            ml[0] = m;
-            ml[1] = sum;
+            ml[2 * row] = m;
+            ml[2 * row + 1] = sum;
+        }
+    }
+};
+
+// A wave's way through its sequences: the loads of the next tile, the next part's first one too, are always
+// under way, and the next part's block-table entries with them.
+template <int kTerms>
+struct Stream {
+    const SharedArgs &a;
+    Walk<false> walk;
+    Rows<kTerms> work;
+    Part load, next;  // the part whose tiles are being loaded, the one behind it
+    bool have_next;
+    Window win, win_next;
+    bf16x8_t q_load[4];  // the loaded part's
+    int len_load;
+    uint32_t slot;  // of the part at work
+
+    struct Item {
+        Tile t;
+        bool first, last;  // of its part
+    };
+
+    __device__ __forceinline__ Stream(const SharedArgs &args, const Walk<false> &wk)
+        : a(args), walk(wk), work(args)
+    {
+        load.tiles = 0;
+        have_next = walk.next(next);  // (a wave has a position at least)
+        win_next.begin(a, next, work.lane);
+    }
+
+    // The loads of the next tile; false: there is none.  They are issued whatever the tile holds (from the
+    // cache's first page where there is none), so that the wait for an earlier tile can count the
+    // loads behind it.
+    __device__ __forceinline__ bool issue(Item &x)
+    {
+        bool there = true;
+        x.first = load.tiles == 0;
+        if (x.first && have_next) {
+            load = next;
+            win = win_next;
+            work.load(load, 0, q_load, len_load);
+            have_next = walk.next(next);
+            if (have_next)
+                win_next.begin(a, next, work.lane);
+        } else if (x.first) {
+            there = false;
+            load.lim = 0;
+        }
+        x.t.tok = load.tok;
+        win.reach(a, load, load.tok, work.lane);
+        int64_t off[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            off[i] = win.place(a, load, load.tok + 16 * i, x.t.live[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            load_half(x.t.h[i], a.k_cache + off[i], a.v_cache + off[i], work.lr, work.lg);
+        load.tok += kTileTokens;
+        --load.tiles;
+        x.last = load.tiles == 0;
+        return there;
+    }
+
+    // One tile of the part at work, with the next one's loads issued in front; false: it was the last.
+    __device__ __forceinline__ bool step(Item &x, Item &behind)
+    {
+        if (x.first) {  // (the part whose first tile was issued last)
+            work.begin(load, 0, q_load, len_load);
+            slot = load.slot;
+        }
+        const bool more = issue(behind);
+        __builtin_amdgcn_sched_barrier(0);  // (all of them in front of the wait for this tile)
+        work.attend(x.t);
+        if (x.last)
+            work.write(a.o_seq, a.ml_seq, slot, work.G);
+        return more;
+    }
+
+    __device__ __forceinline__ void run()
+    {
+        Item x, y;
+        issue(x);
+        while (step(x, y) && step(y, x)) {
+        }
+    }
+};
+
+// A workgroup's way through its groups.  Wave w brings K (even w) or V (odd) of the tiles' half w / 2, 4 rows
+// of 256 bytes an instruction, and keeps kStages - 1 tiles under way in registers; in LDS a row's
+// 16-byte chunk c lies at place c ^ (row % 16), so that the 16 rows of an operand are in different banks.
+constexpr int kStages = 4;  // (even: the LDS has two tiles in turn)
+constexpr int kChunks = kHeadDim * 2 / 16;
+constexpr int kTileChunks = 2 * kTileTokens * kChunks;  // K and V
+static_assert(2 * kTileChunks * 16 >= kMaxGroups * sizeof(int32_t), "the plan's scratch");
+static_assert(2 * kTileChunks * 16 + plan_lds(kMaxBatch, kMaxGroups) + 1024 <= 160 << 10,
+              "LDS of a workgroup");
+
+template <int kTerms>
+struct Team {
+    const SharedArgs &a;
+    u32x4_t *s_tile;
+    const int wave;
+    Walk<true> ahead, walk;
+    Rows<kTerms> work;
+    Part load, next, u;  // being loaded, behind that one, at work
+    bool have_next;
+    Window win, win_next;
+    int fill;  // steps before the first tile is there
+
+    struct Stage {
+        u32x4_t v[4];
+        int tok;
+        bool live[2];
+    };
+
+    __device__ __forceinline__ Team(const SharedArgs &args, const Walk<true> &wk, u32x4_t *lds)
+        : a(args), s_tile(lds), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), ahead(wk),
+          walk(wk), work(args)
+    {
+        load.tiles = 0;
+        have_next = ahead.next(next);  // (a workgroup has a position at least)
+        win_next.begin(a, next, work.lane);
+    }
+
+    __device__ __forceinline__ void issue(Stage &x)
+    {
+        if (load.tiles == 0) {
+            if (have_next) {
+                load = next;
+                win = win_next;
+                have_next = ahead.next(next);
+                if (have_next)
+                    win_next.begin(a, next, work.lane);
+            } else {  // nothing left: the cache's first page, for the count of loads
+                load.lim = 0;
+                load.tiles = 0x7fffffff;
+            }
+        }
+        x.tok = load.tok;
+        win.reach(a, load, load.tok, work.lane);
+        int64_t off[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            off[i] = win.place(a, load, load.tok + 16 * i, x.live[i]);
+        const uint16_t *p = (wave & 1 ? a.v_cache : a.k_cache) + (wave >> 1 ? off[1] : off[0]) +
+                            work.lg * kHeadDim + 8 * work.lr;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            x.v[j] = ld16_nt(p + 4 * j * kHeadDim);
+        load.tok += load.lim ? kTileTokens : 0;
+        --load.tiles;
+    }
+
+    __device__ __forceinline__ void put(const Stage &x, int turn)
+    {
+        u32x4_t *s = s_tile + turn * kTileChunks + (wave & 1) * (kTileTokens * kChunks);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = 4 * j + work.lg;  // (its number in 16)
+            s[(16 * (wave >> 1) + row) * kChunks + (work.lr ^ row)] = x.v[j];
+        }
+    }
+
+    __device__ __forceinline__ void get(Tile &t, int turn) const
+    {
+        const u32x4_t *k = s_tile + turn * kTileChunks, *v = k + kTileTokens * kChunks;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                t.h[i].k[j] = k[(16 * i + work.lr) * kChunks + ((4 * j + work.lg) ^ work.lr)];
+                const int row = 4 * work.lg + j;
+                t.h[i].v[j] = v[(16 * i + row) * kChunks + (work.lr ^ row)];
+            }
+    }
+
+    __device__ __forceinline__ bool next_part()
+    {
+        if (!walk.next(u))
+            return false;
+        bf16x8_t x[4];
+        int tokens;
+        work.load(u, kRows * wave, x, tokens);
+        work.begin(u, kRows * wave, x, tokens);
+        return true;
+    }
+
+    // Brings a tile on its way and attends with the one that was kStages - 1 steps ago; false: it was the last.
+    // The LDS tile that put() writes was read two steps ago, before the last barrier.
+    __device__ __forceinline__ bool step(Stage &behind, const Stage &x, int turn)
+    {
+        issue(behind);
+        __builtin_amdgcn_sched_barrier(0);  // (in front of the wait for this tile)
+        if (fill > 0) {
+            --fill;
+            return true;
+        }
+        put(x, turn);
+        __syncthreads();
+        if (work.rows > 0) {
+            Tile t;
+            t.tok = x.tok;
+            t.live[0] = x.live[0];
+            t.live[1] = x.live[1];
+            get(t, turn);
+            work.attend(t);
+        }
+        if (--u.tiles == 0) {
+            if (work.rows > 0)
+                work.write(a.o_group, a.ml_group, u.slot + wave, kRows);
+            return next_part();
+        }
+        return true;
+    }
+
+    __device__ __forceinline__ void run()
+    {
+        Stage s0, s1, s2, s3;
+        static_assert(kStages == 4, "stages by name");
+        fill = kStages - 1;
+        next_part();
+        while (step(s0, s1, 1) && step(s1, s2, 0) && step(s2, s3, 1) && step(s3, s0, 0)) {
         }
     }
 };
@@ -586,89 +737,78 @@ __global__ __launch_bounds__(kSharedThreads, 2) void k_shared_stream(SharedArgs 
 {
     extern __shared__ int32_t s_plan[];
     __shared__ int32_t s_tmp[kSharedWaves];
+    __shared__ u32x4_t s_tile[2 * kTileChunks];
     const Plan plan(s_plan, a);
-    make_plan(a, plan, s_tmp);
+    make_plan(a, plan, reinterpret_cast<int32_t *>(s_tile), s_tmp);
 
     const uint32_t all = __builtin_amdgcn_readfirstlane(plan.off[a.groups + a.batch]);
     const uint32_t P1 = __builtin_amdgcn_readfirstlane(plan.off[a.groups]), P2 = all - P1;
-    const Sides sides(a, P1, P2, gridDim.x * kSharedWaves);
+    const Sides sides(a, P1, P2, gridDim.x);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        a.plan_waves[0] = sides.w1;
-        a.plan_waves[1] = sides.w2;
+        a.plan_takers[0] = sides.w1;
+        a.plan_takers[1] = sides.w2;
     }
-    // n of the workgroups take the groups, evenly spread among the others over the XCDs and the order of
-    // launch: they share their tiles, so that the memory's time belongs to the others
-    const uint32_t place = place_by_xcd(blockIdx.x, gridDim.x), n = (sides.w1 + kSharedWaves - 1) / kSharedWaves;
-    const uint32_t before = place * n / gridDim.x;
-    const bool shared = (place + 1) * n / gridDim.x > before;
-    const uint32_t w = (shared ? before : place - before) * kSharedWaves +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (w >= (shared ? sides.w1 : sides.w2))
-        return;
-    const Share share(shared ? P1 : P2, shared ? sides.w1 : sides.w2);
-    Walk walk(a, plan, shared, w, share);
-    Streamer<kTerms> st(a, walk);
-    st.run();
+    // those on the groups are spread evenly among the others over the XCDs and the order of launch
+    const uint32_t place = place_by_xcd(blockIdx.x, gridDim.x);
+    const uint32_t before = place * sides.w1 / gridDim.x;
+    if ((place + 1) * sides.w1 / gridDim.x > before) {
+        Team<kTerms> team(a, Walk<true>(a, plan, before, Share(P1, sides.w1)), s_tile);
+        team.run();
+    } else {
+        const uint32_t w = (place - before) * kSharedWaves +
+                           __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (w < sides.w2) {
+            Stream<kTerms> stream(a, Walk<false>(a, plan, w, Share(P2, sides.w2)));
+            stream.run();
+        }
+    }
 }
 
-// The parts of one query head of a sequence: those of its group's segments, at most two waves each (a
-// segment is a position longer than the shortest wave at most), and those of its own unit.
+// The parts of one query head of a sequence: those of its group's unit and those of its own.
 struct Parts {
-    const SharedArgs &a;
-    Share gs;
-    uint32_t first, unit, blocks, rb, size, segs, s0;
-    int g, h, j, begin, row, n_s;
+    int64_t g0, s0;  // the first ones' rows
+    int n_g, n_s, G;
 
-    __device__ __forceinline__ Parts(const SharedArgs &args, int b, int hq)
-        : a(args), gs(args.plan_off[args.groups], args.plan_waves[0])
+    __device__ __forceinline__ Parts(const SharedArgs &a, int b, int hq)
     {
-        const int Hkv = a.num_kv_heads, G = a.num_q_heads / Hkv;
-        h = hq / G;
-        j = hq - h * G;
-        g = a.seq_group[b];
-        size = gs.segment();
-        segs = 0;
+        const int Hkv = a.num_kv_heads;
+        G = a.num_q_heads / Hkv;
+        const int h = hq / G, j = hq - h * G;
+        n_g = n_s = 0;
+        g0 = s0 = 0;
+        const int g = a.seq_group[b];
         if (g >= 0) {
-            first = a.plan_off[g];
-            begin = a.plan_cu[g];
-            blocks = ((a.plan_cu[g + 1] - begin) * G + kRows - 1) / kRows;
-            unit = (a.plan_off[g + 1] - first) / (blocks * Hkv);
-            const int r = (b - begin) * G + j;
-            rb = r / kRows;
-            row = r - rb * kRows;
-            segs = (unit + size - 1) / size;
+            const uint32_t first = a.plan_off[g], all = a.plan_off[g + 1] - first;
+            const int begin = a.plan_cu[g], rows = (a.plan_cu[g + 1] - begin) * G;
+            if (all > 0) {
+                const Share share(a.plan_off[a.groups], a.plan_takers[0]);
+                const uint32_t blocks = (rows + kTeamRows - 1) / kTeamRows, unit = all / (blocks * Hkv);
+                const int r = (b - begin) * G + j;
+                const uint32_t p0 = first + (h * blocks + r / kTeamRows) * unit, w0 = share.taker_of(p0);
+                n_g = share.taker_of(p0 + unit - 1) - w0 + 1;
+                // (the 16 rows' slot of taker w is that of the part, kSharedWaves further for each taker)
+                g0 = (int64_t)(w0 * kSharedWaves + blocks_before(a, g, begin, rows, h, r)) * kRows + r % kRows;
+            }
         }
-        n_s = 0;
         const int32_t *seq = a.plan_off + a.groups;
         const uint32_t own = (seq[b + 1] - seq[b]) / Hkv;
         if (own > 0) {
-            const Share ss(seq[a.batch] - seq[0], a.plan_waves[1]);
-            const uint32_t p0 = seq[b] - seq[0] + h * own, w0 = ss.wave_of(p0);
-            n_s = ss.wave_of(p0 + own - 1) - w0 + 1;
-            s0 = w0 + b * Hkv + h;
+            const Share share(seq[a.batch] - seq[0], a.plan_takers[1]);
+            const uint32_t p0 = seq[b] - seq[0] + h * own, w0 = share.taker_of(p0);
+            n_s = share.taker_of(p0 + own - 1) - w0 + 1;
+            s0 = (int64_t)(w0 + b * Hkv + h) * G + j;
         }
     }
 
-    __device__ __forceinline__ int count() const { return 2 * segs + n_s; }
+    __device__ __forceinline__ int count() const { return n_g + n_s; }
 
-    // Part i: its row of o (128 numbers) and its (m, l); false: there is none.
-    __device__ __forceinline__ bool at(int i, const float *&o, const float *&ml) const
+    // Part i: its row of o (128 numbers) and its (m, l).
+    __device__ __forceinline__ void at(const SharedArgs &a, int i, const float *&o, const float *&ml) const
     {
-        int64_t r;
-        if (i < 2 * (int)segs) {
-            const Segment s = segment_at(a, g, begin, first, unit, blocks, size, h, i >> 1, rb);
-            const uint32_t w = gs.wave_of(s.pos) + (i & 1);
-            if (w > gs.wave_of(s.pos + s.len - 1))
-                return false;
-            r = (int64_t)(w + s.number) * kRows + row;
-            o = a.o_group + r * kHeadDim;
-            ml = a.ml_group + 2 * r;
-        } else {
-            r = (int64_t)(s0 + i - 2 * segs) * (a.num_q_heads / a.num_kv_heads) + j;
-            o = a.o_seq + r * kHeadDim;
-            ml = a.ml_seq + 2 * r;
-        }
-        return true;
+        const bool shared = i < n_g;
+        const int64_t r = shared ? g0 + (int64_t)i * kTeamRows : s0 + (int64_t)(i - n_g) * G;
+        o = (shared ? a.o_group : a.o_seq) + r * kHeadDim;
+        ml = (shared ? a.ml_group : a.ml_seq) + 2 * r;
     }
 };
 
@@ -686,9 +826,10 @@ __global__ __launch_bounds__(kSharedThreads) void k_shared_merge(SharedArgs a)
     const int n = parts.count();
     const float *op, *ml;
     float top = kNoLogit;
-    for (int i = t; i < n; i += 64 * kWaves)
-        if (parts.at(i, op, ml))
-            top = fmaxf(top, ml[0]);
+    for (int i = t; i < n; i += 64 * kWaves) {
+        parts.at(a, i, op, ml);
+        top = fmaxf(top, ml[0]);
+    }
     top = wave_max_f(top);
     if (kWaves > 1) {
         if ((t & 63) == 0)
@@ -701,12 +842,12 @@ __global__ __launch_bounds__(kSharedThreads) void k_shared_merge(SharedArgs a)
     const int side = t >> 5, c = 4 * (t & 31);
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    for (int i = side; i < n; i += kSides)
-        if (parts.at(i, op, ml)) {
-            const float x = exp2f(ml[0] - top);
-            l += ml[1] * x;
-            o += __builtin_bit_cast(f32x4_t, ld16(op + c)) * x;
-        }
+    for (int i = side; i < n; i += kSides) {
+        parts.at(a, i, op, ml);
+        const float x = __builtin_amdgcn_exp2f(ml[0] - top);
+        l += ml[1] * x;
+        o += __builtin_bit_cast(f32x4_t, ld16(op + c)) * x;
+    }
     *reinterpret_cast<f32x4_t *>(&s_o[here][side][c]) = o;
     if (c == 0)
         s_l[here][side] = l;
@@ -722,10 +863,10 @@ __global__ __launch_bounds__(kSharedThreads) void k_shared_merge(SharedArgs a)
     }
 }
 
-// Resident waves of a device of `cus` compute units; the workspace is sized for kMaxCus of them.
+// Workgroups of a launch on `cus` compute units; the workspace is sized for kMaxCus of them.
 constexpr int kMaxCus = 256;
 
-int shared_max_waves(int cus) { return (cus < kMaxCus ? cus : kMaxCus) * kSharedWaves * 2; }
+int shared_blocks(int cus) { return (cus < kMaxCus ? cus : kMaxCus) * 2; }
 
 constexpr int kNarrowRows = 1024;  // query heads and sequences from which a wave merges each
 
@@ -739,12 +880,10 @@ SharedPlan plan_shared(const sparrow_shape_t &s, int groups)
 {
     SharedPlan p;
     const int G = s.num_q_heads / s.num_kv_heads;
-    const size_t waves = shared_max_waves(kMaxCus);
+    const size_t waves = (size_t)shared_blocks(kMaxCus) * kSharedWaves;
     p.plan_bytes = round_up(sizeof(int32_t) * (2 * ((size_t)groups + s.batch) + 4));
-    // slots of a wave and a segment: whole segments are no more than waves, and every row block has
-    // one that is not
     p.group_slots =
-        groups ? 2 * waves + (size_t)s.num_kv_heads * ((size_t)s.batch * G / kRows + groups) : 0;
+        groups ? waves + (size_t)s.num_kv_heads * ((size_t)s.batch * G / kRows + groups) : 0;
     p.seq_slots = waves + (size_t)s.batch * s.num_kv_heads;
     const size_t rows = p.group_slots * kRows + p.seq_slots * G;
     p.bytes = p.plan_bytes + rows * (kHeadDim + 2) * sizeof(float);
@@ -783,13 +922,12 @@ hipError_t launch_shared_attention(const sparrow_shape_t &s, const Groups &g, co
     a.out = out;
     a.out_bf16 = out_dtype == SPARROW_OUT_BF16;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.max_waves = shared_max_waves(device_cus());
     a.min_tiles = 2;
     char *ws = static_cast<char *>(workspace);
     a.plan_off = reinterpret_cast<int32_t *>(ws);
     a.seq_group = a.plan_off + g.n + s.batch + 1;
     a.plan_cu = a.seq_group + s.batch;
-    a.plan_waves = a.plan_cu + g.n + 1;
+    a.plan_takers = a.plan_cu + g.n + 1;
     const size_t group_rows = p.group_slots * kRows;
     const size_t seq_rows = p.seq_slots * (s.num_q_heads / s.num_kv_heads);
     a.o_group = reinterpret_cast<float *>(ws + p.plan_bytes);
@@ -798,13 +936,13 @@ hipError_t launch_shared_attention(const sparrow_shape_t &s, const Groups &g, co
     a.ml_seq = a.ml_group + group_rows * 2;
     // positions of all units at most, with the longest sequences everywhere, stay below 2^31
     const int64_t units = (int64_t)s.num_kv_heads *
-                          (s.batch + (int64_t)s.batch * (s.num_q_heads / s.num_kv_heads) / kRows + g.n);
+                          (s.batch + (int64_t)s.batch * (s.num_q_heads / s.num_kv_heads) / kTeamRows + g.n);
     const int64_t tiles = ((int64_t)s.max_pages_per_seq * s.page_size + kTileTokens - 1) / kTileTokens;
     for (a.step_log2 = 0; ((tiles >> a.step_log2) + 1) * units > 0x7fffffff;)
         ++a.step_log2;
-    const size_t lds = sizeof(int32_t) * (4 * (size_t)g.n + 2 * (size_t)s.batch + 2);
+    const size_t lds = plan_lds(s.batch, g.n);
     auto kernel = a.out_bf16 ? k_shared_stream<1> : k_shared_stream<3>;
-    hipLaunchKernelGGL(kernel, dim3(a.max_waves / kSharedWaves), dim3(kSharedThreads), lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3(shared_blocks(device_cus())), dim3(kSharedThreads), lds, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
