@@ -49,7 +49,7 @@ struct SharedArgs {
     float *o_group, *ml_group;  // [slots][kRows] rows: a slot for each 16 rows of a part
     float *o_seq, *ml_seq;      // [slots][G] rows
     void *out;
-    int64_t num_phys;
+    uint32_t num_phys, page_elems;  // pages (what an int32 entry can name), elements of one
     int groups, batch, num_q_heads, num_kv_heads, ps, ps_log2, max_pages, out_bf16;
     int min_tiles;
     int step_log2;  // a position is 2^step_log2 tiles (more than one only where 2^31 would not do)
@@ -57,8 +57,9 @@ struct SharedArgs {
 };
 
 // How many workgroups take the groups' positions (P1 of them) and how many waves the sequences' (P2): all of
-// the launch's, or where that would be less than min_tiles each, fewer.  A workgroup on a group has half the
-// bytes under way that four waves on sequences have, so its positions count double.
+// the launch's, or where that would be less than min_tiles each, fewer.  kTeamCost is a position's time in a
+// workgroup on a group against that of one in four waves on sequences.
+constexpr float kTeamCost = 1.25f;
 struct Sides {
     uint32_t w1, w2;
     __device__ __forceinline__ Sides(const SharedArgs &a, uint32_t P1, uint32_t P2, uint32_t blocks)
@@ -66,7 +67,7 @@ struct Sides {
         w1 = (P1 + a.min_tiles - 1) / a.min_tiles;
         w2 = (P2 + a.min_tiles - 1) / a.min_tiles;
         if (w1 + (w2 + kSharedWaves - 1) / kSharedWaves > blocks) {
-            const float c1 = 2.f * (float)P1;
+            const float c1 = kTeamCost * (float)P1;
             uint32_t n = (uint32_t)(c1 / (c1 + (float)P2) * blocks + 0.5f);
             n = P1 ? max(n, 1u) : 0u;
             n = P2 ? min(n, blocks - 1) : blocks;
@@ -116,6 +117,9 @@ constexpr size_t plan_lds(size_t batch, size_t groups)
     return sizeof(int32_t) * (3 * groups + 2 * batch + 2);
 }
 
+// A unit takes kPartCost positions more than it has: what a part costs beside its tiles.
+constexpr int kPartCost = 2;
+
 // seq entries: own positions (16 bits) under the first own page.
 constexpr int kSeqTileBits = 16;
 static_assert(SPARROW_MAX_PAGES_PER_SEQ * 128 / kTileTokens < 1 << kSeqTileBits, "tiles of a sequence");
@@ -127,6 +131,11 @@ __device__ __forceinline__ int positions_of(const SharedArgs &a, int tokens)
     return (tokens + (1 << log2) - 1) >> log2;
 }
 static_assert(kTileTokens == 1 << 5, "positions_of");
+
+__device__ __forceinline__ int with_cost(int positions)
+{
+    return positions ? positions + kPartCost : 0;
+}
 
 // pages: LDS of the groups' size, scratch.
 __device__ void make_plan(const SharedArgs &a, const Plan &p, int32_t *pages, int32_t *s_tmp)
@@ -177,8 +186,8 @@ __device__ void make_plan(const SharedArgs &a, const Plan &p, int32_t *pages, in
     const int n = a.groups + a.batch;
     auto positions = [&](int e) -> int {
         if (e >= a.groups)
-            return Hkv * (p.seq[e - a.groups] & ((1 << kSeqTileBits) - 1));
-        return Hkv * positions_of(a, p.lim[e]) *
+            return Hkv * with_cost(p.seq[e - a.groups] & ((1 << kSeqTileBits) - 1));
+        return Hkv * with_cost(positions_of(a, p.lim[e])) *
                (((p.cu[e + 1] - p.cu[e]) * G + kTeamRows - 1) / kTeamRows);
     };
     const int per = (n + kSharedThreads - 1) / kSharedThreads;
@@ -279,46 +288,51 @@ struct Walk {
 
     __device__ __forceinline__ bool next(Part &u)
     {
-        if (pos >= end)
-            return false;
-        while (off[e + 1] == off[e])
-            ++e;
-        const uint32_t first = __builtin_amdgcn_readfirstlane(off[e]);
-        const int step = kTileTokens << a.step_log2;
-        uint32_t at, unit;
-        if (kTeam) {
-            u.b0 = __builtin_amdgcn_readfirstlane(plan.cu[e]);
-            u.lim = __builtin_amdgcn_readfirstlane(plan.lim[e]);
-            const int rows = (__builtin_amdgcn_readfirstlane(plan.cu[e + 1]) - u.b0) * G;
-            const uint32_t blocks = (rows + kTeamRows - 1) / kTeamRows;
-            unit = positions_of(a, u.lim);
-            const uint32_t n = (pos - first) / unit;
-            at = pos - first - n * unit;
-            u.h = n / blocks;
-            u.row0 = (n - u.h * blocks) * kTeamRows;
-            u.rows = min(kTeamRows, rows - u.row0);
-            u.slot = w * kSharedWaves + blocks_before(a, e, u.b0, rows, u.h, u.row0);
-            u.tok = (int)at * step;
-        } else {
-            const int packed = __builtin_amdgcn_readfirstlane(plan.seq[e]);
-            unit = packed & ((1 << kSeqTileBits) - 1);
-            u.b0 = e;
-            u.lim = clamp_len(a.seq_lens[e], a.ps, a.max_pages);
-            u.h = (pos - first) / unit;
-            at = pos - first - u.h * unit;
-            u.slot = w + e * Hkv + u.h;
-            u.row0 = 0;
-            u.rows = G;
-            u.tok = (packed >> kSeqTileBits << a.ps_log2) + (int)at * step;
+        while (pos < end) {
+            while (off[e + 1] == off[e])
+                ++e;
+            const uint32_t first = __builtin_amdgcn_readfirstlane(off[e]);
+            const int step = kTileTokens << a.step_log2;
+            uint32_t at, unit;
+            if (kTeam) {
+                u.b0 = __builtin_amdgcn_readfirstlane(plan.cu[e]);
+                u.lim = __builtin_amdgcn_readfirstlane(plan.lim[e]);
+                const int rows = (__builtin_amdgcn_readfirstlane(plan.cu[e + 1]) - u.b0) * G;
+                const uint32_t blocks = (rows + kTeamRows - 1) / kTeamRows;
+                unit = with_cost(positions_of(a, u.lim));
+                const uint32_t n = (pos - first) / unit;
+                at = pos - first - n * unit;
+                u.h = n / blocks;
+                u.row0 = (n - u.h * blocks) * kTeamRows;
+                u.rows = min(kTeamRows, rows - u.row0);
+                u.slot = w * kSharedWaves + blocks_before(a, e, u.b0, rows, u.h, u.row0);
+                u.tok = 0;
+            } else {
+                const int packed = __builtin_amdgcn_readfirstlane(plan.seq[e]);
+                unit = with_cost(packed & ((1 << kSeqTileBits) - 1));
+                u.b0 = e;
+                u.lim = clamp_len(a.seq_lens[e], a.ps, a.max_pages);
+                u.h = (pos - first) / unit;
+                at = pos - first - u.h * unit;
+                u.slot = w + e * Hkv + u.h;
+                u.row0 = 0;
+                u.rows = G;
+                u.tok = packed >> kSeqTileBits << a.ps_log2;
+            }
+            u.table = a.block_table + (int64_t)u.b0 * a.max_pages;
+            const uint32_t take = min(unit - at, end - pos);
+            pos += take;
+            if (pos == (uint32_t)__builtin_amdgcn_readfirstlane(off[e + 1]))
+                ++e;
+            const int from = max((int)at - kPartCost, 0), to = (int)(at + take) - kPartCost;
+            if (to > from) {
+                u.tok += from * step;
+                // (tiles of the last position may lie behind the unit's tokens)
+                u.tiles = min((to - from) << a.step_log2, (u.lim - u.tok + kTileTokens - 1) / kTileTokens);
+                return true;
+            }
         }
-        u.table = a.block_table + (int64_t)u.b0 * a.max_pages;
-        const uint32_t take = min(unit - at, end - pos);
-        // (tiles of the last position may lie behind the unit's tokens)
-        u.tiles = min((int)take << a.step_log2, (u.lim - u.tok + kTileTokens - 1) / kTileTokens);
-        pos += take;
-        if (pos == (uint32_t)__builtin_amdgcn_readfirstlane(off[e + 1]))
-            ++e;
-        return true;
+        return false;
     }
 };
 
@@ -349,8 +363,10 @@ struct Window {
     __device__ __forceinline__ int64_t place(const SharedArgs &a, const Part &u, int at, bool &live) const
     {
         const int ph = __builtin_amdgcn_readlane(phys, ((at >> a.ps_log2) - page0) & 63);
-        live = ph >= 0 && ph < a.num_phys && at < u.lim;
-        return live ? (((int64_t)ph * a.num_kv_heads + u.h) * a.ps + (at & (a.ps - 1))) * kHeadDim : 0;
+        live = (uint32_t)ph < a.num_phys && at < u.lim;  // (a negative entry is above any count)
+        return live ? (int64_t)((uint64_t)(uint32_t)ph * a.page_elems) +
+                          ((u.h << a.ps_log2) + (at & (a.ps - 1))) * kHeadDim
+                    : 0;
     }
 };
 
@@ -524,8 +540,9 @@ struct Stream {
         : a(args), walk(wk), work(args)
     {
         load.tiles = 0;
-        have_next = walk.next(next);  // (a wave has a position at least)
-        win_next.begin(a, next, work.lane);
+        have_next = walk.next(next);
+        if (have_next)
+            win_next.begin(a, next, work.lane);
     }
 
     // The loads of the next tile; false: there is none.  They are issued whatever the tile holds (from the
@@ -578,6 +595,8 @@ struct Stream {
 
     __device__ __forceinline__ void run()
     {
+        if (!have_next)
+            return;
         Item x, y;
         issue(x);
         while (step(x, y) && step(y, x)) {
@@ -605,7 +624,6 @@ struct Team {
     Part load, next, u;  // being loaded, behind that one, at work
     bool have_next;
     Window win, win_next;
-    int fill;  // steps before the first tile is there
 
     struct Stage {
         u32x4_t v[4];
@@ -618,8 +636,9 @@ struct Team {
           walk(wk), work(args)
     {
         load.tiles = 0;
-        have_next = ahead.next(next);  // (a workgroup has a position at least)
-        win_next.begin(a, next, work.lane);
+        have_next = ahead.next(next);
+        if (have_next)
+            win_next.begin(a, next, work.lane);
     }
 
     __device__ __forceinline__ void issue(Stage &x)
@@ -691,10 +710,6 @@ struct Team {
     {
         issue(behind);
         __builtin_amdgcn_sched_barrier(0);  // (in front of the wait for this tile)
-        if (fill > 0) {
-            --fill;
-            return true;
-        }
         put(x, turn);
         __syncthreads();
         if (work.rows > 0) {
@@ -717,9 +732,12 @@ struct Team {
     {
         Stage s0, s1, s2, s3;
         static_assert(kStages == 4, "stages by name");
-        fill = kStages - 1;
-        next_part();
-        while (step(s0, s1, 1) && step(s1, s2, 0) && step(s2, s3, 1) && step(s3, s0, 0)) {
+        if (!next_part())
+            return;
+        issue(s0);
+        issue(s1);
+        issue(s2);
+        while (step(s3, s0, 0) && step(s0, s1, 1) && step(s1, s2, 0) && step(s2, s3, 1)) {
         }
     }
 };
@@ -784,7 +802,8 @@ struct Parts {
                 const Share share(a.plan_off[a.groups], a.plan_takers[0]);
                 const uint32_t blocks = (rows + kTeamRows - 1) / kTeamRows, unit = all / (blocks * Hkv);
                 const int r = (b - begin) * G + j;
-                const uint32_t p0 = first + (h * blocks + r / kTeamRows) * unit, w0 = share.taker_of(p0);
+                const uint32_t p0 = first + (h * blocks + r / kTeamRows) * unit;
+                const uint32_t w0 = share.taker_of(p0 + kPartCost);
                 n_g = share.taker_of(p0 + unit - 1) - w0 + 1;
                 // (the 16 rows' slot of taker w is that of the part, kSharedWaves further for each taker)
                 g0 = (int64_t)(w0 * kSharedWaves + blocks_before(a, g, begin, rows, h, r)) * kRows + r % kRows;
@@ -794,7 +813,7 @@ struct Parts {
         const uint32_t own = (seq[b + 1] - seq[b]) / Hkv;
         if (own > 0) {
             const Share share(seq[a.batch] - seq[0], a.plan_takers[1]);
-            const uint32_t p0 = seq[b] - seq[0] + h * own, w0 = share.taker_of(p0);
+            const uint32_t p0 = seq[b] - seq[0] + h * own, w0 = share.taker_of(p0 + kPartCost);
             n_s = share.taker_of(p0 + own - 1) - w0 + 1;
             s0 = (int64_t)(w0 + b * Hkv + h) * G + j;
         }
@@ -918,7 +937,8 @@ hipError_t launch_shared_attention(const sparrow_shape_t &s, const Groups &g, co
     a.ps = s.page_size;
     a.ps_log2 = __builtin_ctz(s.page_size);
     a.max_pages = s.max_pages_per_seq;
-    a.num_phys = s.num_phys_pages;
+    a.num_phys = (uint32_t)(s.num_phys_pages < 0x7fffffff ? s.num_phys_pages : 0x80000000ll);
+    a.page_elems = (uint32_t)(s.num_kv_heads * s.page_size * kHeadDim);
     a.out = out;
     a.out_bf16 = out_dtype == SPARROW_OUT_BF16;
     a.scale_log2 = scale * 1.4426950408889634f;
@@ -938,7 +958,7 @@ hipError_t launch_shared_attention(const sparrow_shape_t &s, const Groups &g, co
     const int64_t units = (int64_t)s.num_kv_heads *
                           (s.batch + (int64_t)s.batch * (s.num_q_heads / s.num_kv_heads) / kTeamRows + g.n);
     const int64_t tiles = ((int64_t)s.max_pages_per_seq * s.page_size + kTileTokens - 1) / kTileTokens;
-    for (a.step_log2 = 0; ((tiles >> a.step_log2) + 1) * units > 0x7fffffff;)
+    for (a.step_log2 = 0; ((tiles >> a.step_log2) + 1 + kPartCost) * units > 0x7fffffff;)
         ++a.step_log2;
     const size_t lds = plan_lds(s.batch, g.n);
     auto kernel = a.out_bf16 ? k_shared_stream<1> : k_shared_stream<3>;
