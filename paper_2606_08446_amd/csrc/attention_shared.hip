@@ -59,7 +59,7 @@ struct SharedArgs {
 // How many workgroups take the groups' positions (P1 of them) and how many waves the sequences' (P2): all of
 // the launch's, or where that would be less than min_tiles each, fewer.  kTeamCost is a position's time in a
 // workgroup on a group against that of one in four waves on sequences.
-constexpr float kTeamCost = 1.25f;
+constexpr float kTeamCost = 1.f;
 struct Sides {
     uint32_t w1, w2;
     __device__ __forceinline__ Sides(const SharedArgs &a, uint32_t P1, uint32_t P2, uint32_t blocks)
@@ -766,14 +766,18 @@ __global__ __launch_bounds__(kSharedThreads, 2) void k_shared_stream(SharedArgs 
         a.plan_takers[0] = sides.w1;
         a.plan_takers[1] = sides.w2;
     }
-    // those on the groups are spread evenly among the others over the XCDs and the order of launch
-    const uint32_t place = place_by_xcd(blockIdx.x, gridDim.x);
-    const uint32_t before = place * sides.w1 / gridDim.x;
-    if ((place + 1) * sides.w1 / gridDim.x > before) {
-        Team<kTerms> team(a, Walk<true>(a, plan, before, Share(P1, sides.w1)), s_tile);
+    // Those on the groups are spread evenly over the XCDs and their compute units, and launched first: of two
+    // workgroups on a unit the older one goes ahead, and the sequences' have no order to keep among them.
+    const uint32_t half = gridDim.x / 2, late = blockIdx.x >= half ? 1 : 0;
+    const uint32_t mine = late ? gridDim.x - half : half, w1 = sides.w1;
+    const uint32_t n = late ? w1 - min(w1, half) : min(w1, half);  // of this half's workgroups
+    const uint32_t place = place_by_xcd(blockIdx.x - (late ? half : 0), mine), before = place * n / mine;
+    if ((place + 1) * n / mine > before) {
+        const uint32_t w = (late ? half : 0) + before;
+        Team<kTerms> team(a, Walk<true>(a, plan, w, Share(P1, w1)), s_tile);
         team.run();
     } else {
-        const uint32_t w = (place - before) * kSharedWaves +
+        const uint32_t w = ((late ? half - min(w1, half) : 0) + place - before) * kSharedWaves +
                            __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (w < sides.w2) {
             Stream<kTerms> stream(a, Walk<false>(a, plan, w, Share(P2, sides.w2)));
