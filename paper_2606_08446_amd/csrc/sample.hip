@@ -5,15 +5,21 @@
 //   the sum over top-k's; min-p those with w >= q; and the token is the first kept one, by index,
 //   whose running sum of w exceeds u times the sum over the kept.
 // The outcome is a whole number, so what decides it is held far finer than the logits: weights and
-// sums in fp64 (an exponential of 18 operations, off by 1e-14), histograms in 64-bit fixed point, in
+// sums in fp64 (an exponential of 16 operations, off by 4e-14), histograms in 64-bit fixed point, in
 // orders that depend on the sizes alone.
 //
-// k_sample_stats reads the rows once: the maximum of every 64 vectors, and where it may be asked for
-// the sum of the weights of every 256, relative to their own maximum.  k_sample_pick, one workgroup per
-// row, finds from them which of those blocks can hold a kept token and reads only these: the k-th
-// largest block maximum bounds top-k's last logit from below, (1 - p) / vocab of the whole sum
-// top-p's last weight.  Up to kSampleSort tokens above the bound are sorted in LDS; more are narrowed down
-// by digits of their keys.  Without a filter one span's 256 vectors are all it reads.
+// k_sample_stats reads the rows once: the maximum of every 64 vectors (a block), and where it may be asked
+// for the sum of the weights of every 256 (a span), relative to their own maximum.  The second kernel
+// finds from these which blocks can hold a kept token and reads only them:
+//   no filter     one wave per row: the span that holds the token, then its block (k_sample_plain)
+//   min-p         the blocks that reach m + T ln q: their sums, then one block
+//   top-k         the k-th largest block maximum bounds the last kept logit from below: the tokens above,
+//                 hardly more than k, are sorted in LDS
+//   top-p         a weight of (1 - p) / vocab of the whole bounds it: up to 2048 tokens above are
+//                 sorted; more are located first, by fp32 weights summed in 2048 bins of equal width whose
+//                 error is bounded, so that the tokens of a bin or two are sorted and all above them
+//                 are summed
+//   else          (large top-k, many ties) the border is found by 11-bit digits of the keys
 #include "common.h"
 #include "sample.h"
 #include "wave.h"
@@ -83,47 +89,60 @@ struct Row {
             }
         return x;
     }
-    // its logits: NaN counts as masked, +inf as the largest number, -0 as 0
+    // its logits: NaN counts as masked
     __device__ static __forceinline__ void unpack(u32x4_t v, float (&z)[kElems<kBf16>])
     {
 #pragma unroll
         for (int e = 0; e < kElems<kBf16>; ++e) {
             float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
                             : __uint_as_float(v[e & 3]);
-            f = f != f ? -INFINITY : f;
-            z[e] = fminf(f, FLT_MAX) + 0.f;
+            z[e] = f != f ? -INFINITY : f;
         }
+    }
+    // and +inf as the largest number, -0 as 0
+    __device__ static __forceinline__ void unpack_whole(u32x4_t v, float (&z)[kElems<kBf16>])
+    {
+        unpack(v, z);
+#pragma unroll
+        for (int e = 0; e < kElems<kBf16>; ++e)
+            z[e] = fminf(z[e], FLT_MAX) + 0.f;
     }
 };
 
-// 2^t for t <= 0 (NaN: 0): the nearest whole power and the Taylor series of what is left, at most 1/2
-// either way (the next term is 6e-15).
-__device__ __forceinline__ double exp2_64(double t)
+// 2^(d c), for d c in [-1020, 0]: the nearest whole power, which an addition of 1.5 2^52 leaves in the sum's
+// low bits, and for the rest f, at most 1/2 either way, 1 + f q(f) with the q of degree 8 that agrees with
+// (2^f - 1) / f in the 9 Chebyshev points of [-1/2, 1/2]: off by 4e-14, and exact at 0.
+__device__ __forceinline__ double exp2_fast(double d, double c)
 {
-    constexpr double kLn2 = 0.69314718055994530942;
-    constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4,
-                     c5 = c4 * kLn2 / 5, c6 = c5 * kLn2 / 6, c7 = c6 * kLn2 / 7, c8 = c7 * kLn2 / 8,
-                     c9 = c8 * kLn2 / 9, c10 = c9 * kLn2 / 10, c11 = c10 * kLn2 / 11;
-    t = fmax(t, -2000.);
-    const double n = __builtin_rint(t), f = t - n;
-    double p = fma(c11, f, c10);
-    p = fma(p, f, c9);
-    p = fma(p, f, c8);
-    p = fma(p, f, c7);
-    p = fma(p, f, c6);
-    p = fma(p, f, c5);
-    p = fma(p, f, c4);
-    p = fma(p, f, c3);
-    p = fma(p, f, c2);
-    p = fma(p, f, c1);
+    constexpr double kMagic = 6755399441055744.;
+    const double s = fma(d, c, kMagic), f = fma(d, c, kMagic - s);
+    double p = fma(1.0203121063391729e-07, f, 1.3255224878668817e-06);
+    p = fma(p, f, 1.525268684626772e-05);
+    p = fma(p, f, 0.00015403455852453838);
+    p = fma(p, f, 0.0013333558179043112);
+    p = fma(p, f, 0.009618129159402558);
+    p = fma(p, f, 0.055504108664760424);
+    p = fma(p, f, 0.2402265069581299);
+    p = fma(p, f, 0.6931471805599453);
     p = fma(p, f, 1.);
-    return __builtin_ldexp(p, (int)n);
+    const uint64_t b = __builtin_bit_cast(uint64_t, p);
+    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, s);
+    return __builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) + (n << 20)) << 32 | (uint32_t)b);
+}
+
+// 2^(d c) for any d <= 0, c >= 0: 0 below 2^-1000, and for a product that is no number.
+__device__ __forceinline__ double exp2_64(double d, double c)
+{
+    const double t = d * c;
+    const bool some = t >= -1000.;
+    const double w = exp2_fast(some ? d : 0., some ? c : 0.);
+    return some ? w : 0.;
 }
 
 // w of a logit relative to the maximum m, with c = log2(e) / T.
 __device__ __forceinline__ double weight_of(float z, double m, double c)
 {
-    return exp2_64(((double)z - m) * c);
+    return exp2_64((double)z - m, c);
 }
 
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -137,33 +156,37 @@ __device__ __forceinline__ float logit_of(uint32_t key)
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-__device__ __forceinline__ double shfl_up_64(double x, int d)
+// One DPP move of a double; lanes without a source (or in a masked row) get 0.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ double dpp_move_64(double x)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __shfl_up((uint32_t)b, d, 64), hi = __shfl_up((uint32_t)(b >> 32), d, 64);
+    const uint32_t lo = dpp_move<kCtrl, kRowMask>((uint32_t)b, 0u);
+    const uint32_t hi = dpp_move<kCtrl, kRowMask>((uint32_t)(b >> 32), 0u);
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-__device__ __forceinline__ double shfl_64(double x, int lane)
-{
-    const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __shfl((uint32_t)b, lane, 64), hi = __shfl((uint32_t)(b >> 32), lane, 64);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
+// Inclusive sums over the wave's lanes in their order.
 __device__ __forceinline__ double wave_scan_64(double x)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double y = shfl_up_64(x, d);
-        if (lane >= d)
-            x += y;
-    }
+    x += dpp_move_64<kDppRowShr1, 0xf>(x);
+    x += dpp_move_64<kDppRowShr2, 0xf>(x);
+    x += dpp_move_64<kDppRowShr4, 0xf>(x);
+    x += dpp_move_64<kDppRowShr8, 0xf>(x);
+    x += dpp_move_64<kDppRowBcast15, 0xa>(x);
+    x += dpp_move_64<kDppRowBcast31, 0xc>(x);
     return x;
 }
 
-__device__ __forceinline__ double wave_sum_64(double x) { return shfl_64(wave_scan_64(x), 63); }
+__device__ __forceinline__ double lane_64(double x, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+    const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+__device__ __forceinline__ double wave_sum_64(double x) { return lane_64(wave_scan_64(x), 63); }
 
 // A row's settings; off is k = 0, p = 1, q = 0.
 struct Filters {
@@ -221,7 +244,7 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
 #pragma unroll
             for (int e = 1; e < kE; ++e)
                 top[b] = fmaxf(top[b], z[b][e]);
-            top[b] = wave_max_f(top[b]);
+            top[b] = fminf(wave_max_f(top[b]), FLT_MAX);
             m = fmaxf(m, top[b]);
         }
         if (lane < kSpanBlocks) {
@@ -235,11 +258,28 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
             double sum = 0.;
             if (m > -INFINITY) {
                 const double md = m;
+                // logits raised to `low` have a weight of 2^-1000, which no sum here feels, and need no
+                // other care; where fp32 has no such number, the temperature is far out
+                const float low = (float)(md - 1000. / f.c);
+                const double t = ((double)low - md) * f.c;
+                if (low > -INFINITY && t >= -1019. && t <= -900.) {
 #pragma unroll
-                for (int b = 0; b < kSpanBlocks; ++b)
+                    for (int b = 0; b < kSpanBlocks; ++b)
 #pragma unroll
-                    for (int e = 0; e < kE; ++e)
-                        sum += weight_of(z[b][e], md, f.c);
+                        for (int e = 0; e < kE; ++e)
+                            sum += exp2_fast((double)fminf(fmaxf(z[b][e], low), m) - md, f.c);
+                } else {
+#pragma unroll 1
+                    for (int b = 0; b < kSpanBlocks; ++b)
+#pragma unroll
+                        for (int e = 0; e < kE; ++e) {
+                            float x = z[0][e];
+#pragma unroll
+                            for (int k = 1; k < kSpanBlocks; ++k)
+                                x = b == k ? z[k][e] : x;
+                            sum += weight_of(fminf(x, m), md, f.c);
+                        }
+                }
             }
             sum = wave_sum_64(sum);
             if (lane == 0)
@@ -251,10 +291,11 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
 struct PickLds {
     float max[kMaxBlocks];       // the blocks' maxima
     uint16_t list[kMaxBlocks];   // blocks that may hold a kept token
+    double sum[kMaxBlocks];      // weights kept in a block, or in a listed one
     double red[kPickWaves];
     uint32_t cnt[kPickWaves];
     uint32_t n;                  // a counter, a result
-    uint32_t found;
+    uint32_t found, found2;
     double total, before;
     uint64_t d0;
     union {
@@ -266,20 +307,36 @@ struct PickLds {
             unsigned long long w[kDigits];
             uint32_t n[kDigits];
         } hist;
-        struct {
-            double sum[kMaxBlocks];
-            uint32_t ties[kMaxBlocks];
-        } draw;
+        uint32_t ties[kMaxBlocks];
     };
 };
 static_assert(sizeof(PickLds) <= 64 << 10, "LDS of a workgroup");
 
+// The threads that work together: the workgroup, or its first wave alone (whose LDS accesses are in
+// order by themselves).
+template <bool kWave>
+__device__ __forceinline__ void join()
+{
+    if (kWave) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    } else {
+        __syncthreads();
+    }
+}
+
 // Sums over the workgroup's threads in their order: inclusive scan and the total.  The LDS is free
 // again after the caller's next barrier.
+template <bool kWave = false>
 __device__ __forceinline__ double block_scan_64(double x, double *red, double &total)
 {
     const int wave = threadIdx.x >> 6;
     x = wave_scan_64(x);
+    if (kWave) {
+        total = lane_64(x, 63);
+        return x;
+    }
     if ((threadIdx.x & 63) == 63)
         red[wave] = x;
     __syncthreads();
@@ -293,10 +350,15 @@ __device__ __forceinline__ double block_scan_64(double x, double *red, double &t
     return base + x;
 }
 
+template <bool kWave = false>
 __device__ __forceinline__ uint32_t block_scan_32(uint32_t x, uint32_t *cnt, uint32_t &total)
 {
     const int wave = threadIdx.x >> 6;
     x = wave_scan_add(x);
+    if (kWave) {
+        total = (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+        return x;
+    }
     if ((threadIdx.x & 63) == 63)
         cnt[wave] = x;
     __syncthreads();
@@ -310,7 +372,8 @@ __device__ __forceinline__ uint32_t block_scan_32(uint32_t x, uint32_t *cnt, uin
     return base + x;
 }
 
-// Ascending bitonic sort of size (a power of two, at most kSampleSort) keys.
+// Ascending bitonic sort of size (a power of two, at most two per thread) keys.
+template <bool kWave>
 __device__ __forceinline__ void sort_keys(uint64_t *key, int size)
 {
     const int t = threadIdx.x;
@@ -324,7 +387,7 @@ __device__ __forceinline__ void sort_keys(uint64_t *key, int size)
                     key[i + j] = a;
                 }
             }
-            __syncthreads();
+            join<kWave>();
         }
 }
 
@@ -339,21 +402,24 @@ struct Rule {
     double q;
 };
 
+// A row and the tokens of its blocks, for a wave.
 template <bool kBf16>
-struct Picker {
+struct RowPicker {
     static constexpr int kE = kElems<kBf16>;
     const SampleArgs &a;
-    PickLds &s;
     const Row<kBf16> r;
     const Filters f;
     const int64_t row;
+    double u;
     int vecs, blocks;
     float m;
     double md;
 
-    __device__ __forceinline__ Picker(const SampleArgs &args, PickLds &lds, int64_t row_)
-        : a(args), s(lds), r(args, row_), f(args, row_), row(row_)
+    __device__ __forceinline__ RowPicker(const SampleArgs &args, int64_t row_)
+        : a(args), r(args, row_), f(args, row_), row(row_)
     {
+        const float x = a.uniform[row];
+        u = x > 0.f ? fminf(x, 1.f - FLT_EPSILON / 2) : 0.;
         vecs = r.vecs();
         blocks = (vecs + kBlockVecs - 1) / kBlockVecs;
     }
@@ -369,11 +435,209 @@ struct Picker {
 
     __device__ __forceinline__ void load_block(int b, float (&z)[kE]) const
     {
-        Row<kBf16>::unpack(r.load(min(b * kBlockVecs + (int)(threadIdx.x & 63), vecs)), z);
+        Row<kBf16>::unpack_whole(r.load(min(b * kBlockVecs + (int)(threadIdx.x & 63), vecs)), z);
     }
     __device__ __forceinline__ int index_in(int b, int e) const
     {
         return r.index(b * kBlockVecs + (int)(threadIdx.x & 63), e);
+    }
+
+    // The token of block b (by its first wave) at which the running sum of w exceeds `at`; total: the sum over
+    // all kept tokens.
+    __device__ __forceinline__ void pick_in_block(int b, const float (&z)[kE], const double (&w)[kE],
+                                                  double at, double total)
+    {
+        double sum = 0.;
+        uint32_t at_e = 0xffffffffu, last_e = 0;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            sum += w[e];
+            last_e = w[e] > 0. ? (uint32_t)e : last_e;
+        }
+        double here = wave_scan_64(sum) - sum;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            here += w[e];
+            if (at_e == 0xffffffffu && w[e] > 0. && here > at)
+                at_e = (uint32_t)e;
+        }
+        const uint64_t hits = __ballot(at_e != 0xffffffffu);
+        const uint64_t some = __ballot(sum > 0.);  // (the block holds a kept token)
+        // (none, by rounding: the last one)
+        const int lane = hits ? __builtin_ctzll(hits) : (some ? 63 - __builtin_clzll(some) : 0);
+        const uint32_t el = hits ? at_e : last_e;
+        float zt = z[0];
+#pragma unroll
+        for (int e = 1; e < kE; ++e)
+            zt = el == (uint32_t)e ? z[e] : zt;
+        zt = __shfl(zt, lane, 64);
+        answer(__shfl(index_in(b, (int)el), lane, 64), ((double)zt - md) / f.t - log(total));
+    }
+
+    // The draw without a filter, or the largest logit.  A lane holds neighbouring spans.
+    __device__ __forceinline__ void plain(const Stats &st)
+    {
+        constexpr int kPer = (kMaxSpans + 63) / 64;
+        const int lane = threadIdx.x & 63, per = (st.spans + 63) / 64, first = lane * per;
+        const float *maxima = st.maxima + row * st.spans * kSpanBlocks;
+        float top[kPer];
+        double w[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            top[i] = -INFINITY;
+            w[i] = 0.;
+            if (i < per && first + i < st.spans) {
+                const u32x4_t x = ld16(maxima + (first + i) * kSpanBlocks);
+                top[i] = fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
+                               fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
+                if (!f.greedy)
+                    w[i] = st.sums[row * st.spans + first + i];
+            }
+        }
+        float t = top[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i)
+            t = fmaxf(t, top[i]);
+        m = wave_max_f(t);
+        md = m;
+        if (!(m > -INFINITY)) {  // every token is masked
+            answer(-1, -INFINITY);
+            return;
+        }
+        if (f.greedy) {
+            int span = 0;
+#pragma unroll
+            for (int i = kPer - 1; i >= 0; --i)
+                span = top[i] == m ? first + i : span;
+            span = __builtin_amdgcn_readlane(span, __builtin_ctzll(__ballot(t == m)));
+            int b = kSpanBlocks - 1;
+#pragma unroll
+            for (int i = kSpanBlocks - 2; i >= 0; --i)
+                b = maxima[span * kSpanBlocks + i] == m ? i : b;
+            b += span * kSpanBlocks;
+            float z[kE];
+            load_block(b, z);
+            uint32_t at = 0xffffffffu;
+#pragma unroll
+            for (int e = kE - 1; e >= 0; --e)
+                at = z[e] == m ? (uint32_t)index_in(b, e) : at;
+            answer((int)wave_min(at), 0.);
+            return;
+        }
+        double part = 0.;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            w[i] = w[i] > 0. ? w[i] * weight_of(top[i], md, f.c) : 0.;
+            part += w[i];
+        }
+        const double incl = wave_scan_64(part), total = lane_64(incl, 63), at = u * total;
+        // ---- the span: the first at which the running sum exceeds it (by rounding none: the last)
+        double run = incl - part, before = 0.;
+        int span = -1;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (span < 0 && w[i] > 0. && run + w[i] > at) {
+                span = first + i;
+                before = run;
+            }
+            run += w[i];
+        }
+        const uint64_t hits = __ballot(span >= 0);
+        if (hits) {
+            const int from = __builtin_ctzll(hits);
+            span = __builtin_amdgcn_readlane(span, from);
+            before = lane_64(before, from);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                span = w[i] > 0. ? first + i : span;
+            span = __builtin_amdgcn_readlane(span, 63 - __builtin_clzll(__ballot(part > 0.)));
+            before = -INFINITY;
+        }
+        // ---- the block, the token
+        double wb[kSpanBlocks][kE], sum[kSpanBlocks];
+        float z[kSpanBlocks][kE];
+#pragma unroll
+        for (int b = 0; b < kSpanBlocks; ++b)
+            load_block(span * kSpanBlocks + b, z[b]);
+#pragma unroll
+        for (int b = 0; b < kSpanBlocks; ++b) {
+            sum[b] = 0.;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) {
+                wb[b][e] = weight_of(z[b][e], md, f.c);
+                sum[b] += wb[b][e];
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kSpanBlocks; ++b)
+            sum[b] = wave_sum_64(sum[b]);
+        double left = hits ? at - before : INFINITY;
+        int b = -1;
+        double in_block = 0.;
+#pragma unroll
+        for (int k = 0; k < kSpanBlocks; ++k) {
+            if (b < 0 && sum[k] > left) {
+                b = k;
+                in_block = left;
+            }
+            left -= b < 0 ? sum[k] : 0.;
+        }
+        if (b < 0) {
+#pragma unroll
+            for (int k = 0; k < kSpanBlocks; ++k)
+                b = sum[k] > 0. ? k : b;
+            in_block = INFINITY;
+        }
+        float zb[kE];
+        double ws[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            zb[e] = z[0][e];
+            ws[e] = wb[0][e];
+#pragma unroll
+            for (int k = 1; k < kSpanBlocks; ++k) {
+                zb[e] = b == k ? z[k][e] : zb[e];
+                ws[e] = b == k ? wb[k][e] : ws[e];
+            }
+        }
+        pick_in_block(span * kSpanBlocks + b, zb, ws, in_block, total);
+    }
+};
+
+// One wave per row, without a filter.
+template <bool kBf16>
+__global__ __launch_bounds__(64) void k_sample_plain(SampleArgs a, Stats st)
+{
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        RowPicker<kBf16> p(a, row);
+        p.plain(st);
+    }
+}
+
+// One workgroup per row, with filters.
+template <bool kBf16>
+struct Picker : RowPicker<kBf16> {
+    using Base = RowPicker<kBf16>;
+    using Base::a;
+    using Base::answer;
+    using Base::blocks;
+    using Base::f;
+    using Base::index_in;
+    using Base::load_block;
+    using Base::m;
+    using Base::md;
+    using Base::pick_in_block;
+    using Base::r;
+    using Base::row;
+    using Base::u;
+    using Base::vecs;
+    static constexpr int kE = Base::kE;
+    PickLds &s;
+
+    __device__ __forceinline__ Picker(const SampleArgs &args, PickLds &lds, int64_t row_)
+        : Base(args, row_), s(lds)
+    {
     }
 
     // Calls use(j, z) with the 64 vectors of every listed block j, in the waves' turns.
@@ -394,7 +658,7 @@ struct Picker {
                 const int j = j0 + i * kPickWaves;
                 if (j < n) {
                     float z[kE];
-                    Row<kBf16>::unpack(v[i], z);
+                    Row<kBf16>::unpack_whole(v[i], z);
                     use(j, z);
                 }
             }
@@ -418,47 +682,29 @@ struct Picker {
         return (int)n;
     }
 
-    __device__ __forceinline__ void greedy()
-    {
-        if (threadIdx.x == 0)
-            s.found = 0xffffffffu;
-        __syncthreads();
-        for (int b = threadIdx.x; b < blocks; b += kPickThreads)
-            if (s.max[b] == m)
-                atomicMin(&s.found, (uint32_t)b);
-        __syncthreads();
-        if (threadIdx.x < 64) {
-            const int b = (int)s.found;
-            float z[kE];
-            load_block(b, z);
-            uint32_t at = 0xffffffffu;
-#pragma unroll
-            for (int e = kE - 1; e >= 0; --e)
-                at = z[e] == m ? (uint32_t)index_in(b, e) : at;
-            answer((int)wave_min(at), 0.);
-        }
-    }
-
-    // A lower bound of the k-th largest block maximum, exact to its upper 16 key bits (k <= blocks).
+    // A lower bound of the k-th largest block maximum, exact to its upper 16 key bits (k <= blocks): four
+    // bits a round, one of the 15 values that they may have for each wave.
     __device__ __forceinline__ float kth_maximum(int k)
     {
-        if (threadIdx.x < 64) {
-            uint32_t key = 0;
-            for (int bit = 31; bit >= 16; --bit) {
-                const uint32_t t = key | 1u << bit;
-                int n = 0;
-                for (int b0 = 0; b0 < blocks; b0 += 64) {
-                    const int b = b0 + (int)threadIdx.x;
-                    n += __popcll(__ballot(b < blocks && key_of(s.max[b < blocks ? b : 0]) >= t));
-                }
-                key = n >= k ? t : key;
-            }
-            if (threadIdx.x == 0)
-                s.n = key;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        static_assert(kPickWaves == 16, "a wave for each value of four bits");
+        uint32_t key = 0;
+        for (int shift = 28; shift >= 16; shift -= 4) {
+            const uint32_t t = key | (uint32_t)wave << shift;
+            int n = 0;
+            for (int b = lane; b < blocks; b += 64)
+                n += key_of(s.max[b]) >= t ? 1 : 0;
+            const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add((uint32_t)n), 63);
+            if (lane == 0)
+                s.cnt[wave] = total;
+            __syncthreads();
+            uint32_t v = 0;  // the largest value that k blocks reach
+#pragma unroll
+            for (uint32_t w = 1; w < kPickWaves; ++w)
+                v = s.cnt[w] >= (uint32_t)k ? w : v;
+            key |= v << shift;
+            __syncthreads();
         }
-        __syncthreads();
-        const uint32_t key = s.n;
-        __syncthreads();
         // (keys below that of -inf belong to no number)
         return key <= key_of(-INFINITY) ? -INFINITY : logit_of(key);
     }
@@ -470,6 +716,8 @@ struct Picker {
             s.n = 0;
         __syncthreads();
         each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
+            if (*(volatile uint32_t *)&s.n > (uint32_t)kSampleSort)
+                return;
             const int b = s.list[j];
             uint32_t mine = 0;
 #pragma unroll
@@ -495,14 +743,15 @@ struct Picker {
     }
 
     // The whole rest on n collected tokens; whole: the sum over all tokens (without top-k).
+    template <bool kWave>
     __device__ __forceinline__ void finish_sorted(int n, double whole)
     {
         const int t = threadIdx.x;
         int size = pow2_from(n);
-        for (int i = n + t; i < size; i += kPickThreads)
+        for (int i = n + t; i < size; i += kWave ? 64 : kPickThreads)
             s.sort.key[i] = ~0ull;
-        __syncthreads();
-        sort_keys(s.sort.key, size);
+        join<kWave>();
+        sort_keys<kWave>(s.sort.key, size);
         double w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -510,16 +759,16 @@ struct Picker {
             w[i] = j < n ? weight_of(logit_of(~(uint32_t)(s.sort.key[j] >> 32)), md, f.c) : 0.;
         }
         double total;
-        const double incl = block_scan_64(w[0] + w[1], s.red, total);
+        const double incl = block_scan_64<kWave>(w[0] + w[1], s.red, total);
         const double before[2] = {incl - w[1] - w[0], incl - w[1]};
         int keep = f.k && f.k < n ? f.k : n;
-        __syncthreads();
+        join<kWave>();
         if (f.k) {  // the sum over top-k's
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (2 * t + i == keep - 1)
                     s.total = before[i] + w[i];
-            __syncthreads();
+            join<kWave>();
             whole = s.total;
         }
         const double most = (double)f.p * whole;
@@ -533,14 +782,14 @@ struct Picker {
                 s.sort.w[j] = w[i];
         }
         uint32_t kept;
-        block_scan_32(mine, s.cnt, kept);
+        block_scan_32<kWave>(mine, s.cnt, kept);
         keep = (int)kept;  // (the conditions hold for a first part of the order)
         // ---- the kept by index
         uint64_t key[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             key[i] = s.sort.key[2 * t + i < size ? 2 * t + i : 0];
-        __syncthreads();
+        join<kWave>();
         size = pow2_from(keep);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -550,52 +799,239 @@ struct Picker {
         }
         if (t == 0)
             s.found = (uint32_t)keep - 1;
-        __syncthreads();
-        sort_keys(s.sort.key, size);
+        join<kWave>();
+        sort_keys<kWave>(s.sort.key, size);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * t + i;
             w[i] = j < keep ? s.sort.w[(uint32_t)s.sort.key[j]] : 0.;
         }
-        const double run = block_scan_64(w[0] + w[1], s.red, total);
-        const double at = uniform() * total;
+        const double run = block_scan_64<kWave>(w[0] + w[1], s.red, total);
+        const double at = u * total;
         if (2 * t < keep && run - w[1] > at)
             atomicMin(&s.found, (uint32_t)(2 * t));
         else if (2 * t + 1 < keep && run > at)
             atomicMin(&s.found, (uint32_t)(2 * t + 1));
-        __syncthreads();
+        join<kWave>();
         if (t == 0) {
             const uint64_t k = s.sort.key[s.found];
             answer((int)(k >> 32), log(s.sort.w[(uint32_t)k] / total));
         }
     }
 
-    __device__ __forceinline__ double uniform() const
+    // Top-p alone, of more tokens above tau than are sorted.  whole: the sum over all tokens.  False: too many
+    // lie about the border.
+    __device__ __forceinline__ bool finish_located(int n_list, float tau, double whole)
     {
-        const float u = a.uniform[row];
-        return u > 0.f ? fminf(u, 1.f - FLT_EPSILON / 2) : 0.;
+        constexpr uint32_t kBins = kDigits;
+        const int t = threadIdx.x;
+        const float width = (m - tau) * (1.f / ((float)kBins - 0.5f)), per = 1.f / width;
+        const float cf = (float)f.c;
+        if (!(width > 0.f && per < 1e30f && per > 0.f && cf < 1e30f))
+            return false;
+        auto bin_of = [&](float z) -> uint32_t {  // grows as z falls
+            const float x = (m - z) * per;
+            return x < (float)kBins ? (uint32_t)x : kBins;
+        };
+        // ---- fp32 weights in units of 2^-31 of the sum.  A bin's total is off by a unit for each token, and by
+        // the weights' relative error: 2^-23 from the exponential, and three roundings of the exponent, which
+        // is 43 at most above tau (weights of 2^-24 / 2^19 of the sum): 43 ln 2 * 3 * 2^-24 < 2^-17.
+        const float unit = (float)(2147483648. / whole);
+        uint32_t *hist = s.hist.n;
+        hist[t] = hist[t + kPickThreads] = 0;
+        if (t == 0) {
+            s.n = 0;
+            s.found = s.found2 = kBins;
+        }
+        for (int b = t; b < blocks; b += kPickThreads)
+            s.sum[b] = 0.;
+        __syncthreads();
+        each_block(n_list, [&](int, const float(&z)[kE]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < kE; ++e) {
+                const uint32_t bin = bin_of(z[e]);
+                if (bin < kBins)
+                    atomicAdd(&hist[bin], (uint32_t)(__builtin_amdgcn_exp2f((z[e] - m) * cf) * unit));
+            }
+        });
+        __syncthreads();
+        const uint32_t h0 = hist[2 * t], h1 = hist[2 * t + 1];
+        uint32_t total;
+        const uint32_t incl = block_scan_32(h0 + h1, s.cnt, total);
+        const int64_t error = (int64_t)a.vocab + (1 << 14) + 64;
+        const int64_t most_u = (int64_t)((double)f.p * 2147483648.);
+        const int64_t after[2] = {(int64_t)incl - h1, (int64_t)incl};
+        const int64_t in_front[2] = {(int64_t)incl - h1 - h0, (int64_t)incl - h1};
+        // the first bin that may not be kept whole, the first that is surely left out
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (after[i] + error >= most_u)
+                atomicMin(&s.found, (uint32_t)(2 * t + i));
+            if (in_front[i] - error >= most_u)
+                atomicMin(&s.found2, (uint32_t)(2 * t + i));
+        }
+        __syncthreads();
+        const uint32_t b0 = s.found, b1 = s.found2;
+        __syncthreads();
+        // ---- the sums of the kept bins, block by block; the tokens between are sorted
+        each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
+            const int b = s.list[j];
+            uint32_t mine = 0, kept = 0;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) {
+                const uint32_t bin = bin_of(z[e]);
+                kept |= bin < b0 ? 1u << e : 0u;
+                mine |= bin >= b0 && bin < b1 && bin < kBins ? 1u << e : 0u;
+            }
+            if (__ballot(kept != 0)) {
+                double sum = 0.;
+#pragma unroll
+                for (int e = 0; e < kE; ++e)
+                    if (kept >> e & 1) {
+                        const double w = weight_of(z[e], md, f.c);
+                        sum += w >= (double)f.q ? w : 0.;
+                    }
+                sum = wave_sum_64(sum);
+                if ((threadIdx.x & 63) == 0)
+                    s.sum[b] = sum;
+            }
+            if (__ballot(mine != 0) == 0)
+                return;
+            const uint32_t run = wave_scan_add(__popc(mine));
+            uint32_t at = 0;
+            if ((threadIdx.x & 63) == 63)
+                at = atomicAdd(&s.n, run);
+            at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + run - __popc(mine);
+#pragma unroll
+            for (int e = 0; e < kE; ++e)
+                if (mine >> e & 1) {
+                    if (at < (uint32_t)kSampleSort)
+                        s.sort.key[at] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(b, e);
+                    ++at;
+                }
+        });
+        __syncthreads();
+        const int n = (int)s.n;
+        if (n > kSampleSort)
+            return false;
+        // ---- the sums in fixed point (their order no longer matters), and what lies above the border
+        const double unit60 = fixed_unit(whole);
+        const int per_thread = (blocks + kPickThreads - 1) / kPickThreads;
+        const int block0 = min(blocks, t * per_thread), block1 = min(blocks, block0 + per_thread);
+        uint64_t *fixed = reinterpret_cast<uint64_t *>(s.sum);
+        double part = 0., above;
+        for (int b = block0; b < block1; ++b) {
+            part += s.sum[b];
+            fixed[b] = (uint64_t)__builtin_rint(s.sum[b] * unit60);
+        }
+        block_scan_64(part, s.red, above);
+        // ---- the border: its tokens in order, kept while the sum before is below p of the whole
+        const int size = pow2_from(n);
+        for (int i = n + t; i < size; i += kPickThreads)
+            s.sort.key[i] = ~0ull;
+        __syncthreads();
+        sort_keys<false>(s.sort.key, size);
+        double w[2], all;
+        uint64_t key[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = 2 * t + i;
+            key[i] = j < n ? s.sort.key[j] : ~0ull;
+            w[i] = j < n ? weight_of(logit_of(~(uint32_t)(key[i] >> 32)), md, f.c) : 0.;
+        }
+        const double run = block_scan_64(w[0] + w[1], s.red, all);
+        const double before[2] = {above + (run - w[1] - w[0]), above + (run - w[1])};
+        const double most = (double)f.p * whole;
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (2 * t + i < n && before[i] < most && w[i] >= (double)f.q) {
+                ++mine;
+                const int v = ((int)(uint32_t)key[i] + r.off) / kE;
+                atomicAdd(reinterpret_cast<unsigned long long *>(fixed + v / kBlockVecs),
+                          (unsigned long long)__builtin_rint(w[i] * unit60));
+            }
+        uint32_t kept;
+        block_scan_32(mine, s.cnt, kept);
+        __syncthreads();
+        // a border token is kept up to this one: of its key by index (none: no key reaches it)
+        const uint64_t last = kept ? s.sort.key[kept - 1] : 0;
+        const uint32_t last_key = kept ? ~(uint32_t)(last >> 32) : 0xffffffffu, last_id = (uint32_t)last;
+        // ---- the draw: the block, then the token
+        uint64_t mine64 = 0;
+        for (int b = block0; b < block1; ++b)
+            mine64 += fixed[b];
+        uint64_t run64 = scan_u64(mine64) - mine64;
+        if (t == 0)
+            s.found = kMaxBlocks;
+        __syncthreads();
+        const uint64_t all64 = s.d0, at = (uint64_t)(u * (double)all64);
+        uint64_t here = 0;
+        uint32_t hit = kMaxBlocks;
+        for (int b = block0; b < block1; ++b) {
+            if (hit == kMaxBlocks && run64 + fixed[b] > at && fixed[b]) {
+                hit = (uint32_t)b;
+                here = run64;
+            }
+            run64 += fixed[b];
+        }
+        if (hit < kMaxBlocks)
+            atomicMin(&s.found, hit);
+        __syncthreads();
+        if (hit < kMaxBlocks && s.found == hit)
+            s.before = (double)(at - here) / unit60;  // what is left of the draw in this block
+        __syncthreads();
+        if (t >= 64)
+            return true;
+        const int b = (int)s.found;
+        float z[kE];
+        load_block(b, z);
+        double we[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const uint32_t k = key_of(z[e]), bin = bin_of(z[e]);
+            const bool in = bin < b0 || (bin < kBins && (k > last_key ||
+                                         (k == last_key && (uint32_t)index_in(b, e) <= last_id)));
+            const double x = in ? weight_of(z[e], md, f.c) : 0.;
+            we[e] = x >= (double)f.q ? x : 0.;
+        }
+        pick_in_block(b, z, we, s.before, (double)all64 / unit60);
+        return true;
     }
 
-    // The draw among the listed blocks' kept tokens.  whole > 0: the sum over all kept tokens, of which
-    // `skip` lie before the list.
-    __device__ __forceinline__ void draw(int n, const Rule &rule, double whole, double skip)
+    // A power of two that brings a sum to 2^60 .. 2^61.
+    __device__ __forceinline__ static double fixed_unit(double sum)
+    {
+        const int exponent = (int)(__builtin_bit_cast(uint64_t, sum) >> 52) - 1023;
+        return __builtin_ldexp(1., 60 - exponent);
+    }
+
+    // The draw among the listed blocks' kept tokens.
+    __device__ __forceinline__ void draw(int n, const Rule &rule)
     {
         const double tie_w = weight_of(logit_of(rule.key), md, f.c);
         each_block(n, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
             double sum = 0.;
-            uint32_t ties = 0;
+            uint32_t ties = 0, above = 0;
 #pragma unroll
             for (int e = 0; e < kE; ++e) {
                 const uint32_t key = key_of(z[e]);
-                const double w = weight_of(z[e], md, f.c);
-                sum += key > rule.key && w >= rule.q ? w : 0.;
+                above |= key > rule.key ? 1u << e : 0u;
                 ties += key == rule.key ? 1u : 0u;
             }
-            sum = wave_sum_64(sum);
+            if (__ballot(above != 0)) {
+#pragma unroll
+                for (int e = 0; e < kE; ++e)
+                    if (above >> e & 1) {
+                        const double w = weight_of(z[e], md, f.c);
+                        sum += w >= rule.q ? w : 0.;
+                    }
+                sum = wave_sum_64(sum);
+            }
             ties = wave_scan_add(ties);
             if ((threadIdx.x & 63) == 63) {
-                s.draw.sum[j] = sum;
-                s.draw.ties[j] = ties;
+                s.sum[j] = sum;
+                s.ties[j] = ties;
             }
         });
         __syncthreads();
@@ -605,29 +1041,29 @@ struct Picker {
             s.found = 0xffffffffu;
         uint32_t mine = 0, ties;
         for (int j = j0; j < j1; ++j)
-            mine += s.draw.ties[j];
+            mine += s.ties[j];
         uint32_t first = block_scan_32(mine, s.cnt, ties) - mine;
         double part = 0.;
         const bool tie_in = tie_w >= rule.q;
         for (int j = j0; j < j1; ++j) {
-            const uint32_t c = s.draw.ties[j];
+            const uint32_t c = s.ties[j];
             const uint32_t in = tie_in && first < rule.ties ? min(c, rule.ties - first) : 0u;
-            s.draw.sum[j] += in * tie_w;
-            s.draw.ties[j] = in;  // (from here on: the ties of the block that are kept)
+            s.sum[j] += in * tie_w;
+            s.ties[j] = in;  // (from here on: the ties of the block that are kept)
             first += c;
-            part += s.draw.sum[j];
+            part += s.sum[j];
         }
         double total;
         double run = block_scan_64(part, s.red, total) - part;
-        const double at = whole > 0. ? uniform() * whole - skip : uniform() * total;
+        const double at = u * total;
         uint32_t hit = 0xffffffffu;
         double hit_run = 0.;
         for (int j = j0; j < j1; ++j) {
-            if (hit == 0xffffffffu && run + s.draw.sum[j] > at && s.draw.sum[j] > 0.) {
+            if (hit == 0xffffffffu && run + s.sum[j] > at && s.sum[j] > 0.) {
                 hit = (uint32_t)j;
                 hit_run = run;
             }
-            run += s.draw.sum[j];
+            run += s.sum[j];
         }
         if (hit != 0xffffffffu)
             atomicMin(&s.found, hit);
@@ -643,7 +1079,7 @@ struct Picker {
                 s.found = 0;
             __syncthreads();
             for (int j = j0; j < j1; ++j)
-                if (s.draw.sum[j] > 0.)
+                if (s.sum[j] > 0.)
                     atomicMax(&s.found, (uint32_t)j);
             __syncthreads();
         }
@@ -651,44 +1087,22 @@ struct Picker {
             return;
         const int j = (int)s.found, b = s.list[j];
         float z[kE];
-        double w[kE], sum = 0.;
+        double w[kE];
         load_block(b, z);
         uint32_t c = 0;
 #pragma unroll
         for (int e = 0; e < kE; ++e)
             c += key_of(z[e]) == rule.key ? 1u : 0u;
         uint32_t rank = wave_scan_add(c) - c;
-        uint32_t at_e = 0xffffffffu, last_e = 0;
-        bool any = false;
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
             const uint32_t key = key_of(z[e]);
             const double x = weight_of(z[e], md, f.c);
-            const bool keep = key == rule.key ? rank < s.draw.ties[j] : key > rule.key && x >= rule.q;
+            const bool keep = key == rule.key ? rank < s.ties[j] : key > rule.key && x >= rule.q;
             rank += key == rule.key ? 1u : 0u;
             w[e] = keep ? x : 0.;
-            sum += w[e];
-            last_e = w[e] > 0. ? (uint32_t)e : last_e;
-            any = any || w[e] > 0.;
         }
-        double here = s.before + (wave_scan_64(sum) - sum);
-#pragma unroll
-        for (int e = 0; e < kE; ++e) {
-            here += w[e];
-            if (at_e == 0xffffffffu && w[e] > 0. && here > at)
-                at_e = (uint32_t)e;
-        }
-        const uint64_t hits = last ? 0 : __ballot(at_e != 0xffffffffu);
-        const uint64_t some = __ballot(any);  // (the block's sum is above 0)
-        const int lane = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(some);
-        const uint32_t el = hits ? at_e : last_e;
-        float zt = z[0];
-#pragma unroll
-        for (int e = 1; e < kE; ++e)
-            zt = el == (uint32_t)e ? z[e] : zt;
-        zt = __shfl(zt, lane, 64);
-        const int token = __shfl(index_in(b, (int)el), lane, 64);
-        answer(token, ((double)zt - md) / f.t - log(whole > 0. ? whole : total));
+        pick_in_block(b, z, w, last ? INFINITY : at - s.before, total);
     }
 
     // ---- thresholds by digits of the keys, for more candidates than are sorted
@@ -813,8 +1227,7 @@ struct Picker {
             __syncthreads();
         }
         // a power of two that brings the sum to 2^60 .. 2^61: weights lose 2^-61 of it each
-        const int exponent = (int)(__builtin_bit_cast(uint64_t, whole) >> 52) - 1023;
-        const double unit = __builtin_ldexp(1., 60 - exponent);
+        const double unit = fixed_unit(whole);
         Rule rule{low, 0xffffffffu, (double)f.q};
         double most = whole * unit;
         for (int by_count = f.k ? 1 : 0; by_count >= (f.p < 1.f ? 0 : 1); --by_count) {
@@ -829,6 +1242,11 @@ struct Picker {
 
     __device__ __forceinline__ void run(const Stats &st)
     {
+        if (f.greedy || (f.k == 0 && f.p >= 1.f && !(f.q > 0.f))) {
+            if (threadIdx.x < 64)
+                this->plain(st);
+            return;
+        }
         const int64_t first = row * st.spans;
         float top = -INFINITY;
         for (int b = threadIdx.x; b < blocks; b += kPickThreads) {
@@ -836,9 +1254,11 @@ struct Picker {
             s.max[b] = x;
             top = fmaxf(top, x);
         }
+        const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
+        const double mine = f.k == 0 && t < spans ? st.sums[first + t] : 0.;
         top = wave_max_f(top);
-        if ((threadIdx.x & 63) == 0)
-            s.cnt[threadIdx.x >> 6] = __float_as_uint(top);
+        if ((t & 63) == 0)
+            s.cnt[t >> 6] = __float_as_uint(top);
         __syncthreads();
         m = -INFINITY;
 #pragma unroll
@@ -850,72 +1270,47 @@ struct Picker {
             answer(-1, -INFINITY);
             return;
         }
-        if (f.greedy) {
-            greedy();
-            return;
-        }
-        int n_list = 0;
         double whole = 0.;
-        const bool plain = f.k == 0 && f.p >= 1.f && !(f.q > 0.f);
-        if (f.k == 0) {
-            // ---- a span's sum per thread, brought to the row's maximum
-            const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
+        if (f.k == 0) {  // a span's sum per thread, brought to the row's maximum
             double x = 0.;
-            if (t < spans) {
+            if (mine > 0.) {
                 float sm = s.max[kSpanBlocks * t];
                 for (int b = 1; b < kSpanBlocks; ++b)
                     if (kSpanBlocks * t + b < blocks)
                         sm = fmaxf(sm, s.max[kSpanBlocks * t + b]);
-                if (sm > -INFINITY)
-                    x = st.sums[first + t] * weight_of(sm, md, f.c);
+                x = mine * weight_of(sm, md, f.c);
             }
-            const double incl = block_scan_64(x, s.red, whole);
-            if (plain) {  // one span holds the token
-                const double at = uniform() * whole;
-                if (t == 0) {
-                    s.found = 0xffffffffu;
-                    s.n = 0;
-                }
-                __syncthreads();
-                if (x > 0.) {
-                    if (incl > at)
-                        atomicMin(&s.found, (uint32_t)t);
-                    atomicMax(&s.n, (uint32_t)t);
-                }
-                __syncthreads();
-                const uint32_t hit = s.found == 0xffffffffu ? s.n : s.found;
-                if ((uint32_t)t == hit)
-                    s.total = incl - x;
-                if (t < kSpanBlocks)
-                    s.list[t] = (uint16_t)(kSpanBlocks * hit + t);
-                n_list = min(kSpanBlocks, blocks - kSpanBlocks * (int)hit);
-            }
+            block_scan_64(x, s.red, whole);
             __syncthreads();
         }
-        Rule rule{0u, 0xffffffffu, (double)f.q};
-        if (!plain) {
-            // ---- a bound that every kept token reaches (and what top-p's sum is over)
-            float tau = -INFINITY;
-            if (f.k) {
-                if (f.k <= blocks)
-                    tau = kth_maximum(f.k);
-            } else if (f.p < 1.f) {
-                tau = below(md + log((1. - (double)f.p) * whole / a.vocab) * f.t);
-            }
-            if (f.q > 0.f && !(f.k && f.p < 1.f))
-                tau = fmaxf(tau, below(md + log((double)f.q) * f.t));
-            n_list = list_blocks(tau);
-            if (f.k || f.p < 1.f) {
-                const int n = collect(n_list, tau);
-                if (n <= kSampleSort) {
-                    finish_sorted(n, whole);
-                    return;
-                }
-                __syncthreads();
-                rule = cut_by_digits(n_list, tau, whole);
-            }
+        // ---- a bound that every kept token reaches (and what top-p's sum is over)
+        float tau = -INFINITY;
+        if (f.k) {
+            if (f.k <= blocks)
+                tau = kth_maximum(f.k);
+        } else if (f.p < 1.f) {
+            tau = below(md + log((1. - (double)f.p) * whole / a.vocab) * f.t);
         }
-        draw(n_list, rule, plain ? whole : 0., plain ? s.total : 0.);
+        if (f.q > 0.f && !(f.k && f.p < 1.f))
+            tau = fmaxf(tau, below(md + log((double)f.q) * f.t));
+        const int n_list = list_blocks(tau);
+        Rule rule{0u, 0xffffffffu, (double)f.q};
+        if (f.k || f.p < 1.f) {
+            const int n = collect(n_list, tau);
+            if (n <= kSampleSort) {
+                if (n > 128)
+                    finish_sorted<false>(n, whole);
+                else if (t < 64)
+                    finish_sorted<true>(n, whole);
+                return;
+            }
+            __syncthreads();
+            if (f.k == 0 && finish_located(n_list, tau, whole))
+                return;
+            __syncthreads();
+            rule = cut_by_digits(n_list, tau, whole);
+        }
+        draw(n_list, rule);
     }
 
     // A float below a bound by more than the bound's own error (NaN: none).
@@ -965,8 +1360,12 @@ hipError_t launch_sample(const SampleArgs &a, void *workspace, hipStream_t strea
     if (e != hipSuccess)
         return e;
     blocks = a.rows < kSampleGrid ? a.rows : kSampleGrid;
-    hipLaunchKernelGGL(a.bf16 ? k_sample_pick<true> : k_sample_pick<false>, dim3((unsigned)blocks),
-                       dim3(kPickThreads), 0, stream, a, st);
+    if (!a.top_k && !a.top_p && !a.min_p)
+        hipLaunchKernelGGL(a.bf16 ? k_sample_plain<true> : k_sample_plain<false>,
+                           dim3((unsigned)blocks), dim3(64), 0, stream, a, st);
+    else
+        hipLaunchKernelGGL(a.bf16 ? k_sample_pick<true> : k_sample_pick<false>, dim3((unsigned)blocks),
+                           dim3(kPickThreads), 0, stream, a, st);
     return hipGetLastError();
 }
 
