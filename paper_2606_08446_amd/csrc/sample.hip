@@ -9,17 +9,19 @@
 // orders that depend on the sizes alone.
 //
 // k_sample_stats reads the rows once: the maximum of every 64 vectors (a block), and where it may be asked
-// for the sum of the weights of every 256 (a span), relative to their own maximum.  The second kernel
-// finds from these which blocks can hold a kept token and reads only them:
-//   no filter     one wave per row: the span that holds the token, then its block (k_sample_plain)
+// for the sum of the weights of every 256 (a span), relative to their own maximum.  The other kernels
+// find from these which blocks can hold a kept token and read only them:
+//   no filter     the span that holds the token, then its block
 //   min-p         the blocks that reach m + T ln q: their sums, then one block
 //   top-k         the k-th largest block maximum bounds the last kept logit from below: the tokens above,
 //                 hardly more than k, are sorted in LDS
-//   top-p         a weight of (1 - p) / vocab of the whole bounds it: up to 2048 tokens above are
-//                 sorted; more are located first, by fp32 weights summed in 2048 bins of equal width whose
+//   top-p         a weight of (1 - p) / vocab of the whole bounds it: up to 1024 tokens above are
+//                 sorted; more are located first, by fp32 weights summed in 1024 bins of equal width whose
 //                 error is bounded, so that the tokens of a bin or two are sorted and all above them
 //                 are summed
-//   else          (large top-k, many ties) the border is found by 11-bit digits of the keys
+//   else          (large top-k, many ties) the border is found by 10-bit digits of the keys
+// k_sample_narrow, one wave per row with no barrier to wait at, does what takes at most 64 blocks and 128
+// tokens; the other rows are left to a workgroup each, k_sample_wide.
 #include "common.h"
 #include "sample.h"
 #include "wave.h"
@@ -31,18 +33,20 @@ namespace {
 
 constexpr int kStatThreads = 256;
 constexpr int kStatWaves = kStatThreads / 64;
+constexpr int kStatBlocks = 2048;  // workgroups that keep the device full
 constexpr int kBlockVecs = 64;  // a wave's load
 constexpr int kSpanBlocks = 4;
 constexpr int kSpanVecs = kBlockVecs * kSpanBlocks;
-constexpr int kPickThreads = 1024;
+constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / 64;
-constexpr int kSampleSort = 2048;
-constexpr int kDigitBits = 11;
+constexpr int kSampleSort = 1024;  // tokens that a workgroup sorts, and
+constexpr int kWaveSort = 128;     // a wave
+constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kMaxSpans = (kSampleMaxVocab / 4 + 1 + kSpanVecs - 1) / kSpanVecs;
 constexpr int kMaxBlocks = kMaxSpans * kSpanBlocks;
 constexpr int kSampleGrid = 1 << 20;  // workgroups at most
-static_assert(kMaxSpans <= kPickThreads, "a thread holds one span");
+static_assert(kMaxSpans <= 2 * kPickThreads, "a thread holds two spans");
 static_assert(kSampleSort == 2 * kPickThreads && kDigits == 2 * kPickThreads, "two per thread");
 constexpr double kLog2e = 1.44269504088896340736;
 
@@ -89,14 +93,21 @@ struct Row {
             }
         return x;
     }
+    // whether vectors [v, v + n) lie inside the row
+    __device__ __forceinline__ bool inside(int v, int n) const
+    {
+        return index(v, 0) >= 0 && index(v + n, 0) <= vocab;
+    }
+    __device__ __forceinline__ u32x4_t load_inside(int v) const { return ld16(base + (int64_t)v * 16); }
     // its logits: NaN counts as masked
     __device__ static __forceinline__ void unpack(u32x4_t v, float (&z)[kElems<kBf16>])
     {
 #pragma unroll
         for (int e = 0; e < kElems<kBf16>; ++e) {
-            float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
+            const float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
                             : __uint_as_float(v[e & 3]);
-            z[e] = f != f ? -INFINITY : f;
+            // (the median of a NaN is the least of the others; the builtin becomes two instructions)
+            asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z[e]) : "v"(f), "v"(INFINITY), "v"(-INFINITY));
         }
     }
     // and +inf as the largest number, -0 as 0
@@ -125,9 +136,12 @@ __device__ __forceinline__ double exp2_fast(double d, double c)
     p = fma(p, f, 0.2402265069581299);
     p = fma(p, f, 0.6931471805599453);
     p = fma(p, f, 1.);
-    const uint64_t b = __builtin_bit_cast(uint64_t, p);
-    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, s);
-    return __builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) + (n << 20)) << 32 | (uint32_t)b);
+    // (in one instruction of 32 bits; the compiler makes five of 64 of it)
+    u32x2_t b = __builtin_bit_cast(u32x2_t, p);
+    asm("v_lshl_add_u32 %0, %1, 20, %2"
+        : "=v"(b[1])
+        : "v"(__builtin_bit_cast(u32x2_t, s)[0]), "v"(b[1]));
+    return __builtin_bit_cast(double, b);
 }
 
 // 2^(d c) for any d <= 0, c >= 0: 0 below 2^-1000, and for a product that is no number.
@@ -215,46 +229,103 @@ struct Filters {
 struct Stats {
     double *sums;  // [rows][spans] weights of a span relative to its maximum
     float *maxima; // [rows][spans][kSpanBlocks]
+    int32_t *wide; // [rows] whether k_sample_wide has a row to do
     int spans;     // of a row, at most
 };
 
+// max without the canonical forms that the compiler makes of numbers which might be signalling NaNs (med3
+// has left none).
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(x), "v"(y), "v"(z));
+    return d;
+}
+
+// The maxima of four values over the wave, left in lane 63: the four scans take turns, so that no move reads
+// what one of the last two instructions wrote.  A lane without a source keeps its value.
+__device__ __forceinline__ void wave_max4(float (&x)[4])
+{
+#define SPARROW_MAX4(move)                                             \
+    "v_max_f32_dpp %0, %0, %0 " move "\n v_max_f32_dpp %1, %1, %1 " move \
+    "\n v_max_f32_dpp %2, %2, %2 " move "\n v_max_f32_dpp %3, %3, %3 " move "\n "
+    asm("s_nop 1\n " SPARROW_MAX4("row_shr:1 row_mask:0xf bank_mask:0xf")
+        SPARROW_MAX4("row_shr:2 row_mask:0xf bank_mask:0xf")
+        SPARROW_MAX4("row_shr:4 row_mask:0xf bank_mask:0xf")
+        SPARROW_MAX4("row_shr:8 row_mask:0xf bank_mask:0xf")
+        SPARROW_MAX4("row_bcast:15 row_mask:0xa bank_mask:0xf")
+        SPARROW_MAX4("row_bcast:31 row_mask:0xc bank_mask:0xf")
+        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+#undef SPARROW_MAX4
+}
+
+// The waves of a row's workgroups (blockIdx.y) take its spans in turn, the next one's loads under way.
+// Bound by arithmetic where sums are wanted (19 operations a logit, 15 of them fp64), else by memory.
 template <bool kBf16>
 __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Stats st)
 {
     constexpr int kE = kElems<kBf16>;
     const int lane = threadIdx.x & 63;
-    const int64_t all = a.rows * st.spans;
-    for (int64_t w = (int64_t)blockIdx.x * kStatWaves +
-                     __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-         w < all; w += (int64_t)gridDim.x * kStatWaves) {
-        const int64_t row = w / st.spans;
-        const int span = (int)(w - row * st.spans);
+    const int first = blockIdx.x * kStatWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int step = gridDim.x * kStatWaves;
+    if (first >= st.spans)
+        return;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const Row<kBf16> r(a, row);
+        const Filters f(a, row);
+        const bool sums = f.sums();
         const int vecs = r.vecs();
         u32x4_t v[kSpanBlocks];
+        auto load = [&](int span) __attribute__((always_inline)) {
+            if (r.inside(span * kSpanVecs, kSpanVecs)) {
 #pragma unroll
-        for (int b = 0; b < kSpanBlocks; ++b)
-            v[b] = r.load(min(span * kSpanVecs + b * kBlockVecs + lane, vecs));  // (vecs: nothing)
-        const Filters f(a, row);
-        float z[kSpanBlocks][kE], top[kSpanBlocks], m = -INFINITY;
+                for (int b = 0; b < kSpanBlocks; ++b)
+                    v[b] = r.load_inside(span * kSpanVecs + b * kBlockVecs + lane);
+            } else {
+#pragma unroll 1
+                for (int b = 0; b < kSpanBlocks; ++b) {
+                    const u32x4_t x = r.load(min(span * kSpanVecs + b * kBlockVecs + lane, vecs));
 #pragma unroll
-        for (int b = 0; b < kSpanBlocks; ++b) {
-            Row<kBf16>::unpack(v[b], z[b]);
-            top[b] = z[b][0];
+                    for (int k = 0; k < kSpanBlocks; ++k)
+                        v[k] = b == k ? x : v[k];
+                }
+            }
+        };
+        load(first);
+        for (int span = first; span < st.spans; span += step) {
+            float z[kSpanBlocks][kE], top[kSpanBlocks];
 #pragma unroll
-            for (int e = 1; e < kE; ++e)
-                top[b] = fmaxf(top[b], z[b][e]);
-            top[b] = fminf(wave_max_f(top[b]), FLT_MAX);
-            m = fmaxf(m, top[b]);
-        }
-        if (lane < kSpanBlocks) {
-            float t = top[0];
+            for (int b = 0; b < kSpanBlocks; ++b) {
+                // (here, not behind the loads: the wait for them would come along)
+                asm volatile("" : "+v"(v[b]));
+                Row<kBf16>::unpack(v[b], z[b]);
+            }
+            if (span + step < st.spans)
+                load(span + step);
 #pragma unroll
-            for (int b = 1; b < kSpanBlocks; ++b)
-                t = lane == b ? top[b] : t;
-            st.maxima[w * kSpanBlocks + lane] = t;
-        }
-        if (f.sums()) {
+            for (int b = 0; b < kSpanBlocks; ++b) {
+                top[b] = z[b][0];
+#pragma unroll
+                for (int e = 1; e + 1 < kE; e += 2)
+                    top[b] = max3(top[b], z[b][e], z[b][e + 1]);
+                top[b] = max3(top[b], z[b][kE - 1], top[b]);
+            }
+            wave_max4(top);
+#pragma unroll
+            for (int b = 0; b < kSpanBlocks; ++b)
+                top[b] = fminf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top[b]), 63)),
+                               FLT_MAX);
+            const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            const int64_t at = row * st.spans + span;
+            if (lane < kSpanBlocks) {
+                float t = top[0];
+#pragma unroll
+                for (int b = 1; b < kSpanBlocks; ++b)
+                    t = lane == b ? top[b] : t;
+                st.maxima[at * kSpanBlocks + lane] = t;
+            }
+            if (!sums)
+                continue;
             double sum = 0.;
             if (m > -INFINITY) {
                 const double md = m;
@@ -267,7 +338,7 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
                     for (int b = 0; b < kSpanBlocks; ++b)
 #pragma unroll
                         for (int e = 0; e < kE; ++e)
-                            sum += exp2_fast((double)fminf(fmaxf(z[b][e], low), m) - md, f.c);
+                            sum += exp2_fast((double)__builtin_amdgcn_fmed3f(z[b][e], low, m) - md, f.c);
                 } else {
 #pragma unroll 1
                     for (int b = 0; b < kSpanBlocks; ++b)
@@ -283,7 +354,7 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
             }
             sum = wave_sum_64(sum);
             if (lane == 0)
-                st.sums[w] = sum;
+                st.sums[at] = sum;
         }
     }
 }
@@ -293,7 +364,7 @@ struct PickLds {
     uint16_t list[kMaxBlocks];   // blocks that may hold a kept token
     double sum[kMaxBlocks];      // weights kept in a block, or in a listed one
     double red[kPickWaves];
-    uint32_t cnt[kPickWaves];
+    uint32_t cnt[kPickWaves], reach[16];
     uint32_t n;                  // a counter, a result
     uint32_t found, found2;
     double total, before;
@@ -311,6 +382,18 @@ struct PickLds {
     };
 };
 static_assert(sizeof(PickLds) <= 64 << 10, "LDS of a workgroup");
+
+struct NarrowLds {
+    uint16_t list[64];
+    uint32_t found;
+    double total;
+    double *red;     // (a wave's scans need neither)
+    uint32_t *cnt;
+    struct {
+        uint64_t key[kWaveSort];
+        double w[kWaveSort];
+    } sort;
+};
 
 // The threads that work together: the workgroup, or its first wave alone (whose LDS accesses are in
 // order by themselves).
@@ -474,63 +557,80 @@ struct RowPicker {
         answer(__shfl(index_in(b, (int)el), lane, 64), ((double)zt - md) / f.t - log(total));
     }
 
-    // The draw without a filter, or the largest logit.  A lane holds neighbouring spans.
-    __device__ __forceinline__ void plain(const Stats &st)
+    static constexpr int kPer = (kMaxSpans + 63) / 64;  // spans of a lane at most, neighbouring ones
+
+    // A wave's lanes take the row's spans: maxima of their blocks and of each, sums where there are any; m.
+    __device__ __forceinline__ void load_stats(const Stats &st, u32x4_t (&max4)[kPer], float (&top)[kPer],
+                                               double (&w)[kPer])
     {
-        constexpr int kPer = (kMaxSpans + 63) / 64;
-        const int lane = threadIdx.x & 63, per = (st.spans + 63) / 64, first = lane * per;
+        const int per = (st.spans + 63) / 64, first = (threadIdx.x & 63) * per;
         const float *maxima = st.maxima + row * st.spans * kSpanBlocks;
-        float top[kPer];
-        double w[kPer];
+        constexpr uint32_t kNone = 0xff800000u;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            top[i] = -INFINITY;
+            max4[i] = (u32x4_t){kNone, kNone, kNone, kNone};
             w[i] = 0.;
             if (i < per && first + i < st.spans) {
-                const u32x4_t x = ld16(maxima + (first + i) * kSpanBlocks);
-                top[i] = fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
-                               fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
-                if (!f.greedy)
+                max4[i] = ld16(maxima + (first + i) * kSpanBlocks);
+                if (f.sums())
                     w[i] = st.sums[row * st.spans + first + i];
             }
         }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            top[i] = fmaxf(fmaxf(__uint_as_float(max4[i][0]), __uint_as_float(max4[i][1])),
+                           fmaxf(__uint_as_float(max4[i][2]), __uint_as_float(max4[i][3])));
         float t = top[0];
 #pragma unroll
         for (int i = 1; i < kPer; ++i)
             t = fmaxf(t, top[i]);
         m = wave_max_f(t);
         md = m;
-        if (!(m > -INFINITY)) {  // every token is masked
-            answer(-1, -INFINITY);
-            return;
-        }
-        if (f.greedy) {
-            int span = 0;
+    }
+
+    // The largest logit's token, the draw without a filter.
+    __device__ __forceinline__ void greedy(const Stats &st, const float (&top)[kPer])
+    {
+        const int per = (st.spans + 63) / 64, first = (threadIdx.x & 63) * per;
+        const float *maxima = st.maxima + row * st.spans * kSpanBlocks;
+        int span = -1;
 #pragma unroll
-            for (int i = kPer - 1; i >= 0; --i)
-                span = top[i] == m ? first + i : span;
-            span = __builtin_amdgcn_readlane(span, __builtin_ctzll(__ballot(t == m)));
-            int b = kSpanBlocks - 1;
+        for (int i = kPer - 1; i >= 0; --i)
+            span = top[i] == m ? first + i : span;
+        span = __builtin_amdgcn_readlane(span, __builtin_ctzll(__ballot(span >= 0)));
+        int b = kSpanBlocks - 1;
 #pragma unroll
-            for (int i = kSpanBlocks - 2; i >= 0; --i)
-                b = maxima[span * kSpanBlocks + i] == m ? i : b;
-            b += span * kSpanBlocks;
-            float z[kE];
-            load_block(b, z);
-            uint32_t at = 0xffffffffu;
+        for (int i = kSpanBlocks - 2; i >= 0; --i)
+            b = maxima[span * kSpanBlocks + i] == m ? i : b;
+        b += span * kSpanBlocks;
+        float z[kE];
+        load_block(b, z);
+        uint32_t at = 0xffffffffu;
 #pragma unroll
-            for (int e = kE - 1; e >= 0; --e)
-                at = z[e] == m ? (uint32_t)index_in(b, e) : at;
-            answer((int)wave_min(at), 0.);
-            return;
-        }
-        double part = 0.;
+        for (int e = kE - 1; e >= 0; --e)
+            at = z[e] == m ? (uint32_t)index_in(b, e) : at;
+        answer((int)wave_min(at), 0.);
+    }
+
+    // The spans' sums brought to the row's maximum; the lanes' parts; their sum.
+    __device__ __forceinline__ double whole_sum(const float (&top)[kPer], double (&w)[kPer], double &incl,
+                                                double &part) const
+    {
+        part = 0.;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             w[i] = w[i] > 0. ? w[i] * weight_of(top[i], md, f.c) : 0.;
             part += w[i];
         }
-        const double incl = wave_scan_64(part), total = lane_64(incl, 63), at = u * total;
+        incl = wave_scan_64(part);
+        return lane_64(incl, 63);
+    }
+
+    __device__ __forceinline__ void plain(const Stats &st, const double (&w)[kPer], double incl, double part,
+                                          double total)
+    {
+        const int per = (st.spans + 63) / 64, first = (threadIdx.x & 63) * per;
+        const double at = u * total;
         // ---- the span: the first at which the running sum exceeds it (by rounding none: the last)
         double run = incl - part, before = 0.;
         int span = -1;
@@ -605,18 +705,8 @@ struct RowPicker {
     }
 };
 
-// One wave per row, without a filter.
-template <bool kBf16>
-__global__ __launch_bounds__(64) void k_sample_plain(SampleArgs a, Stats st)
-{
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        RowPicker<kBf16> p(a, row);
-        p.plain(st);
-    }
-}
-
-// One workgroup per row, with filters.
-template <bool kBf16>
+// One row with filters, by a wave or a workgroup with its LDS.
+template <bool kBf16, typename Lds>
 struct Picker : RowPicker<kBf16> {
     using Base = RowPicker<kBf16>;
     using Base::a;
@@ -632,10 +722,10 @@ struct Picker : RowPicker<kBf16> {
     using Base::row;
     using Base::u;
     using Base::vecs;
-    static constexpr int kE = Base::kE;
-    PickLds &s;
+    static constexpr int kE = Base::kE, kPer = Base::kPer;
+    Lds &s;
 
-    __device__ __forceinline__ Picker(const SampleArgs &args, PickLds &lds, int64_t row_)
+    __device__ __forceinline__ Picker(const SampleArgs &args, Lds &lds, int64_t row_)
         : Base(args, row_), s(lds)
     {
     }
@@ -644,7 +734,7 @@ struct Picker : RowPicker<kBf16> {
     template <typename Use>
     __device__ __forceinline__ void each_block(int n, Use use)
     {
-        constexpr int kAhead = 4;
+        constexpr int kAhead = 8;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
         for (int j0 = wave; j0 < n; j0 += kAhead * kPickWaves) {
             u32x4_t v[kAhead];
@@ -683,30 +773,156 @@ struct Picker : RowPicker<kBf16> {
     }
 
     // A lower bound of the k-th largest block maximum, exact to its upper 16 key bits (k <= blocks): four
-    // bits a round, one of the 15 values that they may have for each wave.
+    // bits a round, two of the 16 values that they may have for each wave.
     __device__ __forceinline__ float kth_maximum(int k)
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        static_assert(kPickWaves == 16, "a wave for each value of four bits");
+        static_assert(2 * kPickWaves == 16, "two values of four bits a wave");
         uint32_t key = 0;
         for (int shift = 28; shift >= 16; shift -= 4) {
-            const uint32_t t = key | (uint32_t)wave << shift;
-            int n = 0;
-            for (int b = lane; b < blocks; b += 64)
-                n += key_of(s.max[b]) >= t ? 1 : 0;
-            const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add((uint32_t)n), 63);
-            if (lane == 0)
-                s.cnt[wave] = total;
+            const uint32_t t0 = key | (uint32_t)(2 * wave) << shift, t1 = t0 | 1u << shift;
+            uint32_t n = 0;  // (blocks, at most 2^16 - 1, that reach one and the other)
+            for (int b = lane; b < blocks; b += 64) {
+                const uint32_t x = key_of(s.max[b]);
+                n += (x >= t0 ? 1u : 0u) + (x >= t1 ? 1u << 16 : 0u);
+            }
+            n = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(n), 63);
+            if (lane == 0) {
+                s.reach[2 * wave] = n & 0xffffu;
+                s.reach[2 * wave + 1] = n >> 16;
+            }
             __syncthreads();
             uint32_t v = 0;  // the largest value that k blocks reach
 #pragma unroll
-            for (uint32_t w = 1; w < kPickWaves; ++w)
-                v = s.cnt[w] >= (uint32_t)k ? w : v;
+            for (uint32_t w = 1; w < 16; ++w)
+                v = s.reach[w] >= (uint32_t)k ? w : v;
             key |= v << shift;
             __syncthreads();
         }
-        // (keys below that of -inf belong to no number)
+        return bound_of(key);
+    }
+
+    // The logit of a bound's key (one below that of -inf belongs to no number).
+    __device__ __forceinline__ static float bound_of(uint32_t key)
+    {
         return key <= key_of(-INFINITY) ? -INFINITY : logit_of(key);
+    }
+
+    // The same bound by one wave, from the lanes' maxima; bit by bit.
+    __device__ __forceinline__ static float kth_of(const u32x4_t (&max4)[kPer], int per, int k)
+    {
+        uint32_t key = 0;
+        for (int bit = 31; bit >= 16; --bit) {
+            const uint32_t t = key | 1u << bit;
+            uint32_t n = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (i < per)
+#pragma unroll
+                    for (int j = 0; j < kSpanBlocks; ++j)
+                        n += key_of(__uint_as_float(max4[i][j])) >= t ? 1u : 0u;
+            n = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(n), 63);
+            key = n >= (uint32_t)k ? t : key;
+        }
+        return bound_of(key);
+    }
+
+    // A bound that every token kept reaches (and what top-p's sum is over); kth: that of top-k's blocks.
+    __device__ __forceinline__ float bound(double whole, float kth) const
+    {
+        float tau = -INFINITY;
+        if (f.k)
+            tau = kth;
+        else if (f.p < 1.f)
+            tau = below(md + log((1. - (double)f.p) * whole / a.vocab) * f.t);
+        if (f.q > 0.f && !(f.k && f.p < 1.f))
+            tau = fmaxf(tau, below(md + log((double)f.q) * f.t));
+        return tau;
+    }
+
+    // The row by one wave; false: it takes more than that.
+    __device__ __forceinline__ bool narrow(const Stats &st)
+    {
+        u32x4_t max4[kPer];
+        float top[kPer];
+        double w[kPer], whole = 0., incl = 0., part = 0.;
+        const int lane = threadIdx.x & 63, per = (st.spans + 63) / 64;
+        this->load_stats(st, max4, top, w);
+        if (!(m > -INFINITY)) {  // every token is masked
+            answer(-1, -INFINITY);
+            return true;
+        }
+        if (f.greedy) {
+            this->greedy(st, top);
+            return true;
+        }
+        if (f.k == 0)
+            whole = this->whole_sum(top, w, incl, part);
+        if (f.k == 0 && f.p >= 1.f) {
+            if (f.q > 0.f)
+                return false;
+            this->plain(st, w, incl, part, whole);
+            return true;
+        }
+        if (f.k > kWaveSort)
+            return false;
+        const float tau = bound(whole, f.k <= blocks ? kth_of(max4, per, f.k) : -INFINITY);
+        // ---- the blocks that reach it, in any order
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+#pragma unroll
+            for (int j = 0; j < kSpanBlocks; ++j) {
+                const float x = __uint_as_float(max4[i][j]);
+                mine += x >= tau && x > -INFINITY ? 1u : 0u;
+            }
+        uint32_t at = wave_scan_add(mine);
+        const int n_list = __builtin_amdgcn_readlane((int)at, 63);
+        if (n_list > 64)
+            return false;
+        at -= mine;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+#pragma unroll
+            for (int j = 0; j < kSpanBlocks; ++j) {
+                const float x = __uint_as_float(max4[i][j]);
+                if (x >= tau && x > -INFINITY)
+                    s.list[at++] = (uint16_t)((lane * per + i) * kSpanBlocks + j);
+            }
+        join<true>();
+        // ---- the tokens that do
+        constexpr int kAhead = 8;
+        int n = 0;
+        for (int j0 = 0; j0 < n_list; j0 += kAhead) {
+            u32x4_t v[kAhead];
+            int id[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                id[i] = __builtin_amdgcn_readfirstlane(s.list[min(j0 + i, n_list - 1)]);
+                v[i] = r.load(min(id[i] * kBlockVecs + lane, vecs));
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                float z[kE];
+                Row<kBf16>::unpack_whole(v[i], z);
+#pragma unroll
+                for (int e = 0; e < kE; ++e) {
+                    const bool in = j0 + i < n_list && z[e] >= tau && z[e] > -INFINITY;
+                    const uint64_t lanes = __ballot(in);
+                    if (lanes == 0)
+                        continue;
+                    const int place = n + __popcll(lanes & ((1ull << lane) - 1));
+                    if (in && place < kWaveSort)
+                        s.sort.key[place] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(id[i], e);
+                    n += __popcll(lanes);
+                }
+            }
+            if (n > kWaveSort)
+                return false;
+        }
+        join<true>();
+        finish_sorted<true>(n, whole);
+        return true;
     }
 
     // Tokens of at least tau into the sorting LDS, any order; their number (more than fit: not all).
@@ -1240,22 +1456,17 @@ struct Picker : RowPicker<kBf16> {
         return rule;
     }
 
-    __device__ __forceinline__ void run(const Stats &st)
+    // The row by a workgroup.
+    __device__ __forceinline__ void wide(const Stats &st)
     {
-        if (f.greedy || (f.k == 0 && f.p >= 1.f && !(f.q > 0.f))) {
-            if (threadIdx.x < 64)
-                this->plain(st);
-            return;
-        }
         const int64_t first = row * st.spans;
+        const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
         float top = -INFINITY;
-        for (int b = threadIdx.x; b < blocks; b += kPickThreads) {
+        for (int b = t; b < blocks; b += kPickThreads) {
             const float x = st.maxima[first * kSpanBlocks + b];
             s.max[b] = x;
             top = fmaxf(top, x);
         }
-        const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
-        const double mine = f.k == 0 && t < spans ? st.sums[first + t] : 0.;
         top = wave_max_f(top);
         if ((t & 63) == 0)
             s.cnt[t >> 6] = __float_as_uint(top);
@@ -1266,51 +1477,36 @@ struct Picker : RowPicker<kBf16> {
             m = fmaxf(m, __uint_as_float(s.cnt[w]));
         md = m;
         __syncthreads();
-        if (!(m > -INFINITY)) {  // every token is masked
-            answer(-1, -INFINITY);
-            return;
-        }
         double whole = 0.;
-        if (f.k == 0) {  // a span's sum per thread, brought to the row's maximum
+        if (f.k == 0) {  // the spans' sums, brought to the row's maximum
             double x = 0.;
-            if (mine > 0.) {
-                float sm = s.max[kSpanBlocks * t];
+            for (int i = t; i < spans; i += kPickThreads) {
+                float sm = s.max[kSpanBlocks * i];
                 for (int b = 1; b < kSpanBlocks; ++b)
-                    if (kSpanBlocks * t + b < blocks)
-                        sm = fmaxf(sm, s.max[kSpanBlocks * t + b]);
-                x = mine * weight_of(sm, md, f.c);
+                    if (kSpanBlocks * i + b < blocks)
+                        sm = fmaxf(sm, s.max[kSpanBlocks * i + b]);
+                const double sum = st.sums[first + i];
+                x += sum > 0. ? sum * weight_of(sm, md, f.c) : 0.;
             }
             block_scan_64(x, s.red, whole);
             __syncthreads();
         }
-        // ---- a bound that every kept token reaches (and what top-p's sum is over)
-        float tau = -INFINITY;
-        if (f.k) {
-            if (f.k <= blocks)
-                tau = kth_maximum(f.k);
-        } else if (f.p < 1.f) {
-            tau = below(md + log((1. - (double)f.p) * whole / a.vocab) * f.t);
-        }
-        if (f.q > 0.f && !(f.k && f.p < 1.f))
-            tau = fmaxf(tau, below(md + log((double)f.q) * f.t));
+        const float tau = bound(whole, f.k && f.k <= blocks ? kth_maximum(f.k) : -INFINITY);
         const int n_list = list_blocks(tau);
-        Rule rule{0u, 0xffffffffu, (double)f.q};
-        if (f.k || f.p < 1.f) {
-            const int n = collect(n_list, tau);
-            if (n <= kSampleSort) {
-                if (n > 128)
-                    finish_sorted<false>(n, whole);
-                else if (t < 64)
-                    finish_sorted<true>(n, whole);
-                return;
-            }
-            __syncthreads();
-            if (f.k == 0 && finish_located(n_list, tau, whole))
-                return;
-            __syncthreads();
-            rule = cut_by_digits(n_list, tau, whole);
+        if (f.k == 0 && f.p >= 1.f) {
+            draw(n_list, Rule{0u, 0xffffffffu, (double)f.q});
+            return;
         }
-        draw(n_list, rule);
+        const int n = collect(n_list, tau);
+        if (n <= kSampleSort) {
+            finish_sorted<false>(n, whole);
+            return;
+        }
+        __syncthreads();
+        if (f.k == 0 && finish_located(n_list, tau, whole))
+            return;
+        __syncthreads();
+        draw(n_list, cut_by_digits(n_list, tau, whole));
     }
 
     // A float below a bound by more than the bound's own error (NaN: none).
@@ -1322,14 +1518,28 @@ struct Picker : RowPicker<kBf16> {
 };
 
 template <bool kBf16>
-__global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a, Stats st)
+__global__ __launch_bounds__(64) void k_sample_narrow(SampleArgs a, Stats st)
+{
+    __shared__ NarrowLds s;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        Picker<kBf16, NarrowLds> p(a, s, row);
+        const bool done = p.narrow(st);
+        if (threadIdx.x == 0)
+            st.wide[row] = done ? 0 : 1;
+        join<true>();  // the LDS is written again
+    }
+}
+
+template <bool kBf16>
+__global__ __launch_bounds__(kPickThreads) void k_sample_wide(SampleArgs a, Stats st)
 {
     __shared__ PickLds s;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        Picker<kBf16> p(a, s, row);
-        p.run(st);
-        if (row + gridDim.x < a.rows)
-            __syncthreads();  // the LDS is written again
+        if (st.wide[row] == 0)
+            continue;
+        Picker<kBf16, PickLds> p(a, s, row);
+        p.wide(st);
+        __syncthreads();  // the LDS is written again
     }
 }
 
@@ -1343,29 +1553,35 @@ int sample_spans(int vocab, bool bf16)
 
 size_t sample_workspace(int64_t rows, int vocab, bool bf16)
 {
-    return (size_t)rows * sample_spans(vocab, bf16) * (sizeof(double) + kSpanBlocks * sizeof(float));
+    return (size_t)rows * (sample_spans(vocab, bf16) * (sizeof(double) + kSpanBlocks * sizeof(float)) +
+                           sizeof(int32_t));
 }
 
 hipError_t launch_sample(const SampleArgs &a, void *workspace, hipStream_t stream)
 {
     const int spans = sample_spans(a.vocab, a.bf16);
-    const Stats st{static_cast<double *>(workspace),
-                   reinterpret_cast<float *>(static_cast<double *>(workspace) + a.rows * spans),
-                   spans};
-    int64_t blocks = (a.rows * spans + kStatWaves - 1) / kStatWaves;
-    blocks = blocks < kSampleGrid ? blocks : kSampleGrid;
-    hipLaunchKernelGGL(a.bf16 ? k_sample_stats<true> : k_sample_stats<false>, dim3((unsigned)blocks),
-                       dim3(kStatThreads), 0, stream, a, st);
-    const hipError_t e = hipGetLastError();
+    const int64_t all = a.rows * spans;
+    float *maxima = static_cast<float *>(workspace);  // (16-byte aligned, a span's four in one load)
+    double *sums = reinterpret_cast<double *>(maxima + all * kSpanBlocks);
+    const Stats st{sums, maxima, reinterpret_cast<int32_t *>(sums + all), spans};
+    // a wave for each span where they are few, else as many as keep the device full
+    const int groups = (spans + kStatWaves - 1) / kStatWaves;
+    const int64_t want = (kStatBlocks + a.rows - 1) / a.rows;
+    const int per_row = (int)(want < groups ? want : groups);
+    hipLaunchKernelGGL(a.bf16 ? k_sample_stats<true> : k_sample_stats<false>,
+                       dim3(per_row, (unsigned)(a.rows < 65535 ? a.rows : 65535)), dim3(kStatThreads), 0,
+                       stream, a, st);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    blocks = a.rows < kSampleGrid ? a.rows : kSampleGrid;
-    if (!a.top_k && !a.top_p && !a.min_p)
-        hipLaunchKernelGGL(a.bf16 ? k_sample_plain<true> : k_sample_plain<false>,
-                           dim3((unsigned)blocks), dim3(64), 0, stream, a, st);
-    else
-        hipLaunchKernelGGL(a.bf16 ? k_sample_pick<true> : k_sample_pick<false>, dim3((unsigned)blocks),
-                           dim3(kPickThreads), 0, stream, a, st);
+    const int64_t blocks = a.rows < kSampleGrid ? a.rows : kSampleGrid;
+    hipLaunchKernelGGL(a.bf16 ? k_sample_narrow<true> : k_sample_narrow<false>, dim3((unsigned)blocks),
+                       dim3(64), 0, stream, a, st);
+    e = hipGetLastError();
+    if (e != hipSuccess || (!a.top_k && !a.top_p && !a.min_p))
+        return e;
+    hipLaunchKernelGGL(a.bf16 ? k_sample_wide<true> : k_sample_wide<false>, dim3((unsigned)blocks),
+                       dim3(kPickThreads), 0, stream, a, st);
     return hipGetLastError();
 }
 
