@@ -15,18 +15,22 @@
 //   min-p         the blocks that reach m + T ln q: their sums, then one block
 //   top-k         the k-th largest block maximum bounds the last kept logit from below: the tokens above,
 //                 hardly more than k, are sorted in LDS
-//   top-p         a weight of (1 - p) / vocab of the whole bounds it: up to 1024 tokens above are
-//                 sorted; more are located first, by fp32 weights summed in 1024 bins of equal width whose
-//                 error is bounded, so that the tokens of a bin or two are sorted and all above them
-//                 are summed
+//   top-p         a weight of (1 - p) / vocab of the whole bounds it: tokens of up to 128 blocks, if they are
+//                 no more than 1024, are sorted; others are located first, by fp32 weights summed in
+//                 1024 bins of equal width whose error is bounded, so that the tokens of a bin or two are
+//                 sorted and all above them are summed (an issue of fp64 instructions on one CU: 50 us of
+//                 90 for 151936 tokens)
 //   else          (large top-k, many ties) the border is found by 10-bit digits of the keys
-// k_sample_narrow, one wave per row with no barrier to wait at, does what takes at most 64 blocks and 128
-// tokens; the other rows are left to a workgroup each, k_sample_wide.
+// k_sample_plain does the rows of a call without filters, a wave each with no barrier to wait at; k_sample_pick
+// all rows of other calls, a workgroup each of 8 waves.  Its steps are short and wait for one another: 512
+// threads, whose registers hold them, took 20 us for one row of 151936 with top-20, 1024 took 26 (their
+// 128 registers spill), and a wave for the rows with few tokens before a workgroup for the others 25.
 #include "common.h"
 #include "sample.h"
 #include "wave.h"
 
 #include <cfloat>
+#include <type_traits>
 
 namespace sparrow {
 namespace {
@@ -39,14 +43,13 @@ constexpr int kSpanBlocks = 4;
 constexpr int kSpanVecs = kBlockVecs * kSpanBlocks;
 constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / 64;
-constexpr int kSampleSort = 1024;  // tokens that a workgroup sorts, and
-constexpr int kWaveSort = 128;     // a wave
+constexpr int kSampleSort = 1024;  // tokens that a workgroup sorts
+constexpr int kFewBlocks = 128;    // of which their number is seen by collecting them
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kMaxSpans = (kSampleMaxVocab / 4 + 1 + kSpanVecs - 1) / kSpanVecs;
 constexpr int kMaxBlocks = kMaxSpans * kSpanBlocks;
 constexpr int kSampleGrid = 1 << 20;  // workgroups at most
-static_assert(kMaxSpans <= 2 * kPickThreads, "a thread holds two spans");
 static_assert(kSampleSort == 2 * kPickThreads && kDigits == 2 * kPickThreads, "two per thread");
 constexpr double kLog2e = 1.44269504088896340736;
 
@@ -99,6 +102,23 @@ struct Row {
         return index(v, 0) >= 0 && index(v + n, 0) <= vocab;
     }
     __device__ __forceinline__ u32x4_t load_inside(int v) const { return ld16(base + (int64_t)v * 16); }
+    // Block b's vectors by the wave's lanes, in two steps so that several blocks' loads are under way at once:
+    // one load without a branch, of the nearest vector that is inside the row, and what the two blocks
+    // at the row's ends take beside it.  (A row of no whole vector: all in the second step.)
+    __device__ __forceinline__ u32x4_t block_begin(int b) const
+    {
+        constexpr int kE = kElems<kBf16>;
+        const int lo = off ? 1 : 0, hi = (vocab + off) / kE - 1;  // whole vectors
+        if (hi < lo)
+            return (u32x4_t){0u, 0u, 0u, 0u};
+        return load_inside(min(max(b * kBlockVecs + (int)(threadIdx.x & 63), lo), hi));
+    }
+    __device__ __forceinline__ u32x4_t block_end(int b, u32x4_t x) const
+    {
+        if (!inside(b * kBlockVecs, kBlockVecs))
+            x = load(min(b * kBlockVecs + (int)(threadIdx.x & 63), vecs()));  // (vecs(): nothing)
+        return x;
+    }
     // its logits: NaN counts as masked
     __device__ static __forceinline__ void unpack(u32x4_t v, float (&z)[kElems<kBf16>])
     {
@@ -224,12 +244,12 @@ struct Filters {
         greedy = !(temp > 0.f) || k == 1 || !(p > 0.f);
     }
     __device__ __forceinline__ bool sums() const { return !greedy && k == 0; }
+    __device__ __forceinline__ bool filtered() const { return !greedy && (k || p < 1.f || q > 0.f); }
 };
 
 struct Stats {
     double *sums;  // [rows][spans] weights of a span relative to its maximum
     float *maxima; // [rows][spans][kSpanBlocks]
-    int32_t *wide; // [rows] whether k_sample_wide has a row to do
     int spans;     // of a row, at most
 };
 
@@ -383,43 +403,12 @@ struct PickLds {
 };
 static_assert(sizeof(PickLds) <= 64 << 10, "LDS of a workgroup");
 
-struct NarrowLds {
-    uint16_t list[64];
-    uint32_t found;
-    double total;
-    double *red;     // (a wave's scans need neither)
-    uint32_t *cnt;
-    struct {
-        uint64_t key[kWaveSort];
-        double w[kWaveSort];
-    } sort;
-};
-
-// The threads that work together: the workgroup, or its first wave alone (whose LDS accesses are in
-// order by themselves).
-template <bool kWave>
-__device__ __forceinline__ void join()
-{
-    if (kWave) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    } else {
-        __syncthreads();
-    }
-}
-
 // Sums over the workgroup's threads in their order: inclusive scan and the total.  The LDS is free
 // again after the caller's next barrier.
-template <bool kWave = false>
 __device__ __forceinline__ double block_scan_64(double x, double *red, double &total)
 {
     const int wave = threadIdx.x >> 6;
     x = wave_scan_64(x);
-    if (kWave) {
-        total = lane_64(x, 63);
-        return x;
-    }
     if ((threadIdx.x & 63) == 63)
         red[wave] = x;
     __syncthreads();
@@ -433,15 +422,10 @@ __device__ __forceinline__ double block_scan_64(double x, double *red, double &t
     return base + x;
 }
 
-template <bool kWave = false>
 __device__ __forceinline__ uint32_t block_scan_32(uint32_t x, uint32_t *cnt, uint32_t &total)
 {
     const int wave = threadIdx.x >> 6;
     x = wave_scan_add(x);
-    if (kWave) {
-        total = (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
-        return x;
-    }
     if ((threadIdx.x & 63) == 63)
         cnt[wave] = x;
     __syncthreads();
@@ -456,7 +440,6 @@ __device__ __forceinline__ uint32_t block_scan_32(uint32_t x, uint32_t *cnt, uin
 }
 
 // Ascending bitonic sort of size (a power of two, at most two per thread) keys.
-template <bool kWave>
 __device__ __forceinline__ void sort_keys(uint64_t *key, int size)
 {
     const int t = threadIdx.x;
@@ -470,8 +453,17 @@ __device__ __forceinline__ void sort_keys(uint64_t *key, int size)
                     key[i + j] = a;
                 }
             }
-            join<kWave>();
+            __syncthreads();
         }
+}
+
+// The first of the threads' pairs that `even` or `odd` holds for, into *found unless less is there; one
+// atomic of a wave.
+__device__ __forceinline__ void first_of(uint32_t *found, bool even, bool odd)
+{
+    const uint64_t hits = __ballot(even || odd);
+    if (hits && (int)(threadIdx.x & 63) == __builtin_ctzll(hits))
+        atomicMin(found, 2 * threadIdx.x + (even ? 0u : 1u));
 }
 
 __device__ __forceinline__ int pow2_from(int n)
@@ -518,7 +510,7 @@ struct RowPicker {
 
     __device__ __forceinline__ void load_block(int b, float (&z)[kE]) const
     {
-        Row<kBf16>::unpack_whole(r.load(min(b * kBlockVecs + (int)(threadIdx.x & 63), vecs)), z);
+        Row<kBf16>::unpack_whole(r.block_end(b, r.block_begin(b)), z);
     }
     __device__ __forceinline__ int index_in(int b, int e) const
     {
@@ -703,10 +695,27 @@ struct RowPicker {
         }
         pick_in_block(span * kSpanBlocks + b, zb, ws, in_block, total);
     }
+
+    // The row, which has no filter, by a wave.
+    __device__ __forceinline__ void simple(const Stats &st)
+    {
+        u32x4_t max4[kPer];
+        float top[kPer];
+        double w[kPer], incl, part;
+        load_stats(st, max4, top, w);
+        if (!(m > -INFINITY)) {  // every token is masked
+            answer(-1, -INFINITY);
+        } else if (f.greedy) {
+            greedy(st, top);
+        } else {
+            const double total = whole_sum(top, w, incl, part);
+            plain(st, w, incl, part, total);
+        }
+    }
 };
 
-// One row with filters, by a wave or a workgroup with its LDS.
-template <bool kBf16, typename Lds>
+// One row, by a workgroup with its LDS.
+template <bool kBf16>
 struct Picker : RowPicker<kBf16> {
     using Base = RowPicker<kBf16>;
     using Base::a;
@@ -723,32 +732,36 @@ struct Picker : RowPicker<kBf16> {
     using Base::u;
     using Base::vecs;
     static constexpr int kE = Base::kE, kPer = Base::kPer;
-    Lds &s;
+    PickLds &s;
 
-    __device__ __forceinline__ Picker(const SampleArgs &args, Lds &lds, int64_t row_)
+    __device__ __forceinline__ Picker(const SampleArgs &args, PickLds &lds, int64_t row_)
         : Base(args, row_), s(lds)
     {
     }
 
     // Calls use(j, z) with the 64 vectors of every listed block j, in the waves' turns.
-    template <typename Use>
+    // kStop: until s.n tells of more tokens than are sorted.
+    template <bool kStop = false, typename Use>
     __device__ __forceinline__ void each_block(int n, Use use)
     {
         constexpr int kAhead = 8;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         for (int j0 = wave; j0 < n; j0 += kAhead * kPickWaves) {
+            if (kStop && *(volatile uint32_t *)&s.n > (uint32_t)kSampleSort)
+                break;
             u32x4_t v[kAhead];
+            int id[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int j = min(j0 + i * kPickWaves, n - 1);
-                v[i] = r.load(min((int)s.list[j] * kBlockVecs + lane, vecs));
+                id[i] = __builtin_amdgcn_readfirstlane(s.list[min(j0 + i * kPickWaves, n - 1)]);
+                v[i] = r.block_begin(id[i]);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int j = j0 + i * kPickWaves;
                 if (j < n) {
                     float z[kE];
-                    Row<kBf16>::unpack_whole(v[i], z);
+                    Row<kBf16>::unpack_whole(r.block_end(id[i], v[i]), z);
                     use(j, z);
                 }
             }
@@ -808,25 +821,6 @@ struct Picker : RowPicker<kBf16> {
         return key <= key_of(-INFINITY) ? -INFINITY : logit_of(key);
     }
 
-    // The same bound by one wave, from the lanes' maxima; bit by bit.
-    __device__ __forceinline__ static float kth_of(const u32x4_t (&max4)[kPer], int per, int k)
-    {
-        uint32_t key = 0;
-        for (int bit = 31; bit >= 16; --bit) {
-            const uint32_t t = key | 1u << bit;
-            uint32_t n = 0;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < per)
-#pragma unroll
-                    for (int j = 0; j < kSpanBlocks; ++j)
-                        n += key_of(__uint_as_float(max4[i][j])) >= t ? 1u : 0u;
-            n = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(n), 63);
-            key = n >= (uint32_t)k ? t : key;
-        }
-        return bound_of(key);
-    }
-
     // A bound that every token kept reaches (and what top-p's sum is over); kth: that of top-k's blocks.
     __device__ __forceinline__ float bound(double whole, float kth) const
     {
@@ -840,100 +834,13 @@ struct Picker : RowPicker<kBf16> {
         return tau;
     }
 
-    // The row by one wave; false: it takes more than that.
-    __device__ __forceinline__ bool narrow(const Stats &st)
-    {
-        u32x4_t max4[kPer];
-        float top[kPer];
-        double w[kPer], whole = 0., incl = 0., part = 0.;
-        const int lane = threadIdx.x & 63, per = (st.spans + 63) / 64;
-        this->load_stats(st, max4, top, w);
-        if (!(m > -INFINITY)) {  // every token is masked
-            answer(-1, -INFINITY);
-            return true;
-        }
-        if (f.greedy) {
-            this->greedy(st, top);
-            return true;
-        }
-        if (f.k == 0)
-            whole = this->whole_sum(top, w, incl, part);
-        if (f.k == 0 && f.p >= 1.f) {
-            if (f.q > 0.f)
-                return false;
-            this->plain(st, w, incl, part, whole);
-            return true;
-        }
-        if (f.k > kWaveSort)
-            return false;
-        const float tau = bound(whole, f.k <= blocks ? kth_of(max4, per, f.k) : -INFINITY);
-        // ---- the blocks that reach it, in any order
-        uint32_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-#pragma unroll
-            for (int j = 0; j < kSpanBlocks; ++j) {
-                const float x = __uint_as_float(max4[i][j]);
-                mine += x >= tau && x > -INFINITY ? 1u : 0u;
-            }
-        uint32_t at = wave_scan_add(mine);
-        const int n_list = __builtin_amdgcn_readlane((int)at, 63);
-        if (n_list > 64)
-            return false;
-        at -= mine;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-#pragma unroll
-            for (int j = 0; j < kSpanBlocks; ++j) {
-                const float x = __uint_as_float(max4[i][j]);
-                if (x >= tau && x > -INFINITY)
-                    s.list[at++] = (uint16_t)((lane * per + i) * kSpanBlocks + j);
-            }
-        join<true>();
-        // ---- the tokens that do
-        constexpr int kAhead = 8;
-        int n = 0;
-        for (int j0 = 0; j0 < n_list; j0 += kAhead) {
-            u32x4_t v[kAhead];
-            int id[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                id[i] = __builtin_amdgcn_readfirstlane(s.list[min(j0 + i, n_list - 1)]);
-                v[i] = r.load(min(id[i] * kBlockVecs + lane, vecs));
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                float z[kE];
-                Row<kBf16>::unpack_whole(v[i], z);
-#pragma unroll
-                for (int e = 0; e < kE; ++e) {
-                    const bool in = j0 + i < n_list && z[e] >= tau && z[e] > -INFINITY;
-                    const uint64_t lanes = __ballot(in);
-                    if (lanes == 0)
-                        continue;
-                    const int place = n + __popcll(lanes & ((1ull << lane) - 1));
-                    if (in && place < kWaveSort)
-                        s.sort.key[place] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(id[i], e);
-                    n += __popcll(lanes);
-                }
-            }
-            if (n > kWaveSort)
-                return false;
-        }
-        join<true>();
-        finish_sorted<true>(n, whole);
-        return true;
-    }
-
     // Tokens of at least tau into the sorting LDS, any order; their number (more than fit: not all).
     __device__ __forceinline__ int collect(int n_list, float tau)
     {
         if (threadIdx.x == 0)
             s.n = 0;
         __syncthreads();
-        each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
-            if (*(volatile uint32_t *)&s.n > (uint32_t)kSampleSort)
-                return;
+        each_block<true>(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
             const int b = s.list[j];
             uint32_t mine = 0;
 #pragma unroll
@@ -959,15 +866,14 @@ struct Picker : RowPicker<kBf16> {
     }
 
     // The whole rest on n collected tokens; whole: the sum over all tokens (without top-k).
-    template <bool kWave>
     __device__ __forceinline__ void finish_sorted(int n, double whole)
     {
         const int t = threadIdx.x;
         int size = pow2_from(n);
-        for (int i = n + t; i < size; i += kWave ? 64 : kPickThreads)
+        for (int i = n + t; i < size; i += kPickThreads)
             s.sort.key[i] = ~0ull;
-        join<kWave>();
-        sort_keys<kWave>(s.sort.key, size);
+        __syncthreads();
+        sort_keys(s.sort.key, size);
         double w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -975,16 +881,16 @@ struct Picker : RowPicker<kBf16> {
             w[i] = j < n ? weight_of(logit_of(~(uint32_t)(s.sort.key[j] >> 32)), md, f.c) : 0.;
         }
         double total;
-        const double incl = block_scan_64<kWave>(w[0] + w[1], s.red, total);
+        const double incl = block_scan_64(w[0] + w[1], s.red, total);
         const double before[2] = {incl - w[1] - w[0], incl - w[1]};
         int keep = f.k && f.k < n ? f.k : n;
-        join<kWave>();
+        __syncthreads();
         if (f.k) {  // the sum over top-k's
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (2 * t + i == keep - 1)
                     s.total = before[i] + w[i];
-            join<kWave>();
+            __syncthreads();
             whole = s.total;
         }
         const double most = (double)f.p * whole;
@@ -998,14 +904,14 @@ struct Picker : RowPicker<kBf16> {
                 s.sort.w[j] = w[i];
         }
         uint32_t kept;
-        block_scan_32<kWave>(mine, s.cnt, kept);
+        block_scan_32(mine, s.cnt, kept);
         keep = (int)kept;  // (the conditions hold for a first part of the order)
         // ---- the kept by index
         uint64_t key[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             key[i] = s.sort.key[2 * t + i < size ? 2 * t + i : 0];
-        join<kWave>();
+        __syncthreads();
         size = pow2_from(keep);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -1015,20 +921,17 @@ struct Picker : RowPicker<kBf16> {
         }
         if (t == 0)
             s.found = (uint32_t)keep - 1;
-        join<kWave>();
-        sort_keys<kWave>(s.sort.key, size);
+        __syncthreads();
+        sort_keys(s.sort.key, size);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * t + i;
             w[i] = j < keep ? s.sort.w[(uint32_t)s.sort.key[j]] : 0.;
         }
-        const double run = block_scan_64<kWave>(w[0] + w[1], s.red, total);
+        const double run = block_scan_64(w[0] + w[1], s.red, total);
         const double at = u * total;
-        if (2 * t < keep && run - w[1] > at)
-            atomicMin(&s.found, (uint32_t)(2 * t));
-        else if (2 * t + 1 < keep && run > at)
-            atomicMin(&s.found, (uint32_t)(2 * t + 1));
-        join<kWave>();
+        first_of(&s.found, 2 * t < keep && run - w[1] > at, 2 * t + 1 < keep && run > at);
+        __syncthreads();
         if (t == 0) {
             const uint64_t k = s.sort.key[s.found];
             answer((int)(k >> 32), log(s.sort.w[(uint32_t)k] / total));
@@ -1043,7 +946,11 @@ struct Picker : RowPicker<kBf16> {
         const int t = threadIdx.x;
         const float width = (m - tau) * (1.f / ((float)kBins - 0.5f)), per = 1.f / width;
         const float cf = (float)f.c;
-        if (!(width > 0.f && per < 1e30f && per > 0.f && cf < 1e30f))
+        // (a logit of `low` has a weight that no sum feels, but one that exp2_fast takes)
+        const float low = (float)(md - 1000. / f.c);
+        const double low_t = ((double)low - md) * f.c;
+        if (!(width > 0.f && per < 1e30f && per > 0.f && cf < 1e30f && low > -INFINITY && low < tau &&
+              low_t >= -1019. && low_t <= -900.))
             return false;
         auto bin_of = [&](float z) -> uint32_t {  // grows as z falls
             const float x = (m - z) * per;
@@ -1079,53 +986,59 @@ struct Picker : RowPicker<kBf16> {
         const int64_t after[2] = {(int64_t)incl - h1, (int64_t)incl};
         const int64_t in_front[2] = {(int64_t)incl - h1 - h0, (int64_t)incl - h1};
         // the first bin that may not be kept whole, the first that is surely left out
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (after[i] + error >= most_u)
-                atomicMin(&s.found, (uint32_t)(2 * t + i));
-            if (in_front[i] - error >= most_u)
-                atomicMin(&s.found2, (uint32_t)(2 * t + i));
-        }
+        first_of(&s.found, after[0] + error >= most_u, after[1] + error >= most_u);
+        first_of(&s.found2, in_front[0] - error >= most_u, in_front[1] - error >= most_u);
         __syncthreads();
         const uint32_t b0 = s.found, b1 = s.found2;
         __syncthreads();
         // ---- the sums of the kept bins, block by block; the tokens between are sorted
-        each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
-            const int b = s.list[j];
-            uint32_t mine = 0, kept = 0;
+        const float x0 = (float)b0, x1 = (float)b1;  // (bin < b: x < b)
+        auto kept_sums = [&](auto min_p) __attribute__((always_inline)) {
+            each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
+                const int b = s.list[j];
+                float x[kE];
+                bool some = false, between = false;
 #pragma unroll
-            for (int e = 0; e < kE; ++e) {
-                const uint32_t bin = bin_of(z[e]);
-                kept |= bin < b0 ? 1u << e : 0u;
-                mine |= bin >= b0 && bin < b1 && bin < kBins ? 1u << e : 0u;
-            }
-            if (__ballot(kept != 0)) {
-                double sum = 0.;
+                for (int e = 0; e < kE; ++e) {
+                    x[e] = (m - z[e]) * per;
+                    some |= x[e] < x0;
+                    between |= x[e] >= x0 && x[e] < x1;
+                }
+                if (__ballot(some)) {
+                    double sum = 0.;
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) {
+                        const double w = exp2_fast((double)(x[e] < x0 ? z[e] : low) - md, f.c);
+                        sum += !min_p() || w >= (double)f.q ? w : 0.;
+                    }
+                    sum = wave_sum_64(sum);
+                    if ((threadIdx.x & 63) == 0)
+                        s.sum[b] = sum;
+                }
+                if (__ballot(between) == 0)
+                    return;
+                uint32_t mine = 0;
 #pragma unroll
                 for (int e = 0; e < kE; ++e)
-                    if (kept >> e & 1) {
-                        const double w = weight_of(z[e], md, f.c);
-                        sum += w >= (double)f.q ? w : 0.;
-                    }
-                sum = wave_sum_64(sum);
-                if ((threadIdx.x & 63) == 0)
-                    s.sum[b] = sum;
-            }
-            if (__ballot(mine != 0) == 0)
-                return;
-            const uint32_t run = wave_scan_add(__popc(mine));
-            uint32_t at = 0;
-            if ((threadIdx.x & 63) == 63)
-                at = atomicAdd(&s.n, run);
-            at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + run - __popc(mine);
+                    mine += x[e] >= x0 && x[e] < x1 ? 1u : 0u;
+                const uint32_t run = wave_scan_add(mine);
+                uint32_t at = 0;
+                if ((threadIdx.x & 63) == 63)
+                    at = atomicAdd(&s.n, run);
+                at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + run - mine;
 #pragma unroll
-            for (int e = 0; e < kE; ++e)
-                if (mine >> e & 1) {
-                    if (at < (uint32_t)kSampleSort)
-                        s.sort.key[at] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(b, e);
-                    ++at;
-                }
-        });
+                for (int e = 0; e < kE; ++e)
+                    if (x[e] >= x0 && x[e] < x1) {
+                        if (at < (uint32_t)kSampleSort)
+                            s.sort.key[at] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(b, e);
+                        ++at;
+                    }
+            });
+        };
+        if (f.q > 0.f)
+            kept_sums(std::true_type{});
+        else
+            kept_sums(std::false_type{});
         __syncthreads();
         const int n = (int)s.n;
         if (n > kSampleSort)
@@ -1146,7 +1059,7 @@ struct Picker : RowPicker<kBf16> {
         for (int i = n + t; i < size; i += kPickThreads)
             s.sort.key[i] = ~0ull;
         __syncthreads();
-        sort_keys<false>(s.sort.key, size);
+        sort_keys(s.sort.key, size);
         double w[2], all;
         uint64_t key[2];
 #pragma unroll
@@ -1367,10 +1280,8 @@ struct Picker : RowPicker<kBf16> {
             const uint32_t incl_n = block_scan_32(n0 + n1, s.cnt, total_n);
             const uint64_t incl_w = scan_u64(w0 + w1);
             const uint64_t bn = seen_n + incl_n - n1 - n0, bw = seen_w + incl_w - w1 - w0;
-            if (n0 && (by_count ? bn + n0 >= want : bw + w0 >= want))
-                atomicMin(&s.found, (uint32_t)i);
-            else if (n1 && (by_count ? bn + n0 + n1 >= want : bw + w0 + w1 >= want))
-                atomicMin(&s.found, (uint32_t)i + 1);
+            first_of(&s.found, n0 && (by_count ? bn + n0 >= want : bw + w0 >= want),
+                     n1 && (by_count ? bn + n0 + n1 >= want : bw + w0 + w1 >= want));
             __syncthreads();
             const uint32_t bin = s.found;
             if (bin == 0xffffffffu) {
@@ -1456,8 +1367,7 @@ struct Picker : RowPicker<kBf16> {
         return rule;
     }
 
-    // The row by a workgroup.
-    __device__ __forceinline__ void wide(const Stats &st)
+    __device__ __forceinline__ void pick(const Stats &st)
     {
         const int64_t first = row * st.spans;
         const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
@@ -1477,6 +1387,10 @@ struct Picker : RowPicker<kBf16> {
             m = fmaxf(m, __uint_as_float(s.cnt[w]));
         md = m;
         __syncthreads();
+        if (!(m > -INFINITY)) {  // every token is masked
+            answer(-1, -INFINITY);
+            return;
+        }
         double whole = 0.;
         if (f.k == 0) {  // the spans' sums, brought to the row's maximum
             double x = 0.;
@@ -1497,15 +1411,22 @@ struct Picker : RowPicker<kBf16> {
             draw(n_list, Rule{0u, 0xffffffffu, (double)f.q});
             return;
         }
+        if (f.k == 0 && n_list > kFewBlocks) {
+            if (finish_located(n_list, tau, whole))
+                return;
+            __syncthreads();
+        }
         const int n = collect(n_list, tau);
         if (n <= kSampleSort) {
-            finish_sorted<false>(n, whole);
+            finish_sorted(n, whole);
             return;
         }
         __syncthreads();
-        if (f.k == 0 && finish_located(n_list, tau, whole))
-            return;
-        __syncthreads();
+        if (f.k == 0 && n_list <= kFewBlocks) {
+            if (finish_located(n_list, tau, whole))
+                return;
+            __syncthreads();
+        }
         draw(n_list, cut_by_digits(n_list, tau, whole));
     }
 
@@ -1517,28 +1438,28 @@ struct Picker : RowPicker<kBf16> {
     }
 };
 
+// Rows without top-k, top-p and min-p: a wave each, with no barrier to wait at.
 template <bool kBf16>
-__global__ __launch_bounds__(64) void k_sample_narrow(SampleArgs a, Stats st)
+__global__ __launch_bounds__(64) void k_sample_plain(SampleArgs a, Stats st)
 {
-    __shared__ NarrowLds s;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        Picker<kBf16, NarrowLds> p(a, s, row);
-        const bool done = p.narrow(st);
-        if (threadIdx.x == 0)
-            st.wide[row] = done ? 0 : 1;
-        join<true>();  // the LDS is written again
+        RowPicker<kBf16> p(a, row);
+        p.simple(st);
     }
 }
 
 template <bool kBf16>
-__global__ __launch_bounds__(kPickThreads) void k_sample_wide(SampleArgs a, Stats st)
+__global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a, Stats st)
 {
     __shared__ PickLds s;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        if (st.wide[row] == 0)
+        Picker<kBf16> p(a, s, row);
+        if (!p.f.filtered()) {
+            if (threadIdx.x < 64)
+                p.simple(st);
             continue;
-        Picker<kBf16, PickLds> p(a, s, row);
-        p.wide(st);
+        }
+        p.pick(st);
         __syncthreads();  // the LDS is written again
     }
 }
@@ -1553,8 +1474,7 @@ int sample_spans(int vocab, bool bf16)
 
 size_t sample_workspace(int64_t rows, int vocab, bool bf16)
 {
-    return (size_t)rows * (sample_spans(vocab, bf16) * (sizeof(double) + kSpanBlocks * sizeof(float)) +
-                           sizeof(int32_t));
+    return (size_t)rows * sample_spans(vocab, bf16) * (sizeof(double) + kSpanBlocks * sizeof(float));
 }
 
 hipError_t launch_sample(const SampleArgs &a, void *workspace, hipStream_t stream)
@@ -1563,7 +1483,7 @@ hipError_t launch_sample(const SampleArgs &a, void *workspace, hipStream_t strea
     const int64_t all = a.rows * spans;
     float *maxima = static_cast<float *>(workspace);  // (16-byte aligned, a span's four in one load)
     double *sums = reinterpret_cast<double *>(maxima + all * kSpanBlocks);
-    const Stats st{sums, maxima, reinterpret_cast<int32_t *>(sums + all), spans};
+    const Stats st{sums, maxima, spans};
     // a wave for each span where they are few, else as many as keep the device full
     const int groups = (spans + kStatWaves - 1) / kStatWaves;
     const int64_t want = (kStatBlocks + a.rows - 1) / a.rows;
@@ -1575,13 +1495,12 @@ hipError_t launch_sample(const SampleArgs &a, void *workspace, hipStream_t strea
     if (e != hipSuccess)
         return e;
     const int64_t blocks = a.rows < kSampleGrid ? a.rows : kSampleGrid;
-    hipLaunchKernelGGL(a.bf16 ? k_sample_narrow<true> : k_sample_narrow<false>, dim3((unsigned)blocks),
-                       dim3(64), 0, stream, a, st);
-    e = hipGetLastError();
-    if (e != hipSuccess || (!a.top_k && !a.top_p && !a.min_p))
-        return e;
-    hipLaunchKernelGGL(a.bf16 ? k_sample_wide<true> : k_sample_wide<false>, dim3((unsigned)blocks),
-                       dim3(kPickThreads), 0, stream, a, st);
+    if (a.top_k || a.top_p || a.min_p)
+        hipLaunchKernelGGL(a.bf16 ? k_sample_pick<true> : k_sample_pick<false>, dim3((unsigned)blocks),
+                           dim3(kPickThreads), 0, stream, a, st);
+    else
+        hipLaunchKernelGGL(a.bf16 ? k_sample_plain<true> : k_sample_plain<false>, dim3((unsigned)blocks),
+                           dim3(64), 0, stream, a, st);
     return hipGetLastError();
 }
 
