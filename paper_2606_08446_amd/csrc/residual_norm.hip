@@ -69,6 +69,7 @@ template <> struct Stream8<false> {
         v = ld16_nt(in_row(static_cast<const uint16_t *>(p), row, 16 * i));
     }
     __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(v, f); }
+    __device__ __forceinline__ void arrive() const { asm volatile("" ::"v"(v)); }  // (waits for the load)
     template <bool kNt>
     __device__ static __forceinline__ void store(void *p, int64_t row, uint32_t i, const float (&f)[8])
     {
@@ -89,6 +90,7 @@ template <> struct Stream8<true> {
         for (int i = 0; i < 8; ++i)
             f[i] = __uint_as_float(v[i >> 2][i & 3]);
     }
+    __device__ __forceinline__ void arrive() const { asm volatile("" ::"v"(v[0]), "v"(v[1])); }
     template <bool kNt>
     __device__ static __forceinline__ void store(void *p, int64_t row, uint32_t i, const float (&f)[8])
     {
@@ -324,24 +326,32 @@ struct NormGrad {
         float sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
-            if (live[j]) {
-                float h[8], d[8], w[8];
-                row.h[j].get(h);
-                unpack8(row.dy[j], d);
-                unpack8(wr[j], w);
+            float h[8], d[8], w[8];
+            row.h[j].get(h);
+            unpack8(row.dy[j], d);
+            unpack8(wr[j], w);
+            float hh = 0.f, uh = 0.f, xx = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum[0] += h[e] * h[e];
-                    sum[1] += d[e] * w[e] * h[e];
-                }
-                if (Kind::kPost) {
-                    unpack8(row.x[j], h);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        sum[2] += h[e] * h[e];
-                }
+            for (int e = 0; e < 8; ++e) {
+                hh += h[e] * h[e];
+                uh += d[e] * w[e] * h[e];
             }
+            if (Kind::kPost) {
+                unpack8(row.x[j], h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    xx += h[e] * h[e];
+            }
+            sum[0] += live[j] ? hh : 0.f;
+            sum[1] += live[j] ? uh : 0.f;
+            sum[2] += live[j] ? xx : 0.f;
         }
+        // (dh may be dh_out, which another thread too holds of the row's last vector: nobody stores before
+        // everybody has it)
+        if (g.dh_out)
+#pragma unroll
+            for (int j = 0; j < kVecs; ++j)
+                row.dh[j].arrive();
         block_sums<kWaves>(sum, s_1);
         const float r = rsqrtf(sum[0] * inv_c + a.eps);
         const float c = sum[1] * inv_c * r;  // mean(u k)

@@ -329,6 +329,18 @@ def test_side_stream_and_graph_replays():
         assert all(torch.equal(x, y) for x, y in zip(outs, want + wg)), rep
 
 
+@pytest.mark.parametrize("C", [1040, 2056, 4104, 8200, 16264])
+@pytest.mark.parametrize("stream", [torch.bfloat16, torch.float32])
+def test_gradient_in_place(C, stream):
+    # dh over dh_out, where threads and whole waves lie past the row's end
+    log(f"case residual_norm_bwd in place C={C} {stream}")
+    d, dy, dh = make(1500, C, C, stream=stream, fused=False)
+    want = grad(dy, dh, d)
+    got = grad(dy, dh, d, dh=dh)
+    assert got[0].data_ptr() == dh.data_ptr()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 def test_a_trainers_node():
     d, dy, dh = make(9, 128, 15, stream=torch.float32)
     leaves = [d[n] for n in ("h", "x", "weight", "post_weight", "gate")]
