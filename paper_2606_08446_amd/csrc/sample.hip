@@ -18,8 +18,8 @@
 //   top-p         a weight of (1 - p) / vocab of the whole bounds it: tokens of up to 128 blocks, if they are
 //                 no more than 1024, are sorted; others are located first, by fp32 weights summed in
 //                 1024 bins of equal width whose error is bounded, so that the tokens of a bin or two are
-//                 sorted and all above them are summed (an issue of fp64 instructions on one CU: 50 us of
-//                 90 for 151936 tokens)
+//                 sorted and all above them are summed (bound by the issue of instructions on one CU: for
+//                 151936 bf16 tokens 20 us to locate, 40 to sum, 25 for the rest)
 //   else          (large top-k, many ties) the border is found by 10-bit digits of the keys
 // k_sample_plain does the rows of a call without filters, a wave each with no barrier to wait at; k_sample_pick
 // all rows of other calls, a workgroup each of 8 waves.  Its steps are short and wait for one another: 512
@@ -115,8 +115,10 @@ struct Row {
     }
     __device__ __forceinline__ u32x4_t block_end(int b, u32x4_t x) const
     {
-        if (!inside(b * kBlockVecs, kBlockVecs))
+        if (!inside(b * kBlockVecs, kBlockVecs)) {
             x = load(min(b * kBlockVecs + (int)(threadIdx.x & 63), vecs()));  // (vecs(): nothing)
+            asm volatile("" : "+v"(x));  // (the wait stays here)
+        }
         return x;
     }
     // its logits: NaN counts as masked
@@ -128,6 +130,17 @@ struct Row {
                             : __uint_as_float(v[e & 3]);
             // (the median of a NaN is the least of the others; the builtin becomes two instructions)
             asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z[e]) : "v"(f), "v"(INFINITY), "v"(-INFINITY));
+        }
+    }
+    // its logits clamped to [low, high], NaN counting as low
+    __device__ static __forceinline__ void unpack_clamped(u32x4_t v, float low, float high,
+                                                          float (&z)[kElems<kBf16>])
+    {
+#pragma unroll
+        for (int e = 0; e < kElems<kBf16>; ++e) {
+            const float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
+                            : __uint_as_float(v[e & 3]);
+            asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z[e]) : "v"(f), "v"(low), "v"(high));
         }
     }
     // and +inf as the largest number, -0 as 0
@@ -739,31 +752,47 @@ struct Picker : RowPicker<kBf16> {
     {
     }
 
-    // Calls use(j, z) with the 64 vectors of every listed block j, in the waves' turns.
-    // kStop: until s.n tells of more tokens than are sorted.
+    // Calls use(j, z) with the 64 vectors of every listed block j, in the waves' turns, kAhead blocks' loads
+    // under way.  kStop: until s.n tells of more tokens than are sorted.  (use's code is there kAhead times, and a
+    // row runs it a few dozen times: with 8 the instructions' own loads took longer.)
     template <bool kStop = false, typename Use>
     __device__ __forceinline__ void each_block(int n, Use use)
     {
-        constexpr int kAhead = 8;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        each_vector<kStop>(n, [&](int j, u32x4_t x) __attribute__((always_inline)) {
+            float z[kE];
+            Row<kBf16>::unpack_whole(x, z);
+            use(j, z);
+        });
+    }
+
+    // The same with the vectors as they lie in memory.
+    template <bool kStop = false, typename Use>
+    __device__ __forceinline__ void each_vector(int n, Use use)
+    {
+        constexpr int kAhead = 4;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), last = max(n - 1, 0);
+        u32x4_t v[kAhead];
+        int id[kAhead];
+        auto begin = [&](int i, int j) __attribute__((always_inline)) {
+            id[i] = __builtin_amdgcn_readfirstlane(s.list[min(j, last)]);
+            v[i] = r.block_begin(id[i]);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            begin(i, wave + i * kPickWaves);
+#pragma unroll 1
         for (int j0 = wave; j0 < n; j0 += kAhead * kPickWaves) {
             if (kStop && *(volatile uint32_t *)&s.n > (uint32_t)kSampleSort)
                 break;
-            u32x4_t v[kAhead];
-            int id[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                id[i] = __builtin_amdgcn_readfirstlane(s.list[min(j0 + i * kPickWaves, n - 1)]);
-                v[i] = r.block_begin(id[i]);
-            }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int j = j0 + i * kPickWaves;
-                if (j < n) {
-                    float z[kE];
-                    Row<kBf16>::unpack_whole(r.block_end(id[i], v[i]), z);
-                    use(j, z);
-                }
+                u32x4_t x = v[i];
+                asm volatile("" : "+v"(x));
+                const int b = id[i];
+                begin(i, j + kAhead * kPickWaves);
+                if (j < n)
+                    use(j, r.block_end(b, x));
             }
         }
     }
@@ -946,11 +975,11 @@ struct Picker : RowPicker<kBf16> {
         const int t = threadIdx.x;
         const float width = (m - tau) * (1.f / ((float)kBins - 0.5f)), per = 1.f / width;
         const float cf = (float)f.c;
-        // (a logit of `low` has a weight that no sum feels, but one that exp2_fast takes)
+        // (a logit of `low` has a weight that no sum feels, but one that exp2_fast takes, and no bin)
         const float low = (float)(md - 1000. / f.c);
         const double low_t = ((double)low - md) * f.c;
-        if (!(width > 0.f && per < 1e30f && per > 0.f && cf < 1e30f && low > -INFINITY && low < tau &&
-              low_t >= -1019. && low_t <= -900.))
+        if (!(width > 0.f && per < 1e30f && per > 0.f && cf < 1e30f && low > -INFINITY &&
+              (m - low) * per > (float)kBins && low_t >= -1019. && low_t <= -900.))
             return false;
         auto bin_of = [&](float z) -> uint32_t {  // grows as z falls
             const float x = (m - z) * per;
@@ -969,12 +998,15 @@ struct Picker : RowPicker<kBf16> {
         for (int b = t; b < blocks; b += kPickThreads)
             s.sum[b] = 0.;
         __syncthreads();
-        each_block(n_list, [&](int, const float(&z)[kE]) __attribute__((always_inline)) {
+        each_vector(n_list, [&](int, u32x4_t v) __attribute__((always_inline)) {
+            float z[kE];
+            Row<kBf16>::unpack_clamped(v, low, m, z);
 #pragma unroll
             for (int e = 0; e < kE; ++e) {
-                const uint32_t bin = bin_of(z[e]);
-                if (bin < kBins)
-                    atomicAdd(&hist[bin], (uint32_t)(__builtin_amdgcn_exp2f((z[e] - m) * cf) * unit));
+                const float d = m - z[e], x = d * per;
+                if (x < (float)kBins)
+                    atomicAdd(&hist[(uint32_t)x],
+                              (uint32_t)(__builtin_amdgcn_exp2f(-d * cf) * unit));
             }
         });
         __syncthreads();
@@ -994,9 +1026,10 @@ struct Picker : RowPicker<kBf16> {
         // ---- the sums of the kept bins, block by block; the tokens between are sorted
         const float x0 = (float)b0, x1 = (float)b1;  // (bin < b: x < b)
         auto kept_sums = [&](auto min_p) __attribute__((always_inline)) {
-            each_block(n_list, [&](int j, const float(&z)[kE]) __attribute__((always_inline)) {
+            each_vector(n_list, [&](int j, u32x4_t v) __attribute__((always_inline)) {
                 const int b = s.list[j];
-                float x[kE];
+                float z[kE], x[kE];
+                Row<kBf16>::unpack_clamped(v, low, m, z);
                 bool some = false, between = false;
 #pragma unroll
                 for (int e = 0; e < kE; ++e) {
@@ -1030,7 +1063,7 @@ struct Picker : RowPicker<kBf16> {
                 for (int e = 0; e < kE; ++e)
                     if (x[e] >= x0 && x[e] < x1) {
                         if (at < (uint32_t)kSampleSort)
-                            s.sort.key[at] = (uint64_t)~key_of(z[e]) << 32 | (uint32_t)index_in(b, e);
+                            s.sort.key[at] = (uint64_t)~key_of(z[e] + 0.f) << 32 | (uint32_t)index_in(b, e);
                         ++at;
                     }
             });
@@ -1411,22 +1444,17 @@ struct Picker : RowPicker<kBf16> {
             draw(n_list, Rule{0u, 0xffffffffu, (double)f.q});
             return;
         }
-        if (f.k == 0 && n_list > kFewBlocks) {
-            if (finish_located(n_list, tau, whole))
+        if (f.k || n_list <= kFewBlocks) {
+            const int n = collect(n_list, tau);
+            if (n <= kSampleSort) {
+                finish_sorted(n, whole);
                 return;
+            }
             __syncthreads();
         }
-        const int n = collect(n_list, tau);
-        if (n <= kSampleSort) {
-            finish_sorted(n, whole);
+        if (f.k == 0 && finish_located(n_list, tau, whole))
             return;
-        }
         __syncthreads();
-        if (f.k == 0 && n_list <= kFewBlocks) {
-            if (finish_located(n_list, tau, whole))
-                return;
-            __syncthreads();
-        }
         draw(n_list, cut_by_digits(n_list, tau, whole));
     }
 
