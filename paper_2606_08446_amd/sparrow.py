@@ -956,7 +956,10 @@ def residual_norm(h, x, weight, post_weight=None, gate=None, scale=1.0, eps=1e-6
             raise ValueError("gate, post_weight and h_out go with x")
     else:
         h_out = _given_like(h_out, "h_out", h)
-    y = _given(y, "y", torch.bfloat16, (T, C), dev)
+    if x is None and dt == SPARROW_STREAM_F32:
+        y = _given(y, "y", torch.bfloat16, (T, C), dev)
+    else:
+        y = _given_like(y, "y", h if dt == SPARROW_STREAM_BF16 else x)
     if T > 0:
         _launch("sparrow_residual_norm", dev, T, C, dt, h.data_ptr(), _ptr(x), xs, _ptr(gate), gs,
                 weight.data_ptr(), _ptr(post_weight), float(scale), float(eps), _ptr(h_out),
