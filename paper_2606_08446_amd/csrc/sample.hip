@@ -13,8 +13,8 @@
 // find from these which blocks can hold a kept token and read only them:
 //   no filter     the span that holds the token, then its block
 //   min-p         the blocks that reach m + T ln q: their sums, then one block
-//   top-k         the k-th largest block maximum bounds the last kept logit from below: the tokens above,
-//                 hardly more than k, are sorted in LDS
+//   top-k         the k-th largest span's or block's maximum bounds the last kept logit from below: the
+//                 tokens above, hardly more than k, are sorted in LDS
 //   top-p         a weight of (1 - p) / vocab of the whole bounds it: tokens of up to 128 blocks, if they are
 //                 no more than 1024, are sorted; others are located first, by fp32 weights summed in
 //                 1024 bins of equal width whose error is bounded, so that the tokens of a bin or two are
@@ -393,7 +393,8 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
 }
 
 struct PickLds {
-    float max[kMaxBlocks];       // the blocks' maxima
+    alignas(16) float max[kMaxBlocks];  // the blocks' maxima
+    float top[kMaxSpans];        // the spans'
     uint16_t list[kMaxBlocks];   // blocks that may hold a kept token
     double sum[kMaxBlocks];      // weights kept in a block, or in a listed one
     double red[kPickWaves];
@@ -814,18 +815,18 @@ struct Picker : RowPicker<kBf16> {
         return (int)n;
     }
 
-    // A lower bound of the k-th largest block maximum, exact to its upper 16 key bits (k <= blocks): four
-    // bits a round, two of the 16 values that they may have for each wave.
-    __device__ __forceinline__ float kth_maximum(int k)
+    // A lower bound of the k-th largest of n maxima, of spans where there are k, else of blocks, exact to
+    // its upper 16 key bits: four bits a round, two of the 16 values that they may have for each wave.
+    __device__ __forceinline__ float kth_maximum(const float *maxima, int count, int k)
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
         static_assert(2 * kPickWaves == 16, "two values of four bits a wave");
         uint32_t key = 0;
         for (int shift = 28; shift >= 16; shift -= 4) {
             const uint32_t t0 = key | (uint32_t)(2 * wave) << shift, t1 = t0 | 1u << shift;
-            uint32_t n = 0;  // (blocks, at most 2^16 - 1, that reach one and the other)
-            for (int b = lane; b < blocks; b += 64) {
-                const uint32_t x = key_of(s.max[b]);
+            uint32_t n = 0;  // (of them, at most 2^16 - 1, that reach one and the other)
+            for (int b = lane; b < count; b += 64) {
+                const uint32_t x = key_of(maxima[b]);
                 n += (x >= t0 ? 1u : 0u) + (x >= t1 ? 1u << 16 : 0u);
             }
             n = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(n), 63);
@@ -834,7 +835,7 @@ struct Picker : RowPicker<kBf16> {
                 s.reach[2 * wave + 1] = n >> 16;
             }
             __syncthreads();
-            uint32_t v = 0;  // the largest value that k blocks reach
+            uint32_t v = 0;  // the largest value that k of them reach
 #pragma unroll
             for (uint32_t w = 1; w < 16; ++w)
                 v = s.reach[w] >= (uint32_t)k ? w : v;
@@ -1402,13 +1403,27 @@ struct Picker : RowPicker<kBf16> {
 
     __device__ __forceinline__ void pick(const Stats &st)
     {
+        // ---- the row's statistics; m, and the sum over all tokens
+        constexpr int kOwn = (kMaxSpans + kPickThreads - 1) / kPickThreads;  // spans of a thread
         const int64_t first = row * st.spans;
-        const int spans = (vecs + kSpanVecs - 1) / kSpanVecs, t = threadIdx.x;
-        float top = -INFINITY;
-        for (int b = t; b < blocks; b += kPickThreads) {
-            const float x = st.maxima[first * kSpanBlocks + b];
-            s.max[b] = x;
-            top = fmaxf(top, x);
+        const int t = threadIdx.x;
+        float own[kOwn], top = -INFINITY;
+        double sum[kOwn];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int sp = t + i * kPickThreads;
+            own[i] = -INFINITY;
+            sum[i] = 0.;
+            if (sp < st.spans) {
+                const u32x4_t x = ld16(st.maxima + (first + sp) * kSpanBlocks);
+                if (f.k == 0)
+                    sum[i] = st.sums[first + sp];
+                *reinterpret_cast<u32x4_t *>(s.max + kSpanBlocks * sp) = x;
+                own[i] = fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
+                               fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
+                s.top[sp] = own[i];
+                top = fmaxf(top, own[i]);
+            }
         }
         top = wave_max_f(top);
         if ((t & 63) == 0)
@@ -1427,18 +1442,18 @@ struct Picker : RowPicker<kBf16> {
         double whole = 0.;
         if (f.k == 0) {  // the spans' sums, brought to the row's maximum
             double x = 0.;
-            for (int i = t; i < spans; i += kPickThreads) {
-                float sm = s.max[kSpanBlocks * i];
-                for (int b = 1; b < kSpanBlocks; ++b)
-                    if (kSpanBlocks * i + b < blocks)
-                        sm = fmaxf(sm, s.max[kSpanBlocks * i + b]);
-                const double sum = st.sums[first + i];
-                x += sum > 0. ? sum * weight_of(sm, md, f.c) : 0.;
-            }
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i)
+                x += sum[i] > 0. ? sum[i] * weight_of(own[i], md, f.c) : 0.;
             block_scan_64(x, s.red, whole);
             __syncthreads();
         }
-        const float tau = bound(whole, f.k && f.k <= blocks ? kth_maximum(f.k) : -INFINITY);
+        float kth = -INFINITY;
+        if (f.k && f.k <= st.spans)
+            kth = kth_maximum(s.top, st.spans, f.k);
+        if (f.k && f.k <= blocks && kth == -INFINITY)  // (of most spans every token may be masked)
+            kth = kth_maximum(s.max, blocks, f.k);
+        const float tau = bound(whole, kth);
         const int n_list = list_blocks(tau);
         if (f.k == 0 && f.p >= 1.f) {
             draw(n_list, Rule{0u, 0xffffffffu, (double)f.q});

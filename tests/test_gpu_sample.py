@@ -355,3 +355,24 @@ def test_two_calls_at_once():
     for i in range(2):
         for g in got[i]:
             assert all(torch.equal(x, y) for x, y in zip(g, want[i]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_top_k_of_few_unmasked_spans(dtype):
+    # fewer spans than k hold a token at all, more blocks do; and NaN of either kind among the masked
+    log(f"case sample few spans {dtype}")
+    V = 151936
+    z = torch.full((4, V), -math.inf)
+    g = torch.Generator().manual_seed(77)
+    for i in range(4):
+        for at in range(5000, V - 3000, 16000 + 3000 * i):
+            z[i, at:at + 3000] = torch.randn(3000, generator=g) * 3
+    z[1, ::97] = math.nan
+    z = z.to(dtype).to(DEV)
+    bits = z.view(torch.int32 if dtype == F32 else torch.int16)
+    bits[2, ::89] = 0x7f800001 if dtype == F32 else 0x7f81     # (a signalling NaN)
+    k = torch.tensor([20, 33, 15, 40], dtype=torch.int32, device=DEV)
+    for p in (None, rand(4, 5, 0.5, 0.95)):
+        check(z, rand(4, 6), None, k, p)
+    check(z, rand(4, 7))
+    check(z, rand(4, 8), None, None, rand(4, 9, 0.5, 0.95))
