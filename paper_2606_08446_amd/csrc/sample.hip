@@ -128,7 +128,8 @@ struct Row {
         for (int e = 0; e < kElems<kBf16>; ++e) {
             const float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
                             : __uint_as_float(v[e & 3]);
-            // (the median of a NaN is the least of the others; the builtin becomes two instructions)
+            // (the median with a NaN is the least of the others, with a signalling one the last: least last; the
+            // builtin becomes two instructions)
             asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z[e]) : "v"(f), "v"(INFINITY), "v"(-INFINITY));
         }
     }
@@ -140,7 +141,7 @@ struct Row {
         for (int e = 0; e < kElems<kBf16>; ++e) {
             const float f = kBf16 ? (e & 1 ? bf16_hi(v[(e >> 1) & 3]) : bf16_lo(v[(e >> 1) & 3]))
                             : __uint_as_float(v[e & 3]);
-            asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z[e]) : "v"(f), "v"(low), "v"(high));
+            asm("v_med3_f32 %0, %1, %2, %3" : "=v"(z[e]) : "v"(f), "v"(high), "v"(low));
         }
     }
     // and +inf as the largest number, -0 as 0

@@ -59,7 +59,7 @@ def reference(z, u, t=1.0, k=0, p=1.0, q=0.0):
 def check(z, u, t=None, k=None, p=None, q=None, got=None):
     got = S.sample(z, u, temperature=t, top_k=k, top_p=p, min_p=q) if got is None else got
     tok, lp = got[0].cpu().numpy(), got[1].cpu().numpy().astype(np.float64)
-    zs = z.float().cpu().numpy().astype(np.float64)
+    zs = z.cpu().double().numpy()
 
     def col(x, default):
         return [default] * len(zs) if x is None else x.cpu().numpy().astype(np.float64).tolist()
