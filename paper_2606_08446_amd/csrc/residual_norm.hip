@@ -40,13 +40,19 @@ __device__ __forceinline__ u32x4_t pack8(const float (&f)[8])
                      pack_bf16(f[6], f[7])};
 }
 
-// Place `bytes` of a row, whose start the whole workgroup shares: an address in scalar registers and one 32-bit
-// offset for a thread's place in every array.  (Opaque to the compiler, which would keep a pointer for each.)
+// The place of a row's i-th 16 bytes of bf16: one 32-bit offset for every array, whose rows' starts the whole
+// workgroup shares in scalar registers.  (Opaque to the compiler, which would keep a pointer for each.)
+__device__ __forceinline__ uint32_t place_of(int i)
+{
+    uint32_t bytes = 16u * (uint32_t)i;
+    asm("" : "+v"(bytes));
+    return bytes;
+}
+
 template <typename T>
 __device__ __forceinline__ T *in_row(T *base, int64_t row, uint32_t bytes)
 {
     using Bytes = std::conditional_t<std::is_const_v<T>, const char, char>;
-    asm("" : "+v"(bytes));
     return reinterpret_cast<T *>(reinterpret_cast<Bytes *>(base + row) + bytes);
 }
 
@@ -60,27 +66,27 @@ __device__ __forceinline__ void put16(void *p, u32x4_t v)
         st16(p, v);
 }
 
-// 8 channels of the stream as they lie in memory, the i-th 8 of a row that starts at `row`.
+// 8 channels of the stream as they lie in memory, those at a place of a row that starts at `row`.
 template <bool kF32> struct Stream8;
 template <> struct Stream8<false> {
     u32x4_t v;
-    __device__ __forceinline__ void load(const void *p, int64_t row, uint32_t i)
+    __device__ __forceinline__ void load(const void *p, int64_t row, uint32_t place)
     {
-        v = ld16_nt(in_row(static_cast<const uint16_t *>(p), row, 16 * i));
+        v = ld16_nt(in_row(static_cast<const uint16_t *>(p), row, place));
     }
     __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(v, f); }
     __device__ __forceinline__ void arrive() const { asm volatile("" ::"v"(v)); }  // (waits for the load)
     template <bool kNt>
-    __device__ static __forceinline__ void store(void *p, int64_t row, uint32_t i, const float (&f)[8])
+    __device__ static __forceinline__ void store(void *p, int64_t row, uint32_t place, const float (&f)[8])
     {
-        put16<kNt>(in_row(static_cast<uint16_t *>(p), row, 16 * i), pack8(f));
+        put16<kNt>(in_row(static_cast<uint16_t *>(p), row, place), pack8(f));
     }
 };
 template <> struct Stream8<true> {
     u32x4_t v[2];
-    __device__ __forceinline__ void load(const void *p, int64_t row, uint32_t i)
+    __device__ __forceinline__ void load(const void *p, int64_t row, uint32_t place)
     {
-        const float *q = in_row(static_cast<const float *>(p), row, 32 * i);
+        const float *q = in_row(static_cast<const float *>(p), row, 2 * place);
         v[0] = ld16_nt(q);
         v[1] = ld16_nt(q + 4);
     }
@@ -92,9 +98,9 @@ template <> struct Stream8<true> {
     }
     __device__ __forceinline__ void arrive() const { asm volatile("" ::"v"(v[0]), "v"(v[1])); }
     template <bool kNt>
-    __device__ static __forceinline__ void store(void *p, int64_t row, uint32_t i, const float (&f)[8])
+    __device__ static __forceinline__ void store(void *p, int64_t row, uint32_t place, const float (&f)[8])
     {
-        float *q = in_row(static_cast<float *>(p), row, 32 * i);
+        float *q = in_row(static_cast<float *>(p), row, 2 * place);
         put16<kNt>(q, __builtin_bit_cast(u32x4_t, (f32x4_t){f[0], f[1], f[2], f[3]}));
         put16<kNt>(q + 4, __builtin_bit_cast(u32x4_t, (f32x4_t){f[4], f[5], f[6], f[7]}));
     }
@@ -139,21 +145,20 @@ __device__ __forceinline__ void clear_sums(float (*s)[kN])
             s[threadIdx.x][i] = 0.f;
 }
 
-// sigmoid(a) and sigmoid(-a), both without cancellation and without overflow: with e = e^-|a| they are
-// 1 / (1 + e) and e / (1 + e).  The exponent a log2(e) is taken in two parts, since its rounding alone would
-// cost 2^-18 of e at |a| = 88; exponential and reciprocal are off by 2^-23 each.
+// sigmoid(a) and its slope s (1 - s) without cancellation or overflow: with e = e^-|a|, r = 1 / (1 + e) they
+// are r or e r, and e r^2.  log2(e) is taken in two parts, since the rounding of a log2(e) alone would cost
+// 2^-18 of e at |a| = 88: the first, of 16 bits, gives an exact product with a bf16 number, and 2^x of
+// the second's, at most 7e-4, is 1 + x ln 2 to 2^-23 (no less than 1/2 for an infinite a, where e is 0).
 struct Sigmoid {
-    float s, other;
+    float s, slope;
     __device__ __forceinline__ explicit Sigmoid(float a)
     {
-        constexpr float kHi = 1.44269502f, kLo = 1.92596303e-8f;  // log2(e)
-        const float m = fabsf(a) > 200.f ? -200.f : -fabsf(a), t = m * kHi;  // (a NaN stays)
-        const float lo = fmaf(m, kHi, -t) + m * kLo;
-        const float e2 = __builtin_amdgcn_exp2f(t);
-        const float e = fmaf(e2, lo * 0.693147182f, e2);
+        constexpr float kHi = 47274.f / 32768.f, kLo = 7.0526077e-06f * 0.69314718f;
+        const float m = -fabsf(a);
+        const float e = __builtin_amdgcn_exp2f(m * kHi) * fmaxf(fmaf(m, kLo, 1.f), 0.5f);
         const float r = __builtin_amdgcn_rcpf(1.f + e), q = e * r;
         s = a < 0.f ? q : r;
-        other = a < 0.f ? r : q;
+        slope = q * r;
     }
 };
 
@@ -191,11 +196,12 @@ __global__ __launch_bounds__(Kind::kThreads) void k_residual_norm(NormArgs a, vo
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {  // (threads past the row read its last vector)
             const int i = min((int)(threadIdx.x + j * blockDim.x), vecs - 1);
-            hr[j].load(a.h, t * a.channels, i);
+            const uint32_t place = place_of(i);
+            hr[j].load(a.h, t * a.channels, place);
             if (has_x)
-                xr[j] = ld16_nt(in_row(a.x, t * a.x_stride, 16 * i));
+                xr[j] = ld16_nt(in_row(a.x, t * a.x_stride, place));
             if (Kind::kGate)
-                gr[j] = ld16_nt(in_row(a.gate, t * a.gate_stride, 16 * i));
+                gr[j] = ld16_nt(in_row(a.gate, t * a.gate_stride, place));
             wr[j] = ld16(a.weight + 8 * i);
             if (Kind::kPost)
                 pr[j] = ld16(a.post + 8 * i);
@@ -219,6 +225,7 @@ __global__ __launch_bounds__(Kind::kThreads) void k_residual_norm(NormArgs a, vo
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
             const int i = threadIdx.x + j * blockDim.x;
+            const uint32_t place = place_of(i);
             hr[j].get(h[j]);
             if (has_x) {
                 float x[8];
@@ -241,7 +248,7 @@ __global__ __launch_bounds__(Kind::kThreads) void k_residual_norm(NormArgs a, vo
                 for (int e = 0; e < 8; ++e)
                     h[j][e] += a.scale * x[e];
                 if (i < vecs)
-                    Stream::template store<Kind::kNt>(h_out, t * a.channels, i, h[j]);
+                    Stream::template store<Kind::kNt>(h_out, t * a.channels, place, h[j]);
             }
             if (i < vecs)
 #pragma unroll
@@ -253,13 +260,14 @@ __global__ __launch_bounds__(Kind::kThreads) void k_residual_norm(NormArgs a, vo
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
             const int i = threadIdx.x + j * blockDim.x;
+            const uint32_t place = place_of(i);
             float w[8];
             unpack8(wr[j], w);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 w[e] *= h[j][e] * r;
             if (i < vecs)
-                put16<Kind::kNt>(in_row(y, t * a.channels, 16 * i), pack8(w));
+                put16<Kind::kNt>(in_row(y, t * a.channels, place), pack8(w));
         }
         if (t + gridDim.x < a.tokens)
             __syncthreads();  // the sums' LDS is written again
@@ -279,16 +287,16 @@ struct GradRow {
         if (g.dh_out)
 #pragma unroll
             for (int j = 0; j < Kind::kVecs; ++j)
-                dh[j].load(g.dh_out, t * a.channels, at[j]);
+                dh[j].load(g.dh_out, t * a.channels, place_of(at[j]));
 #pragma unroll
         for (int j = 0; j < Kind::kVecs; ++j) {
-            const int i = at[j];
-            h[j].load(a.h, t * a.channels, i);
-            dy[j] = ld16_nt(in_row(g.dy, t * a.channels, 16 * i));
+            const uint32_t place = place_of(at[j]);
+            h[j].load(a.h, t * a.channels, place);
+            dy[j] = ld16_nt(in_row(g.dy, t * a.channels, place));
             if (Kind::kX)
-                x[j] = ld16_nt(in_row(a.x, t * a.x_stride, 16 * i));
+                x[j] = ld16_nt(in_row(a.x, t * a.x_stride, place));
             if (Kind::kGate)
-                gate[j] = ld16_nt(in_row(a.gate, t * a.gate_stride, 16 * i));
+                gate[j] = ld16_nt(in_row(a.gate, t * a.gate_stride, place));
         }
     }
 };
@@ -354,13 +362,14 @@ struct NormGrad {
                 row.dh[j].arrive();
         block_sums<kWaves>(sum, s_1);
         const float r = rsqrtf(sum[0] * inv_c + a.eps);
-        const float c = sum[1] * inv_c * r;  // mean(u k)
+        const float rc = r * (sum[1] * inv_c * r);  // r mean(u k)
         const float rx = Kind::kPost ? rsqrtf(sum[2] * inv_c + a.eps) : 1.f;
         // ---- dh, dgate; what goes on to x stays in e
         float e_[kVecs][8], dot[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
             const int i = at[j];  // (threads past the row store the last vector's results again)
+            const uint32_t place = place_of(i);
             float h[8], d[8], w[8];
             row.h[j].get(h);
             unpack8(row.dy[j], d);
@@ -370,7 +379,7 @@ struct NormGrad {
             for (int e = 0; e < 8; ++e) {
                 const float k = h[e] * r;
                 dk[e] = d[e] * k;
-                d[e] = r * (d[e] * w[e] - k * c);
+                d[e] = r * (d[e] * w[e]) - k * rc;
             }
             add8(dw[j], s_dw, i, live[j], dk);
             if (g.dh_out) {
@@ -379,7 +388,7 @@ struct NormGrad {
                 for (int e = 0; e < 8; ++e)
                     d[e] += h[e];
             }
-            Stream8<Kind::kF32>::template store<Kind::kNt>(g.dh, t * a.channels, i, d);
+            Stream8<Kind::kF32>::template store<Kind::kNt>(g.dh, t * a.channels, place, d);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 d[e] *= a.scale;
@@ -400,38 +409,40 @@ struct NormGrad {
                 for (int e = 0; e < 8; ++e) {
                     const Sigmoid s(q[e]);
                     const float n = Kind::kPost ? x[e] * p[e] : x[e];
+                    q[e] = d[e] * s.slope * n;
                     d[e] *= s.s;
-                    q[e] = d[e] * n * s.other;
                 }
-                put16<Kind::kNt>(in_row(g.dgate, t * g.dgate_stride, 16 * i), pack8(q));
+                put16<Kind::kNt>(in_row(g.dgate, t * g.dgate_stride, place), pack8(q));
             }
             if (Kind::kPost) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     dk[e] = d[e] * x[e];
                 add8(dp[j], s_dw + a.channels, i, live[j], dk);
+                float here = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     d[e] *= p[e];
-                    dot[0] += live[j] ? d[e] * x[e] : 0.f;
+                    here += d[e] * x[e];
                     e_[j][e] = d[e];
                 }
+                dot[0] += live[j] ? here : 0.f;
             } else if (Kind::kGate || g.dx) {
-                put16<Kind::kNt>(in_row(g.dx, t * g.dx_stride, 16 * i), pack8(d));
+                put16<Kind::kNt>(in_row(g.dx, t * g.dx_stride, place), pack8(d));
             }
         }
         if (Kind::kPost) {
             block_sums<kWaves>(dot, s_2);
-            const float m = dot[0] * inv_c;
+            const float rxm = rx * rx * (dot[0] * inv_c);
 #pragma unroll
             for (int j = 0; j < kVecs; ++j) {
-                const int i = at[j];
+                const uint32_t place = place_of(at[j]);
                 float x[8];
                 unpack8(row.x[j], x);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    x[e] = rx * (e_[j][e] - x[e] * rx * m);
-                put16<Kind::kNt>(in_row(g.dx, t * g.dx_stride, 16 * i), pack8(x));
+                    x[e] = rx * e_[j][e] - x[e] * rxm;
+                put16<Kind::kNt>(in_row(g.dx, t * g.dx_stride, place), pack8(x));
             }
         } else {
             __syncthreads();  // s_1 is written again
@@ -520,9 +531,9 @@ k_residual_norm_bwd(NormArgs a, NormGradArgs g)
                     n.dp[j][e] = Kind::kPost ? s_dw[a.channels + 8 * i + e] : 0.f;
                 }
             }
-            Stream8<true>::store<false>(out, 0, i, n.dw[j]);
+            Stream8<true>::store<false>(out, 0, place_of(i), n.dw[j]);
             if (Kind::kPost)
-                Stream8<true>::store<false>(out, a.channels, i, n.dp[j]);
+                Stream8<true>::store<false>(out, a.channels, place_of(i), n.dp[j]);
         }
     }
 }
