@@ -21,6 +21,10 @@
  *   sparrow_append_score_topk fuses the append into step 2, and
  *   sparrow_decode_step runs the append and steps 2 and 3 in one call.
  *
+ * Around it stand sparrow_residual_norm (between two blocks of a layer), sparrow_qk_norm_rope (in front of
+ * the cache), the 8-bit cache's calls (*_e4m3), sparrow_shared_prefix_decode_attn (dense attention for
+ * the samples of one prompt) and sparrow_sample (the next token from the head's logits).
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - Every array argument is a DEVICE pointer owned by the caller.  The library
@@ -359,7 +363,9 @@ int sparrow_dense_decode_attn(const sparrow_shape_t *shape, const void *q, const
  *     out[b][j] = sum_t w_t V[t],  w = softmax(scale * q[b][j] . K[t]) over t < seq_lens[b]
  * with fp32 sums; the softmax numerators enter the product with V as bf16 for SPARROW_OUT_BF16 and
  * with all of their 24 bits for SPARROW_OUT_F32.  An empty sequence gives a zero row.  The order of the
- * sums depends only on the shape, the groups, the lengths and the device.
+ * sums depends only on the shape, the groups, the lengths and the device.  Tokens that no sequence of a
+ * group reaches may hold anything; where a shared V row that some sequences reach is not finite, sequences
+ * of the group that end before it may get NaN as well.
  *
  * Arguments: as for sparrow_dense_decode_attn, batch * num_kv_heads <= 65535; 0 <= num_groups <=
  * SPARROW_MAX_GROUPS; cu_groups (device int32 [num_groups + 1], non-decreasing; entries outside [0,
