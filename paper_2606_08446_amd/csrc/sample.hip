@@ -45,6 +45,7 @@ constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / 64;
 constexpr int kSampleSort = 1024;  // tokens that a workgroup sorts
 constexpr int kFewBlocks = 128;    // of which their number is seen by collecting them
+constexpr int kFewSpans = 320;     // whose maxima take 5 registers, not 9
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kMaxSpans = (kSampleMaxVocab / 4 + 1 + kSpanVecs - 1) / kSpanVecs;
@@ -400,7 +401,7 @@ struct PickLds {
     uint16_t list[kMaxBlocks];   // blocks that may hold a kept token
     double sum[kMaxBlocks];      // weights kept in a block, or in a listed one
     double red[kPickWaves];
-    uint32_t cnt[kPickWaves], reach[16];
+    uint32_t cnt[kPickWaves];
     uint32_t n;                  // a counter, a result
     uint32_t found, found2;
     double total, before;
@@ -455,10 +456,37 @@ __device__ __forceinline__ uint32_t block_scan_32(uint32_t x, uint32_t *cnt, uin
     return base + x;
 }
 
-// Ascending bitonic sort of size (a power of two, at most two per thread) keys.
-__device__ __forceinline__ void sort_keys(uint64_t *key, int size)
+// n different keys into ascending order, with all ones behind them up to a power of two.  Up to 256 by counting
+// the smaller ones, 64 in an instruction, each wave for every 8th key; more, at most two per thread, by
+// a bitonic network, whose steps are an LDS trip each (32 keys 15 of them: 1.7 us of one row's 17).
+__device__ __forceinline__ void sort_keys(uint64_t *key, int n, int size)
 {
-    const int t = threadIdx.x;
+    constexpr int kRanked = 256;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    if (n <= kRanked) {
+        static_assert(kRanked <= 64 * kPickWaves, "a lane's own key");
+        const int own = wave + kPickWaves * lane;
+        uint64_t all[kRanked / 64], mine = own < n ? key[own] : 0;
+#pragma unroll
+        for (int r = 0; r < kRanked / 64; ++r)
+            all[r] = lane + 64 * r < n ? key[lane + 64 * r] : ~0ull;
+        int rank = 0;
+        for (int q = 0; wave + kPickWaves * q < n; ++q) {
+            const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), q) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, q);
+            int less = 0;
+#pragma unroll
+            for (int r = 0; r < kRanked / 64; ++r)
+                if (64 * r < n)
+                    less += __popcll(__ballot(all[r] < k));
+            rank = lane == q ? less : rank;
+        }
+        __syncthreads();
+        if (own < n)
+            key[rank] = mine;
+        __syncthreads();
+        return;
+    }
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
             if (t < size >> 1) {
@@ -817,34 +845,30 @@ struct Picker : RowPicker<kBf16> {
         return (int)n;
     }
 
-    // A lower bound of the k-th largest of n maxima, of spans where there are k, else of blocks, exact to
-    // its upper 16 key bits: four bits a round, two of the 16 values that they may have for each wave.
-    __device__ __forceinline__ float kth_maximum(const float *maxima, int count, int k)
+    // A lower bound of the k-th largest of count maxima, of the spans where there are k, else of the blocks, exact
+    // to its upper 16 key bits: bit by bit, every wave for itself, with the keys in registers and no
+    // barrier (297 spans: in rounds of four bits with two values for each wave 3.4 us, so 2.6 with registers for
+    // the most spans, and 1.9 with as many as there are).
+    template <int kMost>
+    __device__ __forceinline__ float kth_maximum(const float *maxima, int count, int k) const
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        static_assert(2 * kPickWaves == 16, "two values of four bits a wave");
-        uint32_t key = 0;
-        for (int shift = 28; shift >= 16; shift -= 4) {
-            const uint32_t t0 = key | (uint32_t)(2 * wave) << shift, t1 = t0 | 1u << shift;
-            uint32_t n = 0;  // (of them, at most 2^16 - 1, that reach one and the other)
-            for (int b = lane; b < count; b += 64) {
-                const uint32_t x = key_of(maxima[b]);
-                n += (x >= t0 ? 1u : 0u) + (x >= t1 ? 1u << 16 : 0u);
-            }
-            n = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(n), 63);
-            if (lane == 0) {
-                s.reach[2 * wave] = n & 0xffffu;
-                s.reach[2 * wave + 1] = n >> 16;
-            }
-            __syncthreads();
-            uint32_t v = 0;  // the largest value that k of them reach
+        constexpr int kRegs = (kMost + 63) / 64;
+        const int lane = threadIdx.x & 63;
+        uint32_t x[kRegs];
 #pragma unroll
-            for (uint32_t w = 1; w < 16; ++w)
-                v = s.reach[w] >= (uint32_t)k ? w : v;
-            key |= v << shift;
-            __syncthreads();
+        for (int r = 0; r < kRegs; ++r)
+            x[r] = lane + 64 * r < count ? key_of(maxima[lane + 64 * r]) : 0u;
+        uint32_t bound = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 16; --bit) {
+            const uint32_t t = bound | 1u << bit;
+            int n = 0;
+#pragma unroll
+            for (int r = 0; r < kRegs; ++r)
+                n += __popcll(__ballot(x[r] >= t));
+            bound = n >= k ? t : bound;
         }
-        return bound_of(key);
+        return bound_of(bound);
     }
 
     // The logit of a bound's key (one below that of -inf belongs to no number).
@@ -905,7 +929,7 @@ struct Picker : RowPicker<kBf16> {
         for (int i = n + t; i < size; i += kPickThreads)
             s.sort.key[i] = ~0ull;
         __syncthreads();
-        sort_keys(s.sort.key, size);
+        sort_keys(s.sort.key, n, size);
         double w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -954,7 +978,7 @@ struct Picker : RowPicker<kBf16> {
         if (t == 0)
             s.found = (uint32_t)keep - 1;
         __syncthreads();
-        sort_keys(s.sort.key, size);
+        sort_keys(s.sort.key, keep, size);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * t + i;
@@ -1095,7 +1119,7 @@ struct Picker : RowPicker<kBf16> {
         for (int i = n + t; i < size; i += kPickThreads)
             s.sort.key[i] = ~0ull;
         __syncthreads();
-        sort_keys(s.sort.key, size);
+        sort_keys(s.sort.key, n, size);
         double w[2], all;
         uint64_t key[2];
 #pragma unroll
@@ -1452,9 +1476,10 @@ struct Picker : RowPicker<kBf16> {
         }
         float kth = -INFINITY;
         if (f.k && f.k <= st.spans)
-            kth = kth_maximum(s.top, st.spans, f.k);
+            kth = st.spans <= kFewSpans ? kth_maximum<kFewSpans>(s.top, st.spans, f.k)
+                                        : kth_maximum<kMaxSpans>(s.top, st.spans, f.k);
         if (f.k && f.k <= blocks && kth == -INFINITY)  // (of most spans every token may be masked)
-            kth = kth_maximum(s.max, blocks, f.k);
+            kth = kth_maximum<kMaxBlocks>(s.max, blocks, f.k);
         const float tau = bound(whole, kth);
         const int n_list = list_blocks(tau);
         if (f.k == 0 && f.p >= 1.f) {
