@@ -791,12 +791,19 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
         raise ValueError(f"logits: shape {tuple(logits.shape)} with strides {logits.stride()}, expected "
                          "contiguous vocabulary entries and rows that do not overlap")
     _expect(uniform, "uniform", torch.float32, (T,), dev)
-    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        if t is not None:
-            _expect(t, name, dtype, (T,), dev)
+    if temperature is not None:
+        _expect(temperature, "temperature", torch.float32, (T,), dev)
+    if top_k is not None:
+        _expect(top_k, "top_k", torch.int32, (T,), dev)
+    if top_p is not None:
+        _expect(top_p, "top_p", torch.float32, (T,), dev)
+    if min_p is not None:
+        _expect(min_p, "min_p", torch.float32, (T,), dev)
     logprobs = _given_like(logprobs, "logprobs", uniform)
-    tokens = _given(tokens, "tokens", torch.int32, (T,), dev)
+    if tokens is None:
+        tokens = torch.empty_like(uniform, dtype=torch.int32)
+    else:
+        _expect(tokens, "tokens", torch.int32, (T,), dev)
     if T == 0:
         return tokens, logprobs
     if workspace is None:
