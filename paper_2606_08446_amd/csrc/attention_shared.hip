@@ -796,19 +796,23 @@ struct Parts {
     int64_t g0, s0;  // the first ones' rows
     int n_g, n_s, G;
 
+    // (What the plan says of the sequence and of both sides is loaded at once, in front of what the group needs.)
     __device__ __forceinline__ Parts(const SharedArgs &a, int b, int hq)
     {
         const int Hkv = a.num_kv_heads;
         G = a.num_q_heads / Hkv;
         const int h = hq / G, j = hq - h * G;
+        const int32_t *seq = a.plan_off + a.groups;
+        const int g = a.seq_group[b];
+        const uint32_t begin_s = seq[0], end_s = seq[a.batch], off = seq[b], off_next = seq[b + 1];
+        const uint32_t takers_g = a.plan_takers[0], takers_s = a.plan_takers[1];
         n_g = n_s = 0;
         g0 = s0 = 0;
-        const int g = a.seq_group[b];
         if (g >= 0) {
             const uint32_t first = a.plan_off[g], all = a.plan_off[g + 1] - first;
             const int begin = a.plan_cu[g], rows = (a.plan_cu[g + 1] - begin) * G;
             if (all > 0) {
-                const Share share(a.plan_off[a.groups], a.plan_takers[0]);
+                const Share share(begin_s, takers_g);
                 const uint32_t blocks = (rows + kTeamRows - 1) / kTeamRows, unit = all / (blocks * Hkv);
                 const int r = (b - begin) * G + j;
                 const uint32_t p0 = first + (h * blocks + r / kTeamRows) * unit;
@@ -818,11 +822,10 @@ struct Parts {
                 g0 = (int64_t)(w0 * kSharedWaves + blocks_before(a, g, begin, rows, h, r)) * kRows + r % kRows;
             }
         }
-        const int32_t *seq = a.plan_off + a.groups;
-        const uint32_t own = (seq[b + 1] - seq[b]) / Hkv;
+        const uint32_t own = (off_next - off) / Hkv;
         if (own > 0) {
-            const Share share(seq[a.batch] - seq[0], a.plan_takers[1]);
-            const uint32_t p0 = seq[b] - seq[0] + h * own, w0 = share.taker_of(p0 + kPartCost);
+            const Share share(end_s - begin_s, takers_s);
+            const uint32_t p0 = off - begin_s + h * own, w0 = share.taker_of(p0 + kPartCost);
             n_s = share.taker_of(p0 + own - 1) - w0 + 1;
             s0 = (int64_t)(w0 + b * Hkv + h) * G + j;
         }
@@ -852,7 +855,17 @@ __global__ __launch_bounds__(kSharedThreads) void k_shared_merge(SharedArgs a)
     const int b = row / a.num_q_heads;
     const Parts parts(a, b, row - b * a.num_q_heads);
     const int n = parts.count();
+    const int side = t >> 5, c = 4 * (t & 31);
     const float *op, *ml;
+    // the side's first part, while the parts' maxima are gathered
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    float m0 = kNoLogit, l = 0.f;
+    if (side < n) {
+        parts.at(a, side, op, ml);
+        o = __builtin_bit_cast(f32x4_t, ld16(op + c));
+        m0 = ml[0];
+        l = ml[1];
+    }
     float top = kNoLogit;
     for (int i = t; i < n; i += 64 * kWaves) {
         parts.at(a, i, op, ml);
@@ -867,10 +880,10 @@ __global__ __launch_bounds__(kSharedThreads) void k_shared_merge(SharedArgs a)
         for (int w = 0; w < kWaves; ++w)
             top = fmaxf(top, s_m[here][w]);
     }
-    const int side = t >> 5, c = 4 * (t & 31);
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int i = side; i < n; i += kSides) {
+    const float x0 = __builtin_amdgcn_exp2f(m0 - top);
+    l *= x0;
+    o *= x0;
+    for (int i = side + kSides; i < n; i += kSides) {
         parts.at(a, i, op, ml);
         const float x = __builtin_amdgcn_exp2f(ml[0] - top);
         l += ml[1] * x;
