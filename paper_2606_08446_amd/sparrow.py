@@ -1003,7 +1003,10 @@ def residual_norm_bwd(dy, dh_out, h_out, x, weight, post_weight=None, gate=None,
         dgs = _expect_matrix(dgate, "dgate", (T, C), dev)
     elif gate is not None:
         dgate = torch.empty_like(dy)
-    dweight = _given(dweight, "dweight", torch.float32, (C,), dev)
+    if dweight is None:
+        dweight = torch.empty_like(weight, dtype=torch.float32)
+    else:
+        _expect(dweight, "dweight", torch.float32, (C,), dev)
     if post_weight is not None:
         dpost_weight = _given_like(dpost_weight, "dpost_weight", dweight)
     if T == 0:
