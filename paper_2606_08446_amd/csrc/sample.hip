@@ -237,6 +237,27 @@ __device__ __forceinline__ double lane_64(double x, int lane)
 
 __device__ __forceinline__ double wave_sum_64(double x) { return lane_64(wave_scan_64(x), 63); }
 
+// The sum over the wave, in lane 63: within rows of 16 by exchanges that every lane takes part in, which need no
+// zero for the others.
+__device__ __forceinline__ double wave_total_64(double x)
+{
+    constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;
+    auto add = [](double v, auto ctrl) __attribute__((always_inline)) {
+        const u32x2_t b = __builtin_bit_cast(u32x2_t, v);
+        const u32x2_t o = {
+            (uint32_t)__builtin_amdgcn_mov_dpp((int)b[0], decltype(ctrl)::value, 0xf, 0xf, true),
+            (uint32_t)__builtin_amdgcn_mov_dpp((int)b[1], decltype(ctrl)::value, 0xf, 0xf, true)};
+        return v + __builtin_bit_cast(double, o);
+    };
+    x = add(x, std::integral_constant<int, kSwap1>());
+    x = add(x, std::integral_constant<int, kSwap2>());
+    x = add(x, std::integral_constant<int, kHalfMirror>());
+    x = add(x, std::integral_constant<int, kMirror>());
+    x += dpp_move_64<kDppRowBcast15, 0xa>(x);
+    x += dpp_move_64<kDppRowBcast31, 0xc>(x);
+    return x;
+}
+
 // A row's settings; off is k = 0, p = 1, q = 0.
 struct Filters {
     double c;  // log2(e) / T
@@ -277,21 +298,34 @@ __device__ __forceinline__ float max3(float x, float y, float z)
     return d;
 }
 
-// The maxima of four values over the wave, left in lane 63: the four scans take turns, so that no move reads
-// what one of the last two instructions wrote.  A lane without a source keeps its value.
-__device__ __forceinline__ void wave_max4(float (&x)[4])
+// max of two numbers, as max3 above.
+__device__ __forceinline__ float max2(float x, float y)
 {
-#define SPARROW_MAX4(move)                                             \
-    "v_max_f32_dpp %0, %0, %0 " move "\n v_max_f32_dpp %1, %1, %1 " move \
-    "\n v_max_f32_dpp %2, %2, %2 " move "\n v_max_f32_dpp %3, %3, %3 " move "\n "
-    asm("s_nop 1\n " SPARROW_MAX4("row_shr:1 row_mask:0xf bank_mask:0xf")
-        SPARROW_MAX4("row_shr:2 row_mask:0xf bank_mask:0xf")
-        SPARROW_MAX4("row_shr:4 row_mask:0xf bank_mask:0xf")
-        SPARROW_MAX4("row_shr:8 row_mask:0xf bank_mask:0xf")
-        SPARROW_MAX4("row_bcast:15 row_mask:0xa bank_mask:0xf")
-        SPARROW_MAX4("row_bcast:31 row_mask:0xc bank_mask:0xf")
-        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
-#undef SPARROW_MAX4
+    float d;
+    asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(x), "v"(y));
+    return d;
+}
+
+// The maxima of four values over the wave, in rows of 16 lanes: of x[0], x[2], x[1] and x[3].  Swaps of halves, then
+// of rows, bring two values into one register, whose parts are reduced together.  (A swap reads what an instruction
+// wrote two states ago at the latest; the compiler does not see those inside asm.)
+__device__ __forceinline__ float wave_max4(const float (&x)[4])
+{
+    auto halves = [](float a, float b) __attribute__((always_inline)) {
+        asm("s_nop 1" : "+v"(a), "+v"(b));
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    };
+    float a = halves(x[0], x[1]), b = halves(x[2], x[3]);
+    asm("s_nop 1" : "+v"(a), "+v"(b));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    float top = max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    asm("s_nop 1\n v_max_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n "
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xf\n "
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_ror:2 row_mask:0xf bank_mask:0xf\n "
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_ror:1 row_mask:0xf bank_mask:0xf"
+        : "+v"(top));
+    return top;
 }
 
 // The waves of a row's workgroups (blockIdx.y) take its spans in turn, the next one's loads under way.
@@ -346,20 +380,14 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
                     top[b] = max3(top[b], z[b][e], z[b][e + 1]);
                 top[b] = max3(top[b], z[b][kE - 1], top[b]);
             }
-            wave_max4(top);
-#pragma unroll
-            for (int b = 0; b < kSpanBlocks; ++b)
-                top[b] = fminf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top[b]), 63)),
-                               FLT_MAX);
-            const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            const float row_top = fminf(wave_max4(top), FLT_MAX);  // (its row's block's)
+            auto of_row = [&](int row) __attribute__((always_inline)) {
+                return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(row_top), 16 * row));
+            };
+            const float m = fmaxf(fmaxf(of_row(0), of_row(1)), fmaxf(of_row(2), of_row(3)));
             const int64_t at = row * st.spans + span;
-            if (lane < kSpanBlocks) {
-                float t = top[0];
-#pragma unroll
-                for (int b = 1; b < kSpanBlocks; ++b)
-                    t = lane == b ? top[b] : t;
-                st.maxima[at * kSpanBlocks + lane] = t;
-            }
+            if ((lane & 15) == 0)
+                st.maxima[at * kSpanBlocks + ((lane >> 4 & 1) * 2 + (lane >> 5))] = row_top;
             if (!sums)
                 continue;
             double sum = 0.;
@@ -388,8 +416,8 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
                         }
                 }
             }
-            sum = wave_sum_64(sum);
-            if (lane == 0)
+            sum = wave_total_64(sum);
+            if (lane == 63)
                 st.sums[at] = sum;
         }
     }
