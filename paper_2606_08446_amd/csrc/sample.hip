@@ -329,8 +329,8 @@ __device__ __forceinline__ float wave_max4(const float (&x)[4])
 }
 
 // The waves of a row's workgroups (blockIdx.y) take its spans in turn, the next one's loads under way.
-// Bound by arithmetic where sums are wanted (26 vector instructions a logit, 17 of them for its weight: 256 fp32
-// rows of 151936 in 40 us, 3.9 TB/s), else by memory.
+// Bound by arithmetic where sums are wanted (24 vector instructions a logit, 17 of them for its weight: 256 fp32
+// rows of 151936 in 38 us, 4.1 TB/s), else by memory.
 template <bool kBf16>
 __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Stats st)
 {
