@@ -380,7 +380,8 @@ __global__ __launch_bounds__(kStatThreads) void k_sample_stats(SampleArgs a, Sta
                     top[b] = max3(top[b], z[b][e], z[b][e + 1]);
                 top[b] = max3(top[b], z[b][kE - 1], top[b]);
             }
-            const float row_top = fminf(wave_max4(top), FLT_MAX);  // (its row's block's)
+            // (its row's block's, as unpack_whole has the logits: -0 is 0, whose key it would not have)
+            const float row_top = fminf(wave_max4(top), FLT_MAX) + 0.f;
             auto of_row = [&](int row) __attribute__((always_inline)) {
                 return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(row_top), 16 * row));
             };
