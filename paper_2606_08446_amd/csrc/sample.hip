@@ -742,7 +742,8 @@ struct RowPicker {
         double in_block = 0.;
 #pragma unroll
         for (int k = 0; k < kSpanBlocks; ++k) {
-            if (b < 0 && sum[k] > left) {
+            // (`left` may be below 0 by a rounding, which a block without a kept token does not take)
+            if (b < 0 && sum[k] > 0. && sum[k] > left) {
                 b = k;
                 in_block = left;
             }
