@@ -1016,7 +1016,8 @@ struct Picker : RowPicker<kBf16> {
         }
         const double run = block_scan_64(w[0] + w[1], s.red, total);
         const double at = u * total;
-        first_of(&s.found, 2 * t < keep && run - w[1] > at, 2 * t + 1 < keep && run > at);
+        // (a kept token of no weight: the sum at it may exceed by a rounding what the one before did not)
+        first_of(&s.found, w[0] > 0. && run - w[1] > at, w[1] > 0. && run > at);
         __syncthreads();
         if (t == 0) {
             const uint64_t k = s.sort.key[s.found];

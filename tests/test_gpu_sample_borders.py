@@ -46,3 +46,22 @@ def test_draw_on_a_border_before_a_masked_block(dtype):
     assert bool((c[rows, tok.long()] - w[rows, tok.long()] <= total * (0.5 + 1e-10)).all())
     want = drawn - total.log()
     assert bool(((lp.double() - want).abs() <= 2.0 ** -24 * want.abs() + 1e-11).all())
+
+
+def test_a_kept_token_of_no_weight_is_not_drawn():
+    # The same border among tokens that are sorted: two equal halves of 64, the first token of each, and some others,
+    # so far below the rest that their weights are 0 in 64 bits.  They stay in top-k, and may not be drawn.
+    T, V = 600, 200
+    log("case sample border of kept tokens")
+    g = torch.Generator().manual_seed(6)
+    half = torch.randn((T, 64), generator=g)
+    half[torch.rand((T, 64), generator=g) < 0.2] = -3e4
+    half[:, 0] = -3e4
+    z = torch.full((T, V), -math.inf)
+    z[:, :128] = torch.cat([half, half], 1)
+    u = torch.full((T,), 0.5)
+    for kw in (dict(top_k=torch.full((T,), 128, dtype=torch.int32)), dict(top_p=torch.full((T,), 0.999999))):
+        tok, lp = (t.cpu() for t in S.sample(z.to(DEV), u.to(DEV), **{k: v.to(DEV) for k, v in kw.items()}))
+        drawn = z.double()[torch.arange(T), tok.long()]
+        assert bool((drawn > -1e4).all()), (list(kw), torch.nonzero(drawn <= -1e4).flatten().tolist()[:8])
+        assert bool(lp.isfinite().all())
