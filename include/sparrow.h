@@ -361,8 +361,8 @@ int sparrow_dense_decode_attn(const sparrow_shape_t *shape, const void *q, const
  * Groups of one sequence, and sequences in no group, share nothing.  With that the result is
  * sparrow_dense_decode_attn's,
  *     out[b][j] = sum_t w_t V[t],  w = softmax(scale * q[b][j] . K[t]) over t < seq_lens[b]
- * with fp32 sums; the softmax numerators enter the product with V as bf16 for SPARROW_OUT_BF16 and
- * with all of their 24 bits for SPARROW_OUT_F32.  An empty sequence gives a zero row.  The order of the
+ * with fp32 sums and fp32 softmax numerators (all of their 24 bits enter the product with V), rounded once
+ * for SPARROW_OUT_BF16.  An empty sequence gives a zero row.  The order of the
  * sums depends only on the shape, the groups, the lengths and the device.  Tokens that no sequence of a
  * group reaches may hold anything; where a shared V row that some sequences reach is not finite, sequences
  * of the group that end before it may get NaN as well.

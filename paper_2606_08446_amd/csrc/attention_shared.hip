@@ -19,8 +19,9 @@
 //   O^T[d][row] += sum_t V[t][d] p[t][row]       - 8 x mfma_f32_16x16x32_bf16, whose 32 terms are
 //           taken in the order the logits left them in: lane group lg has tokens 4 lg + j of the first
 //           half, then of the second.  V rows are loaded 8 channels a lane, tile c takes element c.
-// The softmax numerators enter the second product as bf16 for bf16 outputs (half a step of the output's
-// own type each) and as three bf16 terms, all of their 24 bits, for fp32 ones.
+// The softmax numerators enter the second product as three bf16 terms, which is all of their 24 bits, for
+// either type of output: a bf16 one is the fp32 one rounded once.  The matrix cores have the time: with one
+// term 866 instead of 872 us (16 groups of 16), 54 instead of 55 (7 uneven ones), 15.0 instead of 15.1 (8 short samples).
 //
 // Bound by memory: 16 groups of 16 sequences with 8K-16K shared and up to 8K own tokens read 5.46 GB in 850 us,
 // 6.4 TB/s (8 x 8 of up to 4K + 4K: 627 MB in 105 us, 6.0 TB/s); the merge takes 5-9 us more.  What a group costs
@@ -42,6 +43,7 @@ constexpr int kSharedWaves = kSharedThreads / 64;
 constexpr int kTileTokens = 32;
 constexpr int kRows = 16;       // query rows of a wave
 constexpr int kTeamRows = kRows * kSharedWaves;
+constexpr int kTerms = 3;       // bf16 terms of a softmax numerator
 constexpr float kNoLogit = -FLT_MAX;  // a part's maximum before its first token
 
 struct SharedArgs {
@@ -387,7 +389,6 @@ __device__ __forceinline__ float over_groups(float x, Op op)
 }
 
 // 16 query rows of a part at work, by one wave.
-template <int kTerms>
 struct Rows {
     const SharedArgs &a;
     const int lane, lr, lg, G;
@@ -468,18 +469,13 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             float x0 = __builtin_amdgcn_exp2f(z[e] - m_new), x1 = __builtin_amdgcn_exp2f(z[e + 1] - m_new);
-            if (kTerms > 1)
-                sum += x0 + x1;
+            sum += x0 + x1;
 #pragma unroll
             for (int k = 0; k < kTerms; ++k) {
                 const uint32_t b = pack_bf16(x0, x1);
                 p[k][e >> 1] = b;
-                if (kTerms == 1) {
-                    sum += bf16_lo(b) + bf16_hi(b);  // (the weights as they are used)
-                } else {
-                    x0 -= bf16_lo(b);
-                    x1 -= bf16_hi(b);
-                }
+                x0 -= bf16_lo(b);
+                x1 -= bf16_hi(b);
             }
         }
         l = l * alpha + sum;
@@ -524,11 +520,10 @@ struct Rows {
 
 // A wave's way through its sequences: the loads of the next tile, the next part's first one too, are always
 // under way, and the next part's block-table entries with them.
-template <int kTerms>
 struct Stream {
     const SharedArgs &a;
     Walk<false> walk;
-    Rows<kTerms> work;
+    Rows work;
     Part load, next;  // the part whose tiles are being loaded, the one behind it
     bool have_next;
     Window win, win_next;
@@ -619,13 +614,12 @@ static_assert(2 * kTileChunks * 16 >= kMaxGroups * sizeof(int32_t), "the plan's 
 static_assert(2 * kTileChunks * 16 + plan_lds(kMaxBatch, kMaxGroups) + 1024 <= 160 << 10,
               "LDS of a workgroup");
 
-template <int kTerms>
 struct Team {
     const SharedArgs &a;
     u32x4_t *s_tile;
     const int wave;
     Walk<true> ahead, walk;
-    Rows<kTerms> work;
+    Rows work;
     Part load, next, u;  // being loaded, behind that one, at work
     bool have_next;
     Window win, win_next;
@@ -755,7 +749,6 @@ __device__ __forceinline__ int place_by_xcd(int block, int n)
     return n % kXcds ? block : block % kXcds * (n / kXcds) + block / kXcds;
 }
 
-template <int kTerms>
 __global__ __launch_bounds__(kSharedThreads, 2) void k_shared_stream(SharedArgs a)
 {
     extern __shared__ int32_t s_plan[];
@@ -779,13 +772,13 @@ __global__ __launch_bounds__(kSharedThreads, 2) void k_shared_stream(SharedArgs 
     const uint32_t place = place_by_xcd(blockIdx.x - (late ? half : 0), mine), before = place * n / mine;
     if ((place + 1) * n / mine > before) {
         const uint32_t w = (late ? half : 0) + before;
-        Team<kTerms> team(a, Walk<true>(a, plan, w, Share(P1, w1)), s_tile);
+        Team team(a, Walk<true>(a, plan, w, Share(P1, w1)), s_tile);
         team.run();
     } else {
         const uint32_t w = ((late ? half - min(w1, half) : 0) + place - before) * kSharedWaves +
                            __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (w < sides.w2) {
-            Stream<kTerms> stream(a, Walk<false>(a, plan, w, Share(P2, sides.w2)));
+            Stream stream(a, Walk<false>(a, plan, w, Share(P2, sides.w2)));
             stream.run();
         }
     }
@@ -983,8 +976,7 @@ hipError_t launch_shared_attention(const sparrow_shape_t &s, const Groups &g, co
     for (a.step_log2 = 0; ((tiles >> a.step_log2) + 1 + kPartCost) * units > 0x7fffffff;)
         ++a.step_log2;
     const size_t lds = plan_lds(s.batch, g.n);
-    auto kernel = a.out_bf16 ? k_shared_stream<1> : k_shared_stream<3>;
-    hipLaunchKernelGGL(kernel, dim3(shared_blocks(device_cus())), dim3(kSharedThreads), lds, stream, a);
+    hipLaunchKernelGGL(k_shared_stream, dim3(shared_blocks(device_cus())), dim3(kSharedThreads), lds, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
