@@ -20,8 +20,8 @@
 //           taken in the order the logits left them in: lane group lg has tokens 4 lg + j of the first
 //           half, then of the second.  V rows are loaded 8 channels a lane, tile c takes element c.
 // The softmax numerators enter the second product as three bf16 terms, which is all of their 24 bits, for
-// either type of output: a bf16 one is the fp32 one rounded once.  The matrix cores have the time: with one
-// term 866 instead of 872 us (16 groups of 16), 54 instead of 55 (7 uneven ones), 15.0 instead of 15.1 (8 short samples).
+// either type of output: a bf16 one is the fp32 one rounded once.  The matrix cores have the time: with one term
+// 16 groups of 16 took 866 instead of 872 us, 7 uneven ones 54 instead of 55, 8 short samples 15.0 instead of 15.1.
 //
 // Bound by memory: 16 groups of 16 sequences with 8K-16K shared and up to 8K own tokens read 5.46 GB in 850 us,
 // 6.4 TB/s (8 x 8 of up to 4K + 4K: 627 MB in 105 us, 6.0 TB/s); the merge takes 5-9 us more.  What a group costs
@@ -893,7 +893,8 @@ __global__ __launch_bounds__(kSharedThreads) void k_shared_merge(SharedArgs a)
             sum += s_o[here][k][i];
             den += s_l[here][k];
         }
-        store_out(a.out, a.out_bf16, (int64_t)row * kHeadDim + i, den > 0.f ? sum / den : 0.f);
+        // (0: no token; NaN, from a logit that is no number, is a row's result)
+        store_out(a.out, a.out_bf16, (int64_t)row * kHeadDim + i, den == 0.f ? 0.f : sum / den);
     }
 }
 
