@@ -363,9 +363,8 @@ int sparrow_dense_decode_attn(const sparrow_shape_t *shape, const void *q, const
  *     out[b][j] = sum_t w_t V[t],  w = softmax(scale * q[b][j] . K[t]) over t < seq_lens[b]
  * with fp32 sums and fp32 softmax numerators (all of their 24 bits enter the product with V), rounded once
  * for SPARROW_OUT_BF16.  An empty sequence gives a zero row.  The order of the
- * sums depends only on the shape, the groups, the lengths and the device.  Tokens that no sequence of a
- * group reaches may hold anything; where a shared V row that some sequences reach is not finite, sequences
- * of the group that end before it may get NaN as well.
+ * sums depends only on the shape, the groups, the lengths and the device.  What lies behind a
+ * sequence's end may hold anything, the shared tokens that only longer sequences of its group reach too.
  *
  * Arguments: as for sparrow_dense_decode_attn, batch * num_kv_heads <= 65535; 0 <= num_groups <=
  * SPARROW_MAX_GROUPS; cu_groups (device int32 [num_groups + 1], non-decreasing; entries outside [0,

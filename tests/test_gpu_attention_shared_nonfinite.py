@@ -49,3 +49,29 @@ def test_logits_that_are_no_number(where, dtype):
         got, other = S.shared_prefix_decode_attn(*c.args(), out_dtype=dtype), dense(c, dtype)
         assert torch.equal(got.isnan().cpu(), hit[..., None].expand(-1, -1, D))
         assert where == "query" or torch.equal(got.isnan(), other.isnan())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("hq,hkv,ps", [(8, 2, 16), (2, 1, 32), (32, 2, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_sequences_that_end_before_a_v_that_is_not_finite(bad, hq, hkv, ps, dtype):
+    # the shared tokens from `at` on; sequences that end before are as without it, the others hold it
+    for at in (0, 1, 5, 31, 32, 100, 170):
+        log(f"case shared V={bad} at={at} heads={hq},{hkv} ps={ps} out={dtype}")
+        lens = [200, at, 195, max(0, at - 1), 192 + at % 7, at // 2, at + 1, 0, at, 300]
+        c = Case([9, 1], [192, 10], lens, hq, hkv, ps, seed=at)
+        want, size, most = c.reference(1 / math.sqrt(D))
+        c.v[int(c.full[0, at // ps]), :, at % ps, ::3] = bad
+        if at % 2:
+            c.v[int(c.full[0, 180 // ps]), 0, 180 % ps, 7] = -bad
+        got = S.shared_prefix_decode_attn(*c.args(), out_dtype=dtype)
+        other = dense(c, dtype)
+        before = [b for b, n in enumerate(lens) if n <= at or b == 9]
+        tol = (2 * 2 ** -17.5 * most + 2 ** -14) * size + 1e-30
+        if dtype == BF16:
+            tol = tol + 2 ** -7 * size + 2 ** -8 * want.abs()
+        assert bool(((got.cpu().double() - want).abs() <= tol)[before].all())
+        # (a weight of 0 times an infinite V is no number on either side, so weights matter only as far as that)
+        behind = [b for b in range(10) if b not in before]
+        assert torch.equal(got[behind].isfinite(), other[behind].isfinite())
+        assert not bool(got[behind][..., ::3].isfinite().any())
