@@ -454,6 +454,18 @@ def _require_device(t):
         raise RuntimeError("libsparrow runs on the GPU only: tensors must be on a HIP device")
 
 
+def _refuse_recorded(name, *tensors, instead=""):
+    """Raise if autograd records a gradient or carries a tangent for any of the tensors: the library would
+    drop it without a word."""
+    import torch
+    forward = torch.autograd.forward_ad
+    if (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)) or \
+            (forward._current_level >= 0 and
+             any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors)):
+        raise ValueError(f"{name} records no gradient: call it under torch.no_grad() or on detached "
+                         f"tensors{instead}")
+
+
 def _expect(t, name, dtype, shape, device):
     """Raise unless ``t`` is a contiguous tensor on ``device`` with exactly this dtype and shape.
 
@@ -669,8 +681,10 @@ def shared_prefix_decode_attn(q, k_cache, v_cache, block_table, seq_lens, cu_gro
     """Dense paged decode attention for groups of sequences with the same first tokens.  Group g is the
     sequences ``cu_groups[g] .. cu_groups[g+1]-1`` (int32 ``[groups + 1]``) and shares the whole pages of
     its ``prefix_lens[g]`` first tokens (int32 ``[groups]``), which are read once, from the pages of its
-    first sequence.  Returns out [B][Hq][D] (fp32 or bf16)."""
+    first sequence.  Returns out [B][Hq][D] (fp32 or bf16).  Inputs that a gradient is recorded for are
+    refused."""
     import torch
+    _refuse_recorded("shared_prefix_decode_attn", q, k_cache, v_cache)
     B, Hq, Hkv, ps, D, P, M = _expect_cache(q, k_cache, v_cache, block_table, seq_lens)
     if prefix_lens.dim() != 1:
         raise ValueError("prefix_lens must be [groups]")
@@ -775,8 +789,9 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     the row's uniform number (fp32 ``[T]``) from what temperature, top-k, top-p and min-p (``[T]``,
     fp32; top_k int32) leave of its distribution.  Returns (tokens int32 ``[T]``, logprobs fp32
     ``[T]``: the log-probability that each was drawn with); a row with every token masked gives -1 and
-    -inf."""
+    -inf.  Inputs that a gradient is recorded for are refused: the log-probabilities carry none."""
     import torch
+    _refuse_recorded("sample", logits, uniform, temperature, top_p, min_p)
     _require_device(logits)
     if logits.dim() != 2:
         raise ValueError("logits must be [T][V]")
@@ -863,10 +878,8 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, positions, eps=1e-6, q_out=
     autograd node: ``qk_norm_rope_bwd`` is its gradient, and inputs that a gradient is recorded for
     are refused."""
     import torch
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight.requires_grad or
-                                    k_weight.requires_grad):
-        raise ValueError("qk_norm_rope records no gradient: call it under torch.no_grad() or on "
-                         "detached tensors, and qk_norm_rope_bwd for the gradient")
+    _refuse_recorded("qk_norm_rope", q, k, q_weight, k_weight,
+                     instead=", and qk_norm_rope_bwd for the gradient")
     T, Hq, Hk, D, qs, ks = _expect_rope(q, k, q_weight, k_weight, inv_freq, positions)
     dev = q.device
     q_out = _given_like(q_out, "q_out", q)
@@ -952,10 +965,8 @@ def residual_norm(h, x, weight, post_weight=None, gate=None, scale=1.0, eps=1e-6
     h' is h itself.  Returns (h', y); h_out may be h.  No autograd node: ``residual_norm_bwd`` is its
     gradient, and inputs that a gradient is recorded for are refused."""
     import torch
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
-                                       for t in (h, x, weight, post_weight, gate)):
-        raise ValueError("residual_norm records no gradient: call it under torch.no_grad() or on "
-                         "detached tensors, and residual_norm_bwd for the gradient")
+    _refuse_recorded("residual_norm", h, x, weight, post_weight, gate,
+                     instead=", and residual_norm_bwd for the gradient")
     T, C, dt, xs, gs = _expect_norm(h, x, weight, post_weight, gate)
     dev = h.device
     if x is None:
@@ -981,8 +992,10 @@ def residual_norm_bwd(dy, dh_out, h_out, x, weight, post_weight=None, gate=None,
     dweight, dpost_weight), dh in the stream's type, dx and dgate bf16 (they may be views into one
     buffer), the weights' fp32 ``[C]``; None for what the call has no input of.  dh_out None is zero.
     ``block=False`` says that there was no x: dx is None.  x may be None where it is not needed, with
-    neither post_weight nor gate.  dh may be dh_out."""
+    neither post_weight nor gate.  dh may be dh_out.  No second derivatives: inputs that a gradient is
+    recorded for are refused (inside an autograd node's backward none is, without create_graph)."""
     import torch
+    _refuse_recorded("residual_norm_bwd", dy, dh_out, h_out, x, weight, post_weight, gate)
     T, C, dt, xs, gs = _expect_norm(h_out, x, weight, post_weight, gate)
     dev = h_out.device
     if (post_weight is not None or gate is not None) and (x is None or not block):
