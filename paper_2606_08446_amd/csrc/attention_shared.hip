@@ -23,8 +23,8 @@
 // either type of output: a bf16 one is the fp32 one rounded once.  The matrix cores have the time: with one term
 // 16 groups of 16 took 866 instead of 872 us, 7 uneven ones 54 instead of 55, 8 short samples 15.0 instead of 15.1.
 //
-// Bound by memory: 16 groups of 16 sequences with 8K-16K shared and up to 8K own tokens read 5.46 GB in 850 us,
-// 6.4 TB/s (8 x 8 of up to 4K + 4K: 627 MB in 105 us, 6.0 TB/s); the merge takes 5-9 us more.  What a group costs
+// Bound by memory: 16 groups of 16 sequences with 8K-16K shared and up to 8K own tokens read 5.46 GB in 858 us,
+// 6.4 TB/s (8 x 8 of up to 4K + 4K: 627 MB in 104 us, 6.0 TB/s); the merge takes 5-9 us more.  What a group costs
 // is decided by how often its tiles reach a compute unit: the same call took 1228 us with waves that each read
 // them for 16 rows, and 1833 with waves that held all of a unit's rows.
 #include "attention_shared.h"
@@ -64,9 +64,7 @@ struct SharedArgs {
 };
 
 // How many workgroups take the groups' positions (P1 of them) and how many waves the sequences' (P2): all of
-// the launch's, or where that would be less than min_tiles each, fewer.  kTeamCost is a position's time in a
-// workgroup on a group against that of one in four waves on sequences.
-constexpr float kTeamCost = 1.f;
+// the launch's, in proportion, or where that would be less than min_tiles each, fewer.
 struct Sides {
     uint32_t w1, w2;
     __device__ __forceinline__ Sides(const SharedArgs &a, uint32_t P1, uint32_t P2, uint32_t blocks)
@@ -74,7 +72,7 @@ struct Sides {
         w1 = (P1 + a.min_tiles - 1) / a.min_tiles;
         w2 = (P2 + a.min_tiles - 1) / a.min_tiles;
         if (w1 + (w2 + kSharedWaves - 1) / kSharedWaves > blocks) {
-            const float c1 = kTeamCost * (float)P1;
+            const float c1 = (float)P1;
             uint32_t n = (uint32_t)(c1 / (c1 + (float)P2) * blocks + 0.5f);
             n = P1 ? max(n, 1u) : 0u;
             n = P2 ? min(n, blocks - 1) : blocks;
@@ -974,7 +972,9 @@ constexpr int kMaxCus = 256;
 
 int shared_blocks(int cus) { return (cus < kMaxCus ? cus : kMaxCus) * 2; }
 
-constexpr int kNarrowRows = 1024;  // query heads and sequences from which a wave merges each
+// Query heads and sequences from which a wave merges each.  (Four waves and one, whole calls: 128 of them 15.1 and
+// 19.3 us, 512 20.0 and 21.4, 1024 23.2 and 23.3, 2048 35.6 and 34.2, 5120 60.0 and 54.2.)
+constexpr int kNarrowRows = 1024;
 
 struct SharedPlan {
     size_t plan_bytes, group_slots, seq_slots, bytes;
@@ -1029,6 +1029,8 @@ hipError_t launch_shared_attention(const sparrow_shape_t &s, const Groups &g, co
     a.out = out;
     a.out_bf16 = out_dtype == SPARROW_OUT_BF16;
     a.scale_log2 = scale * 1.4426950408889634f;
+    // (with 1, 2, 4 and 8: 8 samples of 2001 shared tokens 16.2, 15.1, 14.9 and 18.2 us, of 500 12.1, 12.7, 14.3 and
+    // 18.5, one sequence of 4096 20.6, 16.3, 18.6 and 24.4; calls that fill the device do not feel it)
     a.min_tiles = 2;
     char *ws = static_cast<char *>(workspace);
     a.plan_off = reinterpret_cast<int32_t *>(ws);

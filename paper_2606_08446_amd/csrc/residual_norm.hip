@@ -170,8 +170,11 @@ template <int kVecs_, int kThreads_, bool kF32_, bool kPost_, bool kGate_, bool 
 struct NormKind {
     static constexpr int kVecs = kVecs_, kThreads = kThreads_, kWaves = kThreads_ / 64;
     static constexpr bool kF32 = kF32_, kPost = kPost_, kGate = kGate_, kX = kPost_ || kGate_, kNt = kNt_;
-    // 1024 threads, of 128 registers each, keep the gradient's weight sums in LDS and no second row (8192 x
-    // 16384: 624 us; with the sums in registers, of which many are spilled, 1057)
+    // 1024 threads, of 128 registers each, keep the gradient's weight sums in LDS and no second row: 8192 x 16384
+    // in 691 us with norm and gate, 502 without the gate, 404 without the norm, 244 without both; with sums and a
+    // second row in registers, of which many more are spilled, 1357, 1083, 632 and 346.  As it is, 42 to 55
+    // registers are spilled with a norm behind the block, up to 12 without.  (Of the smaller forms one spills, 8:
+    // one vector, fp32 stream, norm and gate.)
     static constexpr bool kSumsInLds = kThreads > 512;
 };
 
@@ -612,7 +615,9 @@ void with_kind(const NormArgs &a, bool grad, bool past_caches, Launch launch)
 
 int norm_grad_blocks(int64_t tokens, int channels)
 {
-    // as many as the device holds at once: 4 waves a SIMD, 2 where a thread has 256 registers
+    // As many as the device holds at once: 4 waves a SIMD, 2 for the two vectors of up to 512 threads, whose forms
+    // have 140 to 255 registers.  (3 for those too took longer also where they would fit, without a norm behind
+    // the block: 32768 x 4096, gated, 414 us instead of 391, 1021 x 5120 27 instead of 20.)
     const int threads = norm_threads(channels, true);
     const int waves = norm_vecs(channels, true) == 2 && threads <= 512 ? 8 : 16;
     const int64_t b = 256 * (waves * 64 / threads < 8 ? waves * 64 / threads : 8);
